@@ -1,0 +1,60 @@
+/*
+ * w4a16_mx.h -- C ABI of the library's operators on microscaled 4-bit floating point weights (MXFP4), and of a
+ * mixture-of-experts layer on such weights.  Part of libw4a16.so, beside w4a16.h, whose status codes,
+ * w4a16_status_string and w4a16_last_hip_error serve here too.
+ *
+ * Format (OCP microscaling): 32 consecutive values of a row are a block; an element is e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6
+ * and their negatives), the block's scale e8m0:
+ *
+ *   codes   uint8 [rows, K/2]   the code of an even k is the low nibble; bit 3 of a code is the sign
+ *   scales  uint8 [rows, K/32]  s stands for 2^(s - 127); s = 255: the block's values are NaN
+ *
+ * K is a multiple of 32; rows may be any number.
+ *
+ * All data pointers are DEVICE pointers owned by the caller.  Codes, X and Y of the quantizer and X of the products are
+ * 16-byte aligned, and so is every row of an X with a leading dimension (ld: values from a row to the next).  Scales, ids,
+ * weights and the products' Y need no more than their type's alignment.  Calls only enqueue work on `stream` (a hipStream_t, NULL
+ * = the default stream); none allocates, waits or keeps anything, so all may be captured into a HIP graph, and calls
+ * on different streams may overlap (w4a16_moe_experts: each with its own workspace).  No rows (M, rows or T = 0):
+ * W4A16_OK, nothing is launched.
+ *
+ * Errors: a w4a16_status; on any error nothing is launched.  Results are bitwise reproducible for fixed arguments.
+ */
+#ifndef W4A16_MX_H
+#define W4A16_MX_H
+
+#include "w4a16.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+typedef enum { W4A16_F16 = 0, W4A16_BF16 = 1, W4A16_F32 = 2 } w4a16_dtype;
+
+/*
+ * Quantizes X [rows, K] of type `dtype` (FP16, BF16 or FP32).  Per block, with a = max |x|: s = 127 + clamp(floor(log2 a) - 2,
+ * -127, 127); each element is x / 2^(s - 127) rounded to the nearest element, ties to the even code, beyond 6 to +-6.  A block of
+ * zeros gets s = 0 (its codes keep the signs); one with an infinity or a NaN gets s = 255 and codes 0.  Every byte of codes and
+ * scales is overwritten.
+ */
+int w4a16_mx_quantize(const void *X, int dtype, long long rows, int K, long long ldx, uint8_t *codes, uint8_t *scales, void *stream);
+
+/* The way back: X[r, k] = element * 2^(s - 127), rounded to nearest even where `dtype` has no such number. */
+int w4a16_mx_dequantize(const uint8_t *codes, const uint8_t *scales, long long rows, int K, void *X, int dtype, long long ldx,
+                        void *stream);
+
+/*
+ * Y[M, N] = X[M, K] W[N, K]^T, W in MXFP4, X and Y both FP16 or both BF16 (`dtype`); FP32 sums, one rounding.  X's elements
+ * and the weights enter the products exactly.
+ */
+int w4a16_mx_gemm(const void *X, int dtype, long long ldx, const uint8_t *codes, const uint8_t *scales, int M, int N, int K, void *Y,
+                  long long ldy, void *stream);
+
+/* The same with X in MXFP4 too (w4a16_mx_quantize's output); Y is FP16 or BF16 (`dtype`). */
+int w4a16_mx_gemm_mx(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *codes, const uint8_t *scales, int M, int N, int K,
+                     void *Y, int dtype, long long ldy, void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* W4A16_MX_H */

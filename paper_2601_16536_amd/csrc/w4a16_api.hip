@@ -4,6 +4,7 @@
 // management and dispatch to the kernel launchers.
 #include "../../include/w4a16.h"
 #include "w4a16_internal.h"
+#include "w4a16_mx.h"
 
 #include <cstdio>
 #include <cstdlib>
@@ -911,6 +912,18 @@ int run(const char *entry, const void *X, const uint32_t *Wp, const void *scales
 
 }  // namespace
 
+namespace w4a16 {
+
+void clear_hip_error() { t_hip_error[0] = 0; }
+int hip_status(hipError_t e)
+{
+    if (e == hipSuccess) return W4A16_OK;
+    note_hip_error(e);
+    return W4A16_ERR_HIP;
+}
+
+}  // namespace w4a16
+
 extern "C" {
 
 int w4a16_gemm(const void *X, const uint32_t *Wpacked, const void *scales, const uint32_t *zeros, int group, int M,
@@ -1069,7 +1082,7 @@ const char *w4a16_status_string(int status)
     switch (status) {
     case W4A16_OK: return "ok";
     case W4A16_ERR_NULL: return "null pointer";
-    case W4A16_ERR_SHAPE: return "bad shape (need M >= 1, N % 8 == 0, K % 8 == 0)";
+    case W4A16_ERR_SHAPE: return "bad shape (need M >= 1, N % 8 == 0, K % 8 == 0; MXFP4: K % 32 == 0)";
     case W4A16_ERR_GROUP: return "bad group (need group % 32 == 0 and K % group == 0)";
     case W4A16_ERR_ALIGN: return "pointer not aligned (16 bytes for data, 256 for a workspace)";
     case W4A16_ERR_WORKSPACE: return "workspace too small, or it would have to be allocated while the stream is being captured, or allocation failed";

@@ -1,0 +1,213 @@
+// Device-side pieces shared by the kernels on microscaled 4-bit weights (MXFP4): the format's conversions and the step of the
+// products that a wave makes by itself.
+//
+// Format: 32 values of a row of K are a block; an element is e2m1 (sign, two exponent bits, one fraction bit: 0, 0.5, 1, 1.5, 2, 3,
+// 4, 6), a block's scale e8m0 (2^(s - 127); 255: the block is not a number).  Codes [rows, K/2] bytes, the even k in the low nibble;
+// scales [rows, K/32] bytes.  A binary32 whose exponent field is s is the scale operand that gfx950's conversions take: they read
+// the field alone, 0 as 2^-127 and 255 as NaN, and their results are exact, subnormal ones too, or rounded to nearest even.
+#pragma once
+#include "w4a16_device.h"
+
+namespace w4a16 {
+
+typedef __bf16 bfloat2_t __attribute__((ext_vector_type(2)));
+typedef float float2_t __attribute__((ext_vector_type(2)));
+typedef int int8_vec_t __attribute__((ext_vector_type(8)));
+
+constexpr int kMxBlock = 32;    // values that share a scale
+constexpr int kMxStep = 128;    // k per step of a product: four blocks
+constexpr int kMxStepBlocks = kMxStep / kMxBlock;
+
+__device__ __forceinline__ float scale_operand(uint32_t s) { return __builtin_bit_cast(float, s << 23); }
+
+// The scale as a number: the conversion of the code of 1.
+__device__ __forceinline__ float scale_value(uint32_t s) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(0x2u, scale_operand(s), 0)[0]; }
+
+// Eight codes of one block (a word) -> eight bfloat16, scaled, or eight FP16 element values without the scale.
+__device__ __forceinline__ uint4_t words_bf16(uint32_t w, float scale)
+{
+    return (uint4_t){__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3))};
+}
+__device__ __forceinline__ uint4_t words_f16(uint32_t w, float scale)
+{
+    return (uint4_t){__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 0)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 1)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 2)),
+                     __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(w, scale, 3))};
+}
+
+// Lane (c, p) (c = lane mod 16, p = lane / 16) holds the 16 bytes of block p of row c; afterwards word j of lane (c, p) is word p of
+// block j: a 4 x 4 transposition among the four lanes of a row, in four instructions.  One MFMA of 32 k is then one block of every row.
+__device__ __forceinline__ void blocks_to_words(uint4_t &w)
+{
+    auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false);
+    auto b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false);
+    auto d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    w = (uint4_t){c[0], c[1], d[0], d[1]};
+}
+
+// ---- the formats of X ----
+//
+// 16-bit X: A operand of MFMA j of a step: lane (row, p) holds X[row, 32 j + 8 p .. + 8].
+//   BF16: the scale goes into the weights' operand, exactly (a scaled element is a bfloat16 wherever it is a binary32).
+//   FP16: a scaled element need not be an FP16 number, so the operand is the element alone and the block's sum of products is
+//   multiplied by the scale in FP32: four FMAs per MFMA instead of none.
+// MXFP4 X: one MFMA per step that takes both operands' codes and scales as they are stored.
+struct MxBF16 {
+    static constexpr bool kMx = false;
+    static constexpr int kOut = 1;
+    static __device__ __forceinline__ uint4_t operand(uint32_t w, uint32_t s) { return words_bf16(w, scale_operand(s)); }
+    static __device__ __forceinline__ float4_t multiply(uint4_t x, uint4_t b, uint32_t, float4_t acc)
+    {
+        return ActBF16::mfma(ActBF16::x_operand(x), ActBF16::x_operand(b), acc);
+    }
+};
+struct MxF16 {
+    static constexpr bool kMx = false;
+    static constexpr int kOut = 0;
+    static __device__ __forceinline__ uint4_t operand(uint32_t w, uint32_t) { return words_f16(w, 1.0f); }
+    static __device__ __forceinline__ float4_t multiply(uint4_t x, uint4_t b, uint32_t s, float4_t acc)
+    {
+        const float4_t p = ActF16::mfma(ActF16::x_operand(x), ActF16::x_operand(b), (float4_t){0.f, 0.f, 0.f, 0.f});
+        const float f = scale_value(s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] = __builtin_fmaf(f, p[i], acc[i]);
+        return acc;
+    }
+};
+struct MxFP4 {
+    static constexpr bool kMx = true;
+    static __device__ __forceinline__ float4_t multiply(uint4_t x, uint32_t xs, uint4_t w, uint32_t ws, float4_t acc)
+    {
+        const int8_vec_t a = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}, b = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
+        return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 4, 4, 0, (int)xs, 0, (int)ws);
+    }
+};
+
+// What a wave's product reads.  The pointers are the same in every lane; a lane adds its offsets (32 bits):
+//   w: codes of its row of W (row lane mod 16 of a tile) plus 16 (lane / 16);  s: that row's scales, for MXFP4 X plus lane / 16;
+//   x: its row of X plus 16 (lane / 16) bytes;                                xs (MXFP4 X): that row's scales plus lane / 16.
+template <int CT, int MT>
+struct MxOperands {
+    const uint8_t *w, *s, *x, *xs;
+    uint32_t wo[CT], so[CT], xo[MT], xso[MT];
+};
+
+// acc[t][m] += X (16 rows m) W^T (16 rows of W t) over the steps first, first + stride, ... of K = 32 blocks values; acc in the layout of
+// the 16 x 16 MFMAs: lane (c, p) holds column c, rows 4 p .. 4 p + 3.  DEPTH steps are in flight.  SCALES4: the four scales of a whole
+// step are an aligned word (whole steps only, K % 128 == 0).
+template <class Op, int CT, int MT, bool SCALES4, int DEPTH>
+__device__ __forceinline__ void mx_product(float4_t (&acc)[CT][MT], const MxOperands<CT, MT> &o, int blocks, int first, int stride)
+{
+    constexpr int kXWords = Op::kMx ? 1 : 4;
+    struct Step {
+        uint4_t w[CT], x[MT][kXWords];
+        uint32_t s[CT], xs[MT];
+    };
+    const int part = (int)(threadIdx.x & 63) >> 4;
+    const int whole = blocks / kMxStepBlocks, rest = blocks % kMxStepBlocks;
+    const int n = whole > first ? (whole - first + stride - 1) / stride : 0;
+
+    auto load = [&](Step &f, int c) {
+        const uint8_t *const w = o.w + (size_t)c * 64, *const s = o.s + (size_t)c * 4, *const x = o.x + (size_t)c * (Op::kMx ? 64 : 256);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            f.w[t] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(w + o.wo[t]));
+            if constexpr (Op::kMx) f.s[t] = s[o.so[t]];
+            else if constexpr (SCALES4) f.s[t] = *reinterpret_cast<const uint32_t *>(s + o.so[t]);
+            else f.s[t] = (uint32_t)s[o.so[t]] | (uint32_t)s[o.so[t] + 1] << 8 | (uint32_t)s[o.so[t] + 2] << 16 | (uint32_t)s[o.so[t] + 3] << 24;
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+#pragma unroll
+            for (int j = 0; j < kXWords; ++j) f.x[m][j] = *reinterpret_cast<const uint4_t *>(x + o.xo[m] + j * 64);
+            if constexpr (Op::kMx) f.xs[m] = (o.xs + (size_t)c * 4)[o.xso[m]];
+        }
+    };
+    auto compute = [&](Step &f, int nb) {
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            if constexpr (Op::kMx) {
+#pragma unroll
+                for (int m = 0; m < MT; ++m) acc[t][m] = Op::multiply(f.x[m][0], f.xs[m], f.w[t], f.s[t], acc[t][m]);
+            } else {
+                blocks_to_words(f.w[t]);
+#pragma unroll
+                for (int j = 0; j < kMxStepBlocks; ++j) {
+                    if (j >= nb) break;
+                    const uint32_t s = (f.s[t] >> (8 * j)) & 0xFFu;
+                    const uint4_t b = Op::operand(f.w[t][j], s);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) acc[t][m] = Op::multiply(f.x[m][j], b, s, acc[t][m]);
+                }
+            }
+        }
+    };
+
+    Step f[DEPTH];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (d < n) load(f[d], first + d * stride);
+    int i = 0;
+    for (; i + 2 * DEPTH <= n; i += DEPTH)
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            compute(f[d], kMxStepBlocks);
+            load(f[d], first + (i + d + DEPTH) * stride);
+        }
+    for (; i < n; i += DEPTH)
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            if (i + d < n) compute(f[d], kMxStepBlocks);
+            if (i + d + DEPTH < n) load(f[d], first + (i + d + DEPTH) * stride);
+        }
+
+    // The last step, of one to three blocks: nothing past the rows' ends is read.  A 16-bit product leaves the missing blocks' MFMAs
+    // out; the one of MXFP4 X gets zeros there.
+    if (!SCALES4 && rest && whole >= first && (whole - first) % stride == 0) {
+        Step &l = f[0];
+        const bool have = part < rest;
+        const uint32_t back = have ? 0u : (uint32_t)(part - rest + 1);  // blocks past the end: read the last one again
+        const uint8_t *const w = o.w + (size_t)whole * 64, *const s = o.s + (size_t)whole * 4, *const x = o.x + (size_t)whole * (Op::kMx ? 64 : 256);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            l.w[t] = *reinterpret_cast<const uint4_t *>(w + (o.wo[t] - back * 16));
+            if constexpr (Op::kMx) {
+                l.s[t] = s[o.so[t] - back];
+                if (!have) {
+                    l.w[t] = (uint4_t){0u, 0u, 0u, 0u};
+                    l.s[t] = 127u;
+                }
+            } else {
+                l.s[t] = s[o.so[t]];
+                if (rest > 1) l.s[t] |= (uint32_t)s[o.so[t] + 1] << 8;
+                if (rest > 2) l.s[t] |= (uint32_t)s[o.so[t] + 2] << 16;
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            if constexpr (Op::kMx) {
+                l.x[m][0] = *reinterpret_cast<const uint4_t *>(x + (o.xo[m] - back * 16));
+                l.xs[m] = (o.xs + (size_t)whole * 4)[o.xso[m] - back];
+                if (!have) {
+                    l.x[m][0] = (uint4_t){0u, 0u, 0u, 0u};
+                    l.xs[m] = 127u;
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 3; ++j)
+                    if (j < rest) l.x[m][j] = *reinterpret_cast<const uint4_t *>(x + o.xo[m] + j * 64);
+            }
+        }
+        compute(l, rest);
+    }
+}
+
+// One FP32 result in the format of Y: 0 FP16, 1 BF16 (round to nearest even).
+__device__ __forceinline__ uint16_t to_16bit(float v, int bf16) { return (uint16_t)((bf16 ? ActBF16::pack2(v, 0.f) : pack_half2(v, 0.f)) & 0xFFFFu); }
+
+}  // namespace w4a16

@@ -54,6 +54,36 @@ int w4a16_mx_gemm(const void *X, int dtype, long long ldx, const uint8_t *codes,
 int w4a16_mx_gemm_mx(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *codes, const uint8_t *scales, int M, int N, int K,
                      void *Y, int dtype, long long ldy, void *stream);
 
+/*
+ * A mixture-of-experts router's choice.  For every token t: the `top_k` experts of the largest logits[t, :] (type `dtype`: FP16, BF16
+ * or FP32; rows ld values apart), in descending order, equal ones by ascending index, and their weights:
+ *   W4A16_MOE_SOFTMAX  exp(l - max) / sum over all experts of it;  W4A16_MOE_SIGMOID  1 / (1 + exp(-l)),
+ * with `renormalize` nonzero divided by their sum over the chosen ones, then times `factor`; in FP32.  A logit of -infinity excludes
+ * its expert: where fewer than top_k are left, the remaining places get id -1 and weight 0.  A NaN counts as the largest and
+ * makes weights that depend on it NaN.  1 <= top_k <= 32, top_k <= E <= 1024.  ids int32 [T, top_k], weights FP32 [T, top_k].
+ */
+typedef enum { W4A16_MOE_SOFTMAX = 0, W4A16_MOE_SIGMOID = 1 } w4a16_moe_scoring;
+int w4a16_moe_route(const void *logits, int dtype, int T, int E, long long ld, int top_k, int scoring, int renormalize, float factor,
+                    int32_t *ids, float *weights, void *stream);
+
+/*
+ * A mixture of experts' gated feed-forward layers, for a few tokens (any number works; weights are read once per 64):
+ *
+ *   Y[t] = sum over j of weights[t, j] W2_e (act(W1_e X[t]) * (W3_e X[t])),  e = ids[t, j],
+ *
+ * X and Y [T, H] both FP16 or both BF16 (`dtype`); weights in MXFP4: codes13, scales13 of [E, 2 I, H] (of each expert first the I
+ * rows of W1, the gate, then those of W3), codes2, scales2 of [E, H, I].  act: SiLU, g / (1 + exp(-g)), or GELU, 0.5 g (1 +
+ * tanh(sqrt(2 / pi) (g + 0.044715 g^3))).  An id outside 0 .. E - 1 stands for no expert (its weight is not read); a token without
+ * any gets zeros; an expert named twice counts twice.  FP32 sums; the product of the gate and up halves is rounded to 2^-17 on its way into the second
+ * product.  H and I multiples of 32, E <= 1024, top_k <= 32.  `workspace`: device memory of w4a16_moe_workspace_bytes,
+ * 256-byte aligned, contents irrelevant, used by this call alone until its work on `stream` is done.
+ */
+typedef enum { W4A16_MOE_SILU = 0, W4A16_MOE_GELU = 1 } w4a16_moe_activation;
+size_t w4a16_moe_workspace_bytes(int T, int top_k, int I);
+int w4a16_moe_experts(const void *X, int dtype, long long ldx, const int32_t *ids, const float *weights, const uint8_t *codes13,
+                      const uint8_t *scales13, const uint8_t *codes2, const uint8_t *scales2, int T, int E, int top_k, int H, int I,
+                      int activation, void *Y, long long ldy, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -63,3 +63,51 @@ def gemm(X, codes, scales):
     X = np.asarray(X, np.float64)
     W = values(codes, scales)
     return X @ W.T, np.abs(X) @ np.abs(W).T
+
+
+def route(logits, top_k, sigmoid=False, renormalize=True, factor=1.0):
+    """(ids, weights) one token at a time, from the definition: descending, ties to the lowest index, NaN first, -inf never chosen."""
+    logits = np.asarray(logits, np.float64)
+    T, E = logits.shape
+    ids = np.full((T, top_k), -1, np.int64)
+    weights = np.zeros((T, top_k))
+    for t in range(T):
+        row = logits[t]
+        key = np.where(np.isnan(row), np.inf, row)
+        order = sorted((e for e in range(E) if row[e] != -np.inf), key=lambda e: (not np.isnan(row[e]), -key[e], e))[:top_k]
+        if not order:
+            continue
+        with np.errstate(all="ignore"):
+            if sigmoid:
+                score = 1.0 / (1.0 + np.exp(-row))
+                total = 1.0
+            else:
+                score = np.exp(row - row[order[0]])
+                total = score.sum()
+            chosen = score[order]
+            if renormalize:
+                total = chosen.sum()
+            ids[t, :len(order)] = order
+            weights[t, :len(order)] = chosen / total * factor
+    return ids, weights
+
+
+def activate(g, gelu=False):
+    with np.errstate(over="ignore"):
+        if gelu:
+            return 0.5 * g * (1.0 + np.tanh(np.sqrt(2.0 / np.pi) * (g + 0.044715 * g ** 3)))
+        return g / (1.0 + np.exp(-g))
+
+
+def experts(X, ids, weights, W13, W2, gelu=False):
+    """Y [T, H] of the layer; W13 [E, 2 I, H] and W2 [E, H, I] are values."""
+    X = np.asarray(X, np.float64)
+    Y = np.zeros_like(X)
+    I = W2.shape[2]
+    for t in range(X.shape[0]):
+        for j in range(ids.shape[1]):
+            e = ids[t, j]
+            if 0 <= e < W13.shape[0]:
+                both = W13[e] @ X[t]
+                Y[t] += weights[t, j] * (W2[e] @ (activate(both[:I], gelu) * both[I:]))
+    return Y

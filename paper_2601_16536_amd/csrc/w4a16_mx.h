@@ -27,4 +27,21 @@ struct MxGemmArgs {
 };
 hipError_t launch_mx_rows(const MxGemmArgs &a, hipStream_t stream);
 
+constexpr int kMoeMaxExperts = 1024, kMoeMaxTopK = 32;
+hipError_t launch_moe_route(const void *logits, int type, int T, int E, long long ld, int top_k, bool sigmoid, bool renormalize, float factor,
+                            int32_t *ids, float *weights, hipStream_t stream);
+
+struct MoeArgs {
+    const void *X;                       // FP16 or BF16 [T, H], rows ldx values apart
+    const int32_t *ids;                  // [T, top_k]; outside 0 .. E - 1: no expert
+    const float *weights;                // [T, top_k]
+    const uint8_t *codes13, *scales13;   // [E, 2 I, H]: rows 0 .. I - 1 gate, I .. 2 I - 1 up
+    const uint8_t *codes2, *scales2;     // [E, H, I]
+    void *Y;                             // type of X [T, H]
+    uint16_t *hidden;                    // BF16 [2, T top_k, I]: the upper and the lower term of the activations
+    long long ldx, ldy;
+    int type, T, E, top_k, H, I, activation;
+};
+hipError_t launch_moe_experts(const MoeArgs &a, hipStream_t stream);
+
 }  // namespace w4a16

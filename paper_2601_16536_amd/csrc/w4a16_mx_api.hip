@@ -78,4 +78,46 @@ int w4a16_mx_gemm_mx(const uint8_t *x_codes, const uint8_t *x_scales, const uint
     return hip_status(launch_mx_rows(a, static_cast<hipStream_t>(stream)));
 }
 
+int w4a16_moe_route(const void *logits, int dtype, int T, int E, long long ld, int top_k, int scoring, int renormalize, float factor,
+                    int32_t *ids, float *weights, void *stream)
+{
+    clear_hip_error();
+    if (!(type_16bit(dtype) || dtype == W4A16_F32) || T < 0 || E < 1 || E > kMoeMaxExperts || top_k < 1 || top_k > E || top_k > kMoeMaxTopK ||
+        (T > 1 && ld < E) || (scoring != W4A16_MOE_SOFTMAX && scoring != W4A16_MOE_SIGMOID))
+        return W4A16_ERR_SHAPE;
+    if (T == 0) return W4A16_OK;
+    if (!logits || !ids || !weights) return W4A16_ERR_NULL;
+    if (!aligned(logits, dtype == W4A16_F32 ? 4 : 2) || !aligned(ids, 4) || !aligned(weights, 4)) return W4A16_ERR_ALIGN;
+    return hip_status(launch_moe_route(logits, dtype, T, E, T > 1 ? ld : E, top_k, scoring == W4A16_MOE_SIGMOID, renormalize != 0, factor, ids, weights,
+                                       static_cast<hipStream_t>(stream)));
+}
+
+size_t w4a16_moe_workspace_bytes(int T, int top_k, int I)
+{
+    if (T < 1 || top_k < 1 || I < 1) return 0;
+    return (size_t)T * (size_t)top_k * (size_t)I * 4;
+}
+
+int w4a16_moe_experts(const void *X, int dtype, long long ldx, const int32_t *ids, const float *weights, const uint8_t *codes13,
+                      const uint8_t *scales13, const uint8_t *codes2, const uint8_t *scales2, int T, int E, int top_k, int H, int I,
+                      int activation, void *Y, long long ldy, void *workspace, size_t workspace_bytes, void *stream)
+{
+    clear_hip_error();
+    if (!type_16bit(dtype) || T < 0 || E < 1 || E > kMoeMaxExperts || top_k < 1 || top_k > kMoeMaxTopK || bad_k(H) || bad_k(I) ||
+        (activation != W4A16_MOE_SILU && activation != W4A16_MOE_GELU))
+        return W4A16_ERR_SHAPE;
+    if (T == 0) return W4A16_OK;
+    if (!X || !ids || !weights || !codes13 || !scales13 || !codes2 || !scales2 || !Y || !workspace) return W4A16_ERR_NULL;
+    if (T > 1 && (ldx < H || ldy < H)) return W4A16_ERR_SHAPE;
+    if (!aligned(X, 16) || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(codes13, 16) || !aligned(codes2, 16) || !aligned(Y, 2) ||
+        !aligned(workspace, 256) || bad_rows(T, H, ldx, 8))
+        return W4A16_ERR_ALIGN;
+    // 32-bit offsets inside an expert's matrices and a block of tokens; blocks of tokens in a grid's second and third dimension
+    if ((long long)H * I > (1ll << 31) || H > kMaxLd || I > (1 << 19) || (T > 1 && ldx > kMaxLd) || T > (1 << 21)) return W4A16_ERR_UNSUPPORTED;
+    if (workspace_bytes < w4a16_moe_workspace_bytes(T, top_k, I)) return W4A16_ERR_WORKSPACE;
+    const MoeArgs a = {X, ids, weights, codes13, scales13, codes2, scales2, Y, static_cast<uint16_t *>(workspace), T > 1 ? ldx : H, T > 1 ? ldy : H,
+                       dtype, T, E, top_k, H, I, activation};
+    return hip_status(launch_moe_experts(a, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

@@ -59,16 +59,19 @@ __device__ __forceinline__ void blocks_to_words(uint4_t &w)
 // MXFP4 X: one MFMA per step that takes both operands' codes and scales as they are stored.
 struct MxBF16 {
     static constexpr bool kMx = false;
-    static constexpr int kOut = 1;
+    static constexpr int kTerms = 1;
     static __device__ __forceinline__ uint4_t operand(uint32_t w, uint32_t s) { return words_bf16(w, scale_operand(s)); }
     static __device__ __forceinline__ float4_t multiply(uint4_t x, uint4_t b, uint32_t, float4_t acc)
     {
         return ActBF16::mfma(ActBF16::x_operand(x), ActBF16::x_operand(b), acc);
     }
 };
+struct MxBF16Pair : MxBF16 {  // X is the sum of two BF16 matrices: sixteen bits of an FP32 number's fraction
+    static constexpr int kTerms = 2;
+};
 struct MxF16 {
     static constexpr bool kMx = false;
-    static constexpr int kOut = 0;
+    static constexpr int kTerms = 1;
     static __device__ __forceinline__ uint4_t operand(uint32_t w, uint32_t) { return words_f16(w, 1.0f); }
     static __device__ __forceinline__ float4_t multiply(uint4_t x, uint4_t b, uint32_t s, float4_t acc)
     {
@@ -81,6 +84,7 @@ struct MxF16 {
 };
 struct MxFP4 {
     static constexpr bool kMx = true;
+    static constexpr int kTerms = 1;
     static __device__ __forceinline__ float4_t multiply(uint4_t x, uint32_t xs, uint4_t w, uint32_t ws, float4_t acc)
     {
         const int8_vec_t a = {(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}, b = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], 0, 0, 0, 0};
@@ -90,10 +94,11 @@ struct MxFP4 {
 
 // What a wave's product reads.  The pointers are the same in every lane; a lane adds its offsets (32 bits):
 //   w: codes of its row of W (row lane mod 16 of a tile) plus 16 (lane / 16);  s: that row's scales, for MXFP4 X plus lane / 16;
-//   x: its row of X plus 16 (lane / 16) bytes;                                xs (MXFP4 X): that row's scales plus lane / 16.
+//   x: its row of X plus 16 (lane / 16) bytes;                                xs (MXFP4 X): that row's scales plus lane / 16;
+//   x2: the second term of X, laid out as the first (kTerms = 2).
 template <int CT, int MT>
 struct MxOperands {
-    const uint8_t *w, *s, *x, *xs;
+    const uint8_t *w, *s, *x, *xs, *x2;
     uint32_t wo[CT], so[CT], xo[MT], xso[MT];
 };
 
@@ -103,7 +108,7 @@ struct MxOperands {
 template <class Op, int CT, int MT, bool SCALES4, int DEPTH>
 __device__ __forceinline__ void mx_product(float4_t (&acc)[CT][MT], const MxOperands<CT, MT> &o, int blocks, int first, int stride)
 {
-    constexpr int kXWords = Op::kMx ? 1 : 4;
+    constexpr int kXWords = Op::kMx ? 1 : 4 * Op::kTerms;
     struct Step {
         uint4_t w[CT], x[MT][kXWords];
         uint32_t s[CT], xs[MT];
@@ -114,6 +119,7 @@ __device__ __forceinline__ void mx_product(float4_t (&acc)[CT][MT], const MxOper
 
     auto load = [&](Step &f, int c) {
         const uint8_t *const w = o.w + (size_t)c * 64, *const s = o.s + (size_t)c * 4, *const x = o.x + (size_t)c * (Op::kMx ? 64 : 256);
+        const uint8_t *const x2 = Op::kTerms == 2 ? o.x2 + (size_t)c * 256 : nullptr;
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
             f.w[t] = __builtin_nontemporal_load(reinterpret_cast<const uint4_t *>(w + o.wo[t]));
@@ -124,7 +130,7 @@ __device__ __forceinline__ void mx_product(float4_t (&acc)[CT][MT], const MxOper
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
 #pragma unroll
-            for (int j = 0; j < kXWords; ++j) f.x[m][j] = *reinterpret_cast<const uint4_t *>(x + o.xo[m] + j * 64);
+            for (int j = 0; j < kXWords; ++j) f.x[m][j] = *reinterpret_cast<const uint4_t *>((j < 4 ? x : x2) + o.xo[m] + (j & 3) * 64);
             if constexpr (Op::kMx) f.xs[m] = (o.xs + (size_t)c * 4)[o.xso[m]];
         }
     };
@@ -142,7 +148,9 @@ __device__ __forceinline__ void mx_product(float4_t (&acc)[CT][MT], const MxOper
                     const uint32_t s = (f.s[t] >> (8 * j)) & 0xFFu;
                     const uint4_t b = Op::operand(f.w[t][j], s);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) acc[t][m] = Op::multiply(f.x[m][j], b, s, acc[t][m]);
+                    for (int m = 0; m < MT; ++m)
+#pragma unroll
+                        for (int h = 0; h < Op::kTerms; ++h) acc[t][m] = Op::multiply(f.x[m][4 * h + j], b, s, acc[t][m]);
                 }
             }
         }
@@ -173,6 +181,7 @@ __device__ __forceinline__ void mx_product(float4_t (&acc)[CT][MT], const MxOper
         const bool have = part < rest;
         const uint32_t back = have ? 0u : (uint32_t)(part - rest + 1);  // blocks past the end: read the last one again
         const uint8_t *const w = o.w + (size_t)whole * 64, *const s = o.s + (size_t)whole * 4, *const x = o.x + (size_t)whole * (Op::kMx ? 64 : 256);
+        const uint8_t *const x2 = Op::kTerms == 2 ? o.x2 + (size_t)whole * 256 : nullptr;
 #pragma unroll
         for (int t = 0; t < CT; ++t) {
             l.w[t] = *reinterpret_cast<const uint4_t *>(w + (o.wo[t] - back * 16));
@@ -200,7 +209,10 @@ __device__ __forceinline__ void mx_product(float4_t (&acc)[CT][MT], const MxOper
             } else {
 #pragma unroll
                 for (int j = 0; j < 3; ++j)
-                    if (j < rest) l.x[m][j] = *reinterpret_cast<const uint4_t *>(x + o.xo[m] + j * 64);
+                    if (j < rest) {
+                        l.x[m][j] = *reinterpret_cast<const uint4_t *>(x + o.xo[m] + j * 64);
+                        if constexpr (Op::kTerms == 2) l.x[m][4 + j] = *reinterpret_cast<const uint4_t *>(x2 + o.xo[m] + j * 64);
+                    }
             }
         }
         compute(l, rest);

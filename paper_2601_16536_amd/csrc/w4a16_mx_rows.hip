@@ -30,6 +30,7 @@ __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(MxGemmArgs a, int b
     }
     const size_t row_x = Op::kMx ? (size_t)row_w : (size_t)a.ldx * 2;
     o.x = static_cast<const uint8_t *>(a.X) + (size_t)m0 * row_x;
+    o.x2 = nullptr;
     o.xs = Op::kMx ? a.xs + (size_t)m0 * (uint32_t)blocks : nullptr;
 #pragma unroll
     for (int m = 0; m < MT; ++m) {

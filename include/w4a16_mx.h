@@ -79,7 +79,7 @@ int w4a16_moe_route(const void *logits, int dtype, int T, int E, long long ld, i
  * 256-byte aligned, contents irrelevant, used by this call alone until its work on `stream` is done.
  */
 typedef enum { W4A16_MOE_SILU = 0, W4A16_MOE_GELU = 1 } w4a16_moe_activation;
-size_t w4a16_moe_workspace_bytes(int T, int top_k, int I);
+size_t w4a16_moe_workspace_bytes(int T, int top_k, int H, int I);
 int w4a16_moe_experts(const void *X, int dtype, long long ldx, const int32_t *ids, const float *weights, const uint8_t *codes13,
                       const uint8_t *scales13, const uint8_t *codes2, const uint8_t *scales2, int T, int E, int top_k, int H, int I,
                       int activation, void *Y, long long ldy, void *workspace, size_t workspace_bytes, void *stream);

@@ -1,9 +1,11 @@
 // A mixture of experts' feed-forward layers for a few tokens:
 //     h_p = act(W1_e x_t) * (W3_e x_t)   for every pair p = (t, j), e = ids[p]        (gate_up kernel)
-//     y_t = sum_j weights[p] W2_e h_p                                                  (down kernel)
-// Both are bound by the weights of the experts that some token chose, each of which is read once per 16 of its tokens.  Every workgroup sorts
-// the pairs of a block of 64 tokens by expert for itself (some hundred numbers, in LDS).  Between the kernels h is kept as the sum of two BF16
-// numbers, sixteen bits of its FP32 fraction: its rounding (2^-17) stays below the result's.
+//     z_p = weights[p] W2_e h_p                                                        (down kernel)
+//     y_t = sum_j z_p                                                                  (combine kernel)
+// The first two are bound by the weights of the experts that some token chose, each of which is read once per 16 of its tokens.  Every
+// workgroup sorts the pairs of a block of 64 tokens by expert for itself (some hundred numbers, in LDS) and takes one expert and a run of its rows.  Between
+// the kernels h is kept as the sum of two BF16 numbers, sixteen bits of its FP32 fraction: its rounding (2^-17) stays below the result's; z is FP32, and a token's
+// sum is in the order of its places, so results do not depend on the schedule.
 #include "w4a16_mx.h"
 #include "w4a16_mx_device.h"
 
@@ -72,128 +74,204 @@ __device__ __forceinline__ float activate(float g, int activation)
     return 0.5f * g * (1.0f + tanhf(0.7978845608f * (g + 0.044715f * g * g * g)));
 }
 
-constexpr int kGateWaves = 8;
+constexpr int kWaves = 8;
 
-template <class Op, bool SCALES4>
-__global__ __launch_bounds__(64 * kGateWaves) void moe_gate_up_kernel(MoeArgs a)
+// Of one expert's rows of X (`rows` of them) as many steps at a time as LDS (64 KiB) and the threads' registers hold.
+template <class Op>
+__host__ __device__ inline MxChunk expert_chunk(int steps, int rows)
+{
+    const int held = (kMxXUnits * 64 * kWaves / (rows * Op::kTerms * 16)) & ~1;  // at least eight
+    return mx_chunk<Op>(steps < held ? steps : held, rows);
+}
+
+template <class Op, int NI, bool SCALES4, bool MULTI, int DEPTH>
+__global__ __launch_bounds__(64 * kWaves) void moe_gate_up_kernel(MoeArgs a, int parts)
 {
     __shared__ Lists l;
-    __shared__ float red[kGateWaves][2][256];
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int t0 = (int)blockIdx.z * kBlockTokens, tokens = min(kBlockTokens, a.T - t0);
     make_lists(l, a.ids + (size_t)t0 * a.top_k, tokens * a.top_k, a.E);
     if ((int)blockIdx.y >= l.actives) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int col = lane & 15, part = lane >> 4;
+    const int col = lane & 15, p16 = lane >> 4;
+    const int tiles = kWaves / parts, tile = wave / parts, part = wave - tile * parts;
     const int e = __builtin_amdgcn_readfirstlane(l.active[blockIdx.y]);
     const int begin = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y]), end = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y + 1]);
-    const int blocks = a.H / kMxBlock;
+    const int blocks = a.H / kMxBlock, steps = (blocks + kMxStepBlocks - 1) / kMxStepBlocks;
     const uint32_t row_w = (uint32_t)a.H / 2;
-    const size_t i0 = (size_t)blockIdx.x * 16, pairs = (size_t)a.T * (size_t)a.top_k;
+    const int i0 = (int)blockIdx.x * tiles * 16;
+    const size_t pairs = (size_t)a.T * (size_t)a.top_k;
 
-    MxOperands<2, 1> o;
-    const size_t row0 = (size_t)e * 2 * (size_t)a.I + i0;
+    MxWeights<2> o;
+    const size_t row0 = (size_t)e * 2 * (size_t)a.I + (size_t)min(i0 + 16 * tile, a.I - 16);  // (a tile past the end repeats the last one; not stored)
     o.w = a.codes13 + row0 * row_w;
     o.s = a.scales13 + row0 * (uint32_t)blocks;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
         const uint32_t r = (uint32_t)(t * a.I + col);
-        o.wo[t] = r * row_w + (uint32_t)part * 16;
+        o.wo[t] = r * row_w + (uint32_t)p16 * 16;
         o.so[t] = r * (uint32_t)blocks;
     }
-    o.x = static_cast<const uint8_t *>(a.X) + (size_t)t0 * (size_t)a.ldx * 2;
-    o.xs = o.x2 = nullptr;
-    for (int r0 = begin; r0 < end; r0 += 16) {
-        o.xo[0] = (uint32_t)(l.order[min(r0 + col, end - 1)] / a.top_k) * (uint32_t)(a.ldx * 2) + (uint32_t)part * 16;
-        o.xso[0] = 0;
-        float4_t acc[2][1] = {{(float4_t){0.f, 0.f, 0.f, 0.f}}, {(float4_t){0.f, 0.f, 0.f, 0.f}}};
-        mx_product<Op, 2, 1, SCALES4, 2>(acc, o, blocks, wave, kGateWaves);
-        if (r0 != begin) __syncthreads();  // the sums of the rows before have been read
+    const uint8_t *const x = static_cast<const uint8_t *>(a.X) + (size_t)t0 * (size_t)a.ldx * 2;
+    float *const red = reinterpret_cast<float *>(lds);
+    for (int r0 = begin; r0 < end; r0 += kMxRows) {
+        const int rows = min(kMxRows, end - r0);
+        float4_t acc[2] = {(float4_t){0.f, 0.f, 0.f, 0.f}, (float4_t){0.f, 0.f, 0.f, 0.f}};
+        mx_stream<Op, 2, NI, SCALES4, MULTI, DEPTH>(acc, o, blocks, part, parts, expert_chunk<Op>(steps, rows), rows, lds,
+                                                    [&](int r, int) { return x + (size_t)(l.order[r0 + r] / a.top_k) * (size_t)a.ldx * 2; }, [&](int) { return x; });
 #pragma unroll
-        for (int t = 0; t < 2; ++t) *reinterpret_cast<float4_t *>(&red[wave][t][lane * 4]) = acc[t][0];
+        for (int t = 0; t < 2; ++t) *reinterpret_cast<float4_t *>(red + (wave * 2 + t) * 256 + lane * 4) = acc[t];
         __syncthreads();
-        const int q = (int)threadIdx.x;
-        if (q < 256) {
-            const int r = q >> 4, c = q & 15, at = (((r >> 2) << 4) | c) * 4 + (r & 3);
+        for (int q = (int)threadIdx.x; q < 16 * tiles * rows; q += 64 * kWaves) {
+            const int r = q / (16 * tiles), c = q - r * 16 * tiles, at = (((r >> 2) << 4) | (c & 15)) * 4 + (r & 3);
+            const float *const from = red + (c >> 4) * parts * 512 + at;
             float g = 0.f, u = 0.f;
-#pragma unroll
-            for (int w = 0; w < kGateWaves; ++w) {
-                g += red[w][0][at];
-                u += red[w][1][at];
+            for (int w = 0; w < parts; ++w) {
+                g += from[w * 512];
+                u += from[w * 512 + 256];
             }
-            if (r0 + r < end) {
+            if (i0 + c < a.I) {
                 const float h = activate(g, a.activation) * u;
                 const uint16_t hi = to_16bit(h, 1);
                 const float low = h - __builtin_bit_cast(float, (uint32_t)hi << 16);
-                uint16_t *const to = a.hidden + ((size_t)t0 * a.top_k + l.order[r0 + r]) * (size_t)a.I + i0 + (size_t)c;
+                uint16_t *const to = a.hidden + ((size_t)t0 * a.top_k + l.order[r0 + r]) * (size_t)a.I + (size_t)(i0 + c);
                 to[0] = hi;
                 to[pairs * (size_t)a.I] = to_16bit(low, 1);
             }
         }
+        __syncthreads();
     }
 }
 
-constexpr int kDownWaves = 16;
-
-template <bool SCALES4>
-__global__ __launch_bounds__(64 * kDownWaves) void moe_down_kernel(MoeArgs a, int split)
+template <int CT, bool SCALES4, bool MULTI, int DEPTH>
+__global__ __launch_bounds__(64 * kWaves) void moe_down_kernel(MoeArgs a, int parts)
 {
     __shared__ Lists l;
-    extern __shared__ float slabs[];  // [waves][tokens][16]
-    const int t0 = (int)blockIdx.y * kBlockTokens, tokens = min(kBlockTokens, a.T - t0);
-    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int col = lane & 15, part = lane >> 4;
-    float *const slab = slabs + (size_t)wave * tokens * 16;
-    for (int i = lane; i < tokens * 16; i += 64) slab[i] = 0.f;
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+    const int t0 = (int)blockIdx.z * kBlockTokens, tokens = min(kBlockTokens, a.T - t0);
     make_lists(l, a.ids + (size_t)t0 * a.top_k, tokens * a.top_k, a.E);
+    if ((int)blockIdx.y >= l.actives) return;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int col = lane & 15, p16 = lane >> 4;
+    const int tiles = kWaves / parts, tile = wave / parts, part = wave - tile * parts;
+    const int e = __builtin_amdgcn_readfirstlane(l.active[blockIdx.y]);
+    const int begin = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y]), end = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y + 1]);
     const int blocks = a.I / kMxBlock, steps = (blocks + kMxStepBlocks - 1) / kMxStepBlocks;
     const uint32_t row_w = (uint32_t)a.I / 2;
-    const size_t n0 = (size_t)blockIdx.x * 16, pairs = (size_t)a.T * (size_t)a.top_k;
+    const int n0 = (int)blockIdx.x * tiles * 16 * CT, base = min(n0 + 16 * CT * tile, a.H - 16);
+    const size_t pairs = (size_t)a.T * (size_t)a.top_k;
 
-    MxOperands<1, 1> o;
-    o.wo[0] = (uint32_t)col * row_w + (uint32_t)part * 16;
-    o.so[0] = (uint32_t)col * (uint32_t)blocks;
-    o.x = reinterpret_cast<const uint8_t *>(a.hidden + (size_t)t0 * a.top_k * (size_t)a.I);
-    o.x2 = o.x + pairs * (size_t)a.I * 2;
-    o.xs = nullptr;
-    o.xso[0] = 0;
-    const int items = l.actives * split;  // an expert's share of K; `split` divides the waves
-    for (int item = wave; item < items; item += kDownWaves) {
-        const int act = item / split, share = item % split;
-        const int e = __builtin_amdgcn_readfirstlane(l.active[act]);
-        const int begin = __builtin_amdgcn_readfirstlane(l.begin[act]), end = __builtin_amdgcn_readfirstlane(l.begin[act + 1]);
-        const size_t row0 = (size_t)e * (size_t)a.H + n0;
-        o.w = a.codes2 + row0 * row_w;
-        o.s = a.scales2 + row0 * (uint32_t)blocks;
-        for (int r0 = begin; r0 < end; r0 += 16) {
-            o.xo[0] = (uint32_t)l.order[min(r0 + col, end - 1)] * (uint32_t)a.I * 2 + (uint32_t)part * 16;
-            float4_t acc[1][1] = {{(float4_t){0.f, 0.f, 0.f, 0.f}}};
-            mx_product<MxBF16Pair, 1, 1, SCALES4, 2>(acc, o, blocks, share, split);
+    MxWeights<CT> o;
+    const size_t row0 = (size_t)e * (size_t)a.H + (size_t)base;
+    o.w = a.codes2 + row0 * row_w;
+    o.s = a.scales2 + row0 * (uint32_t)blocks;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int r = r0 + part * 4 + i;
-                if (r < end) {
-                    const int p = l.order[r];
-                    const float v = a.weights[(size_t)t0 * a.top_k + p] * acc[0][0][i];
-                    __builtin_amdgcn_ds_atomic_fadd_f32((__attribute__((address_space(3))) float *)&slab[(p / a.top_k) * 16 + col], v);
-                }
+    for (int t = 0; t < CT; ++t) {
+        const uint32_t r = (uint32_t)(min(base + 16 * t, a.H - 16) - base + col);
+        o.wo[t] = r * row_w + (uint32_t)p16 * 16;
+        o.so[t] = r * (uint32_t)blocks;
+    }
+    const uint8_t *const x = reinterpret_cast<const uint8_t *>(a.hidden + (size_t)t0 * a.top_k * (size_t)a.I);
+    const size_t second = pairs * (size_t)a.I * 2;
+    float *const red = reinterpret_cast<float *>(lds);
+    for (int r0 = begin; r0 < end; r0 += kMxRows) {
+        const int rows = min(kMxRows, end - r0);
+        float4_t acc[CT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) acc[t] = (float4_t){0.f, 0.f, 0.f, 0.f};
+        mx_stream<MxBF16Pair, CT, 4, SCALES4, MULTI, DEPTH>(acc, o, blocks, part, parts, expert_chunk<MxBF16Pair>(steps, rows), rows, lds,
+                                                            [&](int r, int term) { return x + (size_t)l.order[r0 + r] * (size_t)a.I * 2 + (term ? second : 0); }, [&](int) { return x; });
+#pragma unroll
+        for (int t = 0; t < CT; ++t) *reinterpret_cast<float4_t *>(red + (wave * CT + t) * 256 + lane * 4) = acc[t];
+        __syncthreads();
+        const int width = 16 * CT * tiles;
+        for (int q = (int)threadIdx.x; q < width * rows; q += 64 * kWaves) {
+            const int r = q / width, c = q - r * width, at = (((r >> 2) << 4) | (c & 15)) * 4 + (r & 3);
+            const float *const from = red + ((c / (16 * CT)) * parts * CT + (c >> 4) % CT) * 256 + at;
+            float v = 0.f;
+            for (int w = 0; w < parts; ++w) v += from[w * CT * 256];
+            if (n0 + c < a.H) {
+                const size_t p = (size_t)t0 * a.top_k + l.order[r0 + r];
+                a.partial[p * (size_t)a.H + (size_t)(n0 + c)] = a.weights[p] * v;
             }
         }
-    }
-    (void)steps;
-    __syncthreads();
-    for (int q = (int)threadIdx.x; q < tokens * 16; q += 64 * kDownWaves) {
-        float v = 0.f;
-        for (int w = 0; w < kDownWaves; ++w) v += slabs[(size_t)w * tokens * 16 + q];
-        static_cast<uint16_t *>(a.Y)[(size_t)(t0 + (q >> 4)) * (size_t)a.ldy + n0 + (size_t)(q & 15)] = to_16bit(v, a.type == kTypeBF16);
+        __syncthreads();
     }
 }
 
-template <class Op>
-void launch_gate_up(const MoeArgs &a, dim3 grid, hipStream_t stream)
+// Four outputs of a token per thread.
+__global__ __launch_bounds__(256) void moe_combine_kernel(MoeArgs a)
 {
+    const long long q = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int quads = a.H / 4;
+    const long long t = q / quads;
+    if (t >= a.T) return;
+    const int h = (int)(q - t * quads) * 4;
+    float4_t v = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < a.top_k; ++j) {
+        const size_t p = (size_t)t * (size_t)a.top_k + (size_t)j;
+        const int e = a.ids[p];
+        if (e < 0 || e >= a.E) continue;
+        const float4_t z = *reinterpret_cast<const float4_t *>(a.partial + p * (size_t)a.H + (size_t)h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += z[i];
+    }
+    uint16_t *const y = static_cast<uint16_t *>(a.Y) + (size_t)t * (size_t)a.ldy + (size_t)h;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = to_16bit(v[i], a.type == kTypeBF16);
+}
+
+// Shares of K per tile: about sixteen waves to a compute unit, a pair of steps to each.
+int shares(long long tiles, int steps)
+{
+    int parts = 1;
+    while (parts < kWaves && parts * tiles < 4096 && parts * 4 <= steps) parts *= 2;
+    return parts;
+}
+
+template <class Kernel>
+hipError_t enqueue(Kernel kernel, dim3 grid, size_t lds, hipStream_t stream, const MoeArgs &a, int parts)
+{
+    if (lds > 49152) {  // beside the lists
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), lds, stream, a, parts);
+    return hipGetLastError();
+}
+
+// LDS for up to `rows` rows of an expert.
+template <class Op>
+size_t chunk_lds(int steps, int rows, size_t sums)
+{
+    size_t most = sums;
+    for (int r = 1; r <= rows; ++r) {
+        const size_t b = mx_chunk_bytes<Op>(expert_chunk<Op>(steps, r), r);
+        if (b > most) most = b;
+    }
+    return most;
+}
+
+template <class Op, int NI, bool MULTI>
+hipError_t launch_gate_up(const MoeArgs &a, int slots, unsigned token_blocks, int rows, hipStream_t stream)
+{
+    const int steps = (a.H + kMxStep - 1) / kMxStep, parts = shares((long long)a.I / 16 * slots, steps), per = kWaves / parts * 16;
+    const dim3 grid((unsigned)((a.I + per - 1) / per), (unsigned)slots, token_blocks);
+    const size_t lds = chunk_lds<Op>(steps, rows, kWaves * 2048);
     const bool scales4 = a.H % kMxStep == 0 && (reinterpret_cast<uintptr_t>(a.scales13) & 3u) == 0;
-    if (scales4) hipLaunchKernelGGL((moe_gate_up_kernel<Op, true>), grid, dim3(64 * kGateWaves), 0, stream, a);
-    else hipLaunchKernelGGL((moe_gate_up_kernel<Op, false>), grid, dim3(64 * kGateWaves), 0, stream, a);
+    return scales4 ? enqueue(&moe_gate_up_kernel<Op, NI, true, MULTI, 2>, grid, lds, stream, a, parts)
+                   : enqueue(&moe_gate_up_kernel<Op, NI, false, MULTI, 2>, grid, lds, stream, a, parts);
+}
+
+template <int CT, bool MULTI>
+hipError_t launch_down(const MoeArgs &a, int slots, unsigned token_blocks, int rows, hipStream_t stream)
+{
+    const int steps = (a.I + kMxStep - 1) / kMxStep, parts = shares((long long)a.H / (16 * CT) * slots, steps), per = kWaves / parts * 16 * CT;
+    const dim3 grid((unsigned)((a.H + per - 1) / per), (unsigned)slots, token_blocks);
+    const size_t lds = chunk_lds<MxBF16Pair>(steps, rows, kWaves * CT * 1024);
+    const bool scales4 = a.I % kMxStep == 0 && (reinterpret_cast<uintptr_t>(a.scales2) & 3u) == 0;
+    return scales4 ? enqueue(&moe_down_kernel<CT, true, MULTI, 2>, grid, lds, stream, a, parts)
+                   : enqueue(&moe_down_kernel<CT, false, MULTI, 2>, grid, lds, stream, a, parts);
 }
 
 }  // namespace
@@ -203,18 +281,14 @@ hipError_t launch_moe_experts(const MoeArgs &a, hipStream_t stream)
     const unsigned token_blocks = (unsigned)((a.T + kBlockTokens - 1) / kBlockTokens);
     const int tokens = a.T < kBlockTokens ? a.T : kBlockTokens;
     const int slots = a.E < tokens * a.top_k ? a.E : tokens * a.top_k;  // experts that a block can have chosen
-    const dim3 gate_grid((unsigned)(a.I / 16), (unsigned)slots, token_blocks);
-    if (a.type == kTypeBF16) launch_gate_up<MxBF16>(a, gate_grid, stream);
-    else launch_gate_up<MxF16>(a, gate_grid, stream);
-    hipError_t e = hipGetLastError();
+    const int rows = tokens * a.top_k < kMxRows ? tokens * a.top_k : kMxRows;
+    const bool bf16 = a.type == kTypeBF16;
+    hipError_t e = bf16 ? launch_gate_up<MxBF16, 4, true>(a, slots, token_blocks, rows, stream) : launch_gate_up<MxF16, 4, true>(a, slots, token_blocks, rows, stream);
     if (e != hipSuccess) return e;
-    int split = 1;
-    while (split < kDownWaves && slots * split < kDownWaves) split *= 2;
-    const bool scales4 = a.I % kMxStep == 0 && (reinterpret_cast<uintptr_t>(a.scales2) & 3u) == 0;
-    const size_t lds = (size_t)kDownWaves * tokens * 16 * sizeof(float);
-    const dim3 down_grid((unsigned)(a.H / 16), token_blocks);
-    if (scales4) hipLaunchKernelGGL((moe_down_kernel<true>), down_grid, dim3(64 * kDownWaves), lds, stream, a, split);
-    else hipLaunchKernelGGL((moe_down_kernel<false>), down_grid, dim3(64 * kDownWaves), lds, stream, a, split);
+    e = launch_down<2, true>(a, slots, token_blocks, rows, stream);
+    if (e != hipSuccess) return e;
+    const unsigned long long quads = (unsigned long long)a.T * (unsigned)(a.H / 4);
+    hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream, a);
     return hipGetLastError();
 }
 

@@ -39,6 +39,7 @@ struct MoeArgs {
     const uint8_t *codes2, *scales2;     // [E, H, I]
     void *Y;                             // type of X [T, H]
     uint16_t *hidden;                    // BF16 [2, T top_k, I]: the upper and the lower term of the activations
+    float *partial;                      // [T top_k, H]: the places' results, weighted
     long long ldx, ldy;
     int type, T, E, top_k, H, I, activation;
 };

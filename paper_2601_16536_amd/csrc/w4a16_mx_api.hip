@@ -17,7 +17,7 @@ bool bad_k(int K) { return K < kMxBlock || K % kMxBlock != 0; }
 bool bad_rows(long long rows, int K, long long ld, int per) { return rows > 1 && (ld < K || ld % per != 0); }
 
 // 32-bit offsets inside a tile of 64 rows.
-constexpr long long kMaxLd = 1ll << 24;
+constexpr long long kMaxLd = 1ll << 23;
 
 int check_gemm(int M, int N, int K, int dtype, long long ldy)
 {
@@ -92,10 +92,10 @@ int w4a16_moe_route(const void *logits, int dtype, int T, int E, long long ld, i
                                        static_cast<hipStream_t>(stream)));
 }
 
-size_t w4a16_moe_workspace_bytes(int T, int top_k, int I)
+size_t w4a16_moe_workspace_bytes(int T, int top_k, int H, int I)
 {
-    if (T < 1 || top_k < 1 || I < 1) return 0;
-    return (size_t)T * (size_t)top_k * (size_t)I * 4;
+    if (T < 1 || top_k < 1 || H < 1 || I < 1) return 0;
+    return (size_t)T * (size_t)top_k * ((size_t)H + (size_t)I) * 4;
 }
 
 int w4a16_moe_experts(const void *X, int dtype, long long ldx, const int32_t *ids, const float *weights, const uint8_t *codes13,
@@ -113,9 +113,10 @@ int w4a16_moe_experts(const void *X, int dtype, long long ldx, const int32_t *id
         !aligned(workspace, 256) || bad_rows(T, H, ldx, 8))
         return W4A16_ERR_ALIGN;
     // 32-bit offsets inside an expert's matrices and a block of tokens; blocks of tokens in a grid's second and third dimension
-    if ((long long)H * I > (1ll << 31) || H > kMaxLd || I > (1 << 19) || (T > 1 && ldx > kMaxLd) || T > (1 << 21)) return W4A16_ERR_UNSUPPORTED;
-    if (workspace_bytes < w4a16_moe_workspace_bytes(T, top_k, I)) return W4A16_ERR_WORKSPACE;
-    const MoeArgs a = {X, ids, weights, codes13, scales13, codes2, scales2, Y, static_cast<uint16_t *>(workspace), T > 1 ? ldx : H, T > 1 ? ldy : H,
+    if ((long long)H * I > (1ll << 31) || H > kMaxLd || I > (1 << 18) || (T > 1 && ldx > kMaxLd) || T > (1 << 21)) return W4A16_ERR_UNSUPPORTED;
+    if (workspace_bytes < w4a16_moe_workspace_bytes(T, top_k, H, I)) return W4A16_ERR_WORKSPACE;
+    const MoeArgs a = {X, ids, weights, codes13, scales13, codes2, scales2, Y, static_cast<uint16_t *>(workspace),
+                       reinterpret_cast<float *>(static_cast<uint16_t *>(workspace) + 2 * (size_t)T * (size_t)top_k * (size_t)I), T > 1 ? ldx : H, T > 1 ? ldy : H,
                        dtype, T, E, top_k, H, I, activation};
     return hip_status(launch_moe_experts(a, static_cast<hipStream_t>(stream)));
 }

@@ -1,83 +1,112 @@
-// Y = X W^T with W in MXFP4, few rows of X: weights streamed from memory straight into the MFMAs' operands.
+// Y = X W^T with W in MXFP4 and up to sixteen rows of X per workgroup: weights streamed from memory straight into the MFMAs' operands.
 //
-// A workgroup owns 16 CT rows of W (columns of Y) and 16 MT rows of X; its waves take the steps of K (128 values) in turn, each with
-// sums of its own, which meet in LDS and are added in the order of the waves: results do not depend on the schedule.
+// The waves of a workgroup are `parts` shares of K times tiles of 16 rows of W (columns of Y).  The shares' sums meet in LDS and are added
+// in their order: results do not depend on the schedule.
 #include "w4a16_mx.h"
 #include "w4a16_mx_device.h"
 
 namespace w4a16 {
 namespace {
 
-template <class Op, int CT, int MT, bool SCALES4, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(MxGemmArgs a, int bf16)
+struct RowsPlan {
+    MxChunk chunk;
+    int parts, tiles;  // per workgroup
+    size_t lds;
+    bool multi;
+};
+
+template <class Op, int NI, bool SCALES4, bool MULTI, int WAVES, int DEPTH>
+__global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(MxGemmArgs a, MxChunk chunk, int parts)
 {
-    __shared__ float red[WAVES][CT * MT][256];
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];  // X; then the shares' sums
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int col = lane & 15, part = lane >> 4;
-    const int n0 = (int)blockIdx.x * 16 * CT, m0 = (int)blockIdx.y * 16 * MT;
+    const int col = lane & 15, p16 = lane >> 4;
+    const int tiles = WAVES / parts, tile = wave / parts, part = wave - tile * parts;
+    const int n0 = ((int)blockIdx.x * tiles + tile) * 16, m0 = (int)blockIdx.y * kMxRows, rows = min(kMxRows, a.M - m0);
     const int blocks = a.K / kMxBlock;
     const uint32_t row_w = (uint32_t)a.K / 2;
 
-    // Rows past the ends read the last one; what comes of them is not stored.
-    MxOperands<CT, MT> o;
-    o.w = a.codes + (size_t)n0 * row_w;
-    o.s = a.scales + (size_t)n0 * (uint32_t)blocks;
-#pragma unroll
-    for (int t = 0; t < CT; ++t) {
-        const uint32_t n = (uint32_t)min(16 * t + col, a.N - 1 - n0);
-        o.wo[t] = n * row_w + (uint32_t)part * 16;
-        o.so[t] = n * (uint32_t)blocks + (Op::kMx ? (uint32_t)part : 0u);
-    }
+    // Rows of W past the end read the last one; what comes of them is not stored.
+    MxWeights<1> o;
+    const int base = min(n0, a.N - 1);
+    const uint32_t n = (uint32_t)min(col, a.N - 1 - base);
+    o.w = a.codes + (size_t)base * row_w;
+    o.s = a.scales + (size_t)base * (uint32_t)blocks;
+    o.wo[0] = n * row_w + (uint32_t)p16 * 16;
+    o.so[0] = n * (uint32_t)blocks;
     const size_t row_x = Op::kMx ? (size_t)row_w : (size_t)a.ldx * 2;
-    o.x = static_cast<const uint8_t *>(a.X) + (size_t)m0 * row_x;
-    o.x2 = nullptr;
-    o.xs = Op::kMx ? a.xs + (size_t)m0 * (uint32_t)blocks : nullptr;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const uint32_t r = (uint32_t)min(16 * m + col, a.M - 1 - m0);
-        o.xo[m] = r * (uint32_t)row_x + (uint32_t)part * 16;
-        o.xso[m] = r * (uint32_t)blocks + (uint32_t)part;
-    }
+    const uint8_t *const x = static_cast<const uint8_t *>(a.X) + (size_t)m0 * row_x, *const xs = Op::kMx ? a.xs + (size_t)m0 * (uint32_t)blocks : nullptr;
 
-    float4_t acc[CT][MT];
-#pragma unroll
-    for (int t = 0; t < CT; ++t)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) acc[t][m] = (float4_t){0.f, 0.f, 0.f, 0.f};
-    mx_product<Op, CT, MT, SCALES4, MT >= 4 ? 1 : 2>(acc, o, blocks, wave, WAVES);
+    float4_t acc[1] = {(float4_t){0.f, 0.f, 0.f, 0.f}};
+    mx_stream<Op, 1, NI, SCALES4, MULTI, DEPTH>(acc, o, blocks, part, parts, chunk, rows, lds, [&](int r, int) { return x + (size_t)r * row_x; },
+                                                [&](int r) { return xs + (size_t)r * (uint32_t)blocks; });
 
-#pragma unroll
-    for (int t = 0; t < CT; ++t)
-#pragma unroll
-        for (int m = 0; m < MT; ++m) *reinterpret_cast<float4_t *>(&red[wave][t * MT + m][lane * 4]) = acc[t][m];
+    float *const red = reinterpret_cast<float *>(lds);
+    *reinterpret_cast<float4_t *>(red + wave * 256 + lane * 4) = acc[0];
     __syncthreads();
-    // Output e of the workgroup: row e / (16 CT), column e mod (16 CT), of which lane 16 ((row mod 16) / 4) + column mod 16 held number row mod 4.
-    for (int e = (int)threadIdx.x; e < CT * MT * 256; e += 64 * WAVES) {
-        const int r = e / (16 * CT), c = e % (16 * CT);
-        const int tile = (c >> 4) * MT + (r >> 4), at = ((((r & 15) >> 2) << 4) | (c & 15)) * 4 + (r & 3);
+    // Output e of the workgroup: row e / (16 tiles), column e mod (16 tiles); lane 16 (row / 4) + column mod 16 held number row mod 4 of it.
+    const int width = 16 * tiles, c0 = (int)blockIdx.x * width;
+    for (int e = (int)threadIdx.x; e < width * rows; e += 64 * WAVES) {
+        const int r = e / width, c = e - r * width, at = (((r >> 2) << 4) | (c & 15)) * 4 + (r & 3);
+        const float *const from = red + (c >> 4) * parts * 256 + at;
         float v = 0.f;
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) v += red[w][tile][at];
-        if (m0 + r < a.M && n0 + c < a.N) static_cast<uint16_t *>(a.Y)[(size_t)(m0 + r) * (size_t)a.ldy + (size_t)(n0 + c)] = to_16bit(v, bf16);
+        for (int w = 0; w < parts; ++w) v += from[w * 256];
+        if (c0 + c < a.N) static_cast<uint16_t *>(a.Y)[(size_t)(m0 + r) * (size_t)a.ldy + (size_t)(c0 + c)] = to_16bit(v, a.type == kTypeBF16);
     }
 }
 
-template <class Op, int CT, int MT, int WAVES>
-hipError_t launch(const MxGemmArgs &a, hipStream_t stream)
+template <class Op, int NI, int WAVES, int DEPTH>
+hipError_t launch(const MxGemmArgs &a, const RowsPlan &p, hipStream_t stream)
 {
-    const dim3 grid((unsigned)((a.N + 16 * CT - 1) / (16 * CT)), (unsigned)((a.M + 16 * MT - 1) / (16 * MT)));
+    const int per = 16 * p.tiles;
+    const dim3 grid((unsigned)((a.N + per - 1) / per), (unsigned)((a.M + kMxRows - 1) / kMxRows));
     const bool scales4 = a.K % kMxStep == 0 && (reinterpret_cast<uintptr_t>(a.scales) & 3u) == 0;
-    const int bf16 = a.type == kTypeBF16;
-    if (scales4) hipLaunchKernelGGL((mx_rows_kernel<Op, CT, MT, true, WAVES>), grid, dim3(64 * WAVES), 0, stream, a, bf16);
-    else hipLaunchKernelGGL((mx_rows_kernel<Op, CT, MT, false, WAVES>), grid, dim3(64 * WAVES), 0, stream, a, bf16);
-    return hipGetLastError();
+    auto go = [&](auto kernel) {
+        if (p.lds > 65536) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds);
+            if (e != hipSuccess) return e;
+        }
+        hipLaunchKernelGGL(kernel, grid, dim3(64 * WAVES), p.lds, stream, a, p.chunk, p.parts);
+        return hipGetLastError();
+    };
+    if (scales4) return p.multi ? go(&mx_rows_kernel<Op, NI, true, true, WAVES, DEPTH>) : go(&mx_rows_kernel<Op, NI, true, false, WAVES, DEPTH>);
+    return p.multi ? go(&mx_rows_kernel<Op, NI, false, true, WAVES, DEPTH>) : go(&mx_rows_kernel<Op, NI, false, false, WAVES, DEPTH>);
+}
+
+template <class Op>
+RowsPlan plan(const MxGemmArgs &a, int waves)
+{
+    RowsPlan p;
+    const int rows = a.M < kMxRows ? a.M : kMxRows, steps = (a.K + kMxStep - 1) / kMxStep;
+    const long long tiles = ((long long)a.N + 15) / 16 * ((a.M + kMxRows - 1) / kMxRows);
+    // about sixteen waves to a compute unit
+    p.parts = 1;
+    while (p.parts < waves && p.parts * tiles < 4096 && p.parts * 4 <= steps) p.parts *= 2;
+    p.tiles = waves / p.parts;
+    const size_t limit = waves == 16 ? 131072 : 65536;
+    int chunk = steps;
+    const int by_units = kMxXUnits * 64 * waves / (rows * Op::kTerms * (Op::kMx ? 4 : 16));  // of what a thread's registers hold
+    if (mx_chunk_bytes<Op>(mx_chunk<Op>(steps, rows), rows) > limit || steps > 4 * by_units) {
+        chunk = by_units;
+        chunk -= chunk % 2;
+        if (chunk > 2 * p.parts) chunk -= chunk % (2 * p.parts);
+    }
+    p.multi = chunk < steps;
+    p.chunk = mx_chunk<Op>(chunk, rows);
+    p.lds = mx_chunk_bytes<Op>(p.chunk, rows);
+    const size_t sums = (size_t)waves * 1024;
+    if (p.lds < sums) p.lds = sums;
+    return p;
 }
 
 template <class Op>
 hipError_t launch_rows(const MxGemmArgs &a, hipStream_t stream)
 {
-    if (a.M <= 16) return launch<Op, 1, 1, 8>(a, stream);
-    return launch<Op, 2, 2, 8>(a, stream);
+    const int waves = ((long long)a.N + 15) / 16 * ((a.M + kMxRows - 1) / kMxRows) <= 256 ? 16 : 8;
+    const RowsPlan p = plan<Op>(a, waves);
+    if constexpr (Op::kMx || Op::kTerms == 2) return waves == 16 ? launch<Op, 4, 16, 4>(a, p, stream) : launch<Op, 4, 8, 4>(a, p, stream);
+    else if (a.M == 1) return waves == 16 ? launch<Op, 1, 16, 4>(a, p, stream) : launch<Op, 1, 8, 4>(a, p, stream);
+    else return waves == 16 ? launch<Op, 4, 16, 4>(a, p, stream) : launch<Op, 4, 8, 4>(a, p, stream);
 }
 
 }  // namespace

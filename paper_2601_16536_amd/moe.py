@@ -28,16 +28,16 @@ def lib():
         L = mx.lib()
         vp, ci, ll, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_longlong, ctypes.c_size_t
         L.w4a16_moe_route.argtypes = [vp, ci, ci, ci, ll, ci, ci, ci, ctypes.c_float, vp, vp, vp]
-        L.w4a16_moe_workspace_bytes.argtypes = [ci, ci, ci]
+        L.w4a16_moe_workspace_bytes.argtypes = [ci, ci, ci, ci]
         L.w4a16_moe_workspace_bytes.restype = sz
         L.w4a16_moe_experts.argtypes = [vp, ci, ll, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, vp, ll, vp, sz, vp]
         _lib = L
     return _lib
 
 
-def workspace_bytes(T: int, top_k: int, I: int) -> int:
+def workspace_bytes(T: int, top_k: int, H: int, I: int) -> int:
     """Bytes of workspace that `experts` needs."""
-    return int(lib().w4a16_moe_workspace_bytes(T, top_k, I))
+    return int(lib().w4a16_moe_workspace_bytes(T, top_k, H, I))
 
 
 def route(logits, top_k: int, scoring: str = "softmax", renormalize: bool = True, factor: float = 1.0, out=None, stream=None):
@@ -78,7 +78,7 @@ def _check_choice(ids, weights, T: int) -> None:
 def experts(X, ids, weights, codes13, scales13, codes2, scales2, activation: str = "silu", out=None, workspace=None, stream=None):
     """Y [T, H]: for every token the weighted sum of its experts' W2 (act(W1 x) * (W3 x)).  X [T, H] float16 or bfloat16; codes13, scales13
     of [E, 2 I, H], codes2, scales2 of [E, H, I] in MXFP4; activation 'silu' or 'gelu'.  `workspace`: a CUDA uint8 tensor of
-    workspace_bytes(T, top_k, I), 256-byte aligned, this call's own until its work is done; by default one from torch's allocator
+    workspace_bytes(T, top_k, H, I), 256-byte aligned, this call's own until its work is done; by default one from torch's allocator
     (on the current stream: with an explicit stream bring one)."""
     import torch
     code = mx.type_code(X.dtype, False)
@@ -92,7 +92,7 @@ def experts(X, ids, weights, codes13, scales13, codes2, scales2, activation: str
     _check_choice(ids, weights, T)
     top_k = ids.shape[1]
     Y, ldy = mx._out_matrix(out, T, H, X, X.dtype)
-    need = T * top_k * I * 4
+    need = T * top_k * (H + I) * 4
     if workspace is None:
         if stream is not None:
             raise ValueError("with an explicit stream the workspace has to be brought too")

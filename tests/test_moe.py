@@ -88,7 +88,7 @@ def test_argument_checks_need_no_gpu(moe):
     x = moe.lib().w4a16_moe_experts
 
     def experts(X=16, dtype=1, ldx=64, ids=16, weights=16, c13=16, s13=16, c2=16, s2=16, T=2, E=4, top_k=2, H=64, I=32, act=0, Y=16, ldy=64, ws=256,
-                ws_bytes=2 * 2 * 32 * 4):
+                ws_bytes=2 * 2 * 96 * 4):
         return x(X, dtype, ldx, ids, weights, c13, s13, c2, s2, T, E, top_k, H, I, act, Y, ldy, ws, ws_bytes, 0)
     assert experts(X=0, T=0) == b.OK
     for name in ("X", "ids", "weights", "c13", "s13", "c2", "s2", "Y", "ws"):
@@ -98,9 +98,9 @@ def test_argument_checks_need_no_gpu(moe):
         assert experts(**bad) == b.ERR_SHAPE, bad
     for bad in (dict(X=24), dict(ids=18), dict(c13=24), dict(c2=20), dict(Y=17), dict(ws=128), dict(ldx=68)):
         assert experts(**bad) == b.ERR_ALIGN, bad
-    assert experts(ws_bytes=2 * 2 * 32 * 4 - 1) == b.ERR_WORKSPACE
+    assert experts(ws_bytes=2 * 2 * 96 * 4 - 1) == b.ERR_WORKSPACE
     assert experts(H=1 << 17, ldx=1 << 17, ldy=1 << 17, I=1 << 15, ws_bytes=1 << 40) == b.ERR_UNSUPPORTED
-    assert moe.workspace_bytes(2, 2, 32) == 512 and moe.workspace_bytes(0, 2, 32) == 0
+    assert moe.workspace_bytes(2, 2, 64, 32) == 1536 and moe.workspace_bytes(0, 2, 64, 32) == 0
 
 
 # ---- the kernels ----
@@ -294,7 +294,7 @@ def test_reproducible_streams_graphs_and_canaries(moe, T):
     want = layer()
     for _ in range(5):
         assert torch.equal(want, layer())
-    need = moe.workspace_bytes(T, top_k, I)
+    need = moe.workspace_bytes(T, top_k, H, I)
     ws = torch.full((need + 512,), 255, dtype=torch.uint8, device="cuda")
     flat = torch.full((16 + T * (H + 6),), 9.0, dtype=torch.bfloat16, device="cuda")
     out = flat[5:5 + T * (H + 6)].view(T, H + 6)[:, :H]

@@ -9,11 +9,11 @@
  *   codes   uint8 [rows, K/2]   the code of an even k is the low nibble; bit 3 of a code is the sign
  *   scales  uint8 [rows, K/32]  s stands for 2^(s - 127); s = 255: the block's values are NaN
  *
- * K is a multiple of 32; rows may be any number.
+ * K is a multiple of 32 (in products at most 131072); rows may be any number.
  *
  * All data pointers are DEVICE pointers owned by the caller.  Codes, X and Y of the quantizer and X of the products are
- * 16-byte aligned, and so is every row of an X with a leading dimension (ld: values from a row to the next).  Scales, ids,
- * weights and the products' Y need no more than their type's alignment.  Calls only enqueue work on `stream` (a hipStream_t, NULL
+ * 16-byte aligned, and so are every row of an X with a leading dimension (ld: values from a row to the next) and the experts'
+ * scales.  Other scales, ids, weights, logits and the products' Y need no more than their type's alignment.  Calls only enqueue work on `stream` (a hipStream_t, NULL
  * = the default stream); none allocates, waits or keeps anything, so all may be captured into a HIP graph, and calls
  * on different streams may overlap (w4a16_moe_experts: each with its own workspace).  No rows (M, rows or T = 0):
  * W4A16_OK, nothing is launched.
@@ -75,7 +75,7 @@ int w4a16_moe_route(const void *logits, int dtype, int T, int E, long long ld, i
  * rows of W1, the gate, then those of W3), codes2, scales2 of [E, H, I].  act: SiLU, g / (1 + exp(-g)), or GELU, 0.5 g (1 +
  * tanh(sqrt(2 / pi) (g + 0.044715 g^3))).  An id outside 0 .. E - 1 stands for no expert (its weight is not read); a token without
  * any gets zeros; an expert named twice counts twice.  FP32 sums; the product of the gate and up halves is rounded to 2^-17 on its way into the second
- * product.  H and I multiples of 32, E <= 1024, top_k <= 32.  `workspace`: device memory of w4a16_moe_workspace_bytes,
+ * product.  H and I multiples of 32, at most 32768, E <= 1024, top_k <= 32.  `workspace`: device memory of w4a16_moe_workspace_bytes,
  * 256-byte aligned, contents irrelevant, used by this call alone until its work on `stream` is done.
  */
 typedef enum { W4A16_MOE_SILU = 0, W4A16_MOE_GELU = 1 } w4a16_moe_activation;

@@ -75,58 +75,219 @@ __device__ __forceinline__ float activate(float g, int activation)
 }
 
 constexpr int kWaves = 8;
+constexpr int kPassRows = 16;  // of an expert's tokens at a time
 
-// Of one expert's rows of X (`rows` of them) as many steps at a time as LDS (64 KiB) and the threads' registers hold.
+// ---- one expert's product: X and the scales whole in LDS, codes streamed from memory ----
+//
+// A wave holds CT tiles of 16 x 16 sums and walks its share of K by pairs of steps (256 values, 128 bytes of W's rows, a line), DEPTH pairs in
+// flight.  X's rows and the scales come to LDS by loads that pass no register, so that two workgroups share a compute unit.
+
+// LDS rows of X: whole KiB (what a wave's load writes) and 64 bytes, so that four rows use different banks; a second term's rows follow.
+__host__ __device__ inline uint32_t x_row(int K) { return (((uint32_t)K * 2u + 1023u) & ~1023u) + 64u; }
+// LDS of the scales of 16 rows: as they are, to whole KiB.
+__host__ __device__ inline uint32_t scale_group(int K) { return ((uint32_t)K / 2u + 1023u) & ~1023u; }
 template <class Op>
-__host__ __device__ inline MxChunk expert_chunk(int steps, int rows)
+__host__ __device__ inline uint32_t pass_lds(int K, int rows, int groups) { return (uint32_t)(rows * Op::kTerms) * x_row(K) + (uint32_t)groups * scale_group(K); }
+
+typedef __attribute__((address_space(3))) void *lds_ptr_t;
+
+// KiB `i` of `bytes` bytes at `from` to LDS; zeros past them.
+__device__ __forceinline__ void kib_to_lds(const uint8_t *from, uint32_t bytes, int i, uint8_t *to)
 {
-    const int held = (kMxXUnits * 64 * kWaves / (rows * Op::kTerms * 16)) & ~1;  // at least eight
-    return mx_chunk<Op>(steps < held ? steps : held, rows);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(from), 0, bytes, kRawBuffer), (lds_ptr_t)(to + i * 1024), 16,
+                                             ((uint32_t)threadIdx.x & 63u) * 16u, i * 1024, 0, 0);
 }
 
-template <class Op, int NI, bool SCALES4, bool MULTI, int DEPTH>
-__global__ __launch_bounds__(64 * kWaves) void moe_gate_up_kernel(MoeArgs a, int parts)
+template <class Op, int CT, bool WHOLE, int DEPTH>
+struct Stream {
+    static constexpr int kPairBlocks = 2 * kMxStepBlocks;
+    struct Pair {
+        uint4_t w[2][CT];
+    };
+    const uint8_t *w;               // codes: the tiles' first row
+    uint32_t wo[CT], so[CT];        // the lane's row and 16 (lane / 16) bytes; its row of scales in LDS
+    const uint8_t *x, *s;           // LDS
+    uint32_t xo, second;            // the lane's row of X; from a row of the first term to the second's
+    int blocks;
+
+    __device__ __forceinline__ void load(Pair &f, int k, bool full) const
+    {
+        const uint8_t *const p = w + (size_t)k * 128;
+        const int p16 = (int)(threadIdx.x & 63) >> 4;
+        uint32_t back0 = 0u, back1 = 0u;
+        if (!full) {  // blocks past the end read the last one again
+            const int last = blocks - k * kPairBlocks - 1;
+            back0 = (uint32_t)max(p16 - last, 0) * 16;
+            back1 = (uint32_t)max(p16 + kMxStepBlocks - last, 0) * 16;
+        }
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            f.w[0][t] = *reinterpret_cast<const uint4_t *>(p + (wo[t] - back0));
+            f.w[1][t] = *reinterpret_cast<const uint4_t *>(p + (wo[t] + 64 - back1));
+        }
+    }
+    // The eight scales of a pair.  Rows of scales that are not whole words begin at any byte.
+    __device__ __forceinline__ uint2_t scales(uint32_t at) const
+    {
+        if constexpr (WHOLE) {
+            const uint32_t *const p = reinterpret_cast<const uint32_t *>(s + at);
+            return (uint2_t){p[0], p[1]};
+        } else {
+            const uint32_t *const p = reinterpret_cast<const uint32_t *>(s + (at & ~3u));
+            return (uint2_t){__builtin_amdgcn_alignbyte(p[1], p[0], at & 3u), __builtin_amdgcn_alignbyte(p[2], p[1], at & 3u)};
+        }
+    }
+    __device__ __forceinline__ void step(float4_t (&acc)[CT], uint4_t (&c)[CT], const uint32_t (&sc)[CT], const uint8_t *at, int have) const
+    {
+        uint4_t xv[Op::kTerms][kMxStepBlocks];
+#pragma unroll
+        for (int h = 0; h < Op::kTerms; ++h)
+#pragma unroll
+            for (int j = 0; j < kMxStepBlocks; ++j) xv[h][j] = *reinterpret_cast<const uint4_t *>(at + h * second + j * 64);
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            blocks_to_words(c[t]);
+#pragma unroll
+            for (int j = 0; j < kMxStepBlocks; ++j) {
+                if (!WHOLE && j >= have) break;
+                const uint32_t v = (sc[t] >> (8 * j)) & 0xFFu;
+                const uint4_t b = Op::operand(c[t][j], v);
+#pragma unroll
+                for (int h = 0; h < Op::kTerms; ++h) acc[t] = Op::template multiply<4>(xv[h][j], b, v, acc[t]);
+            }
+        }
+    }
+    __device__ __forceinline__ void compute(float4_t (&acc)[CT], Pair &f, int k, bool full) const
+    {
+        uint32_t s0[CT], s1[CT];
+#pragma unroll
+        for (int t = 0; t < CT; ++t) {
+            const uint2_t v = scales(so[t] + (uint32_t)k * kPairBlocks);
+            s0[t] = v[0];
+            s1[t] = v[1];
+        }
+        const uint8_t *const at = x + xo + (uint32_t)k * 512u;
+        const int left = blocks - k * kPairBlocks;
+        step(acc, f.w[0], s0, at, full ? kMxStepBlocks : min(left, kMxStepBlocks));
+        if (full || left > kMxStepBlocks) step(acc, f.w[1], s1, at + 256, full ? kMxStepBlocks : left - kMxStepBlocks);
+    }
+    // Pairs begin .. end - 1.  Asks for the first codes, then waits for what the workgroup has asked into LDS.
+    __device__ __forceinline__ void run(float4_t (&acc)[CT], int begin, int end) const
+    {
+        const int whole = blocks / kPairBlocks;
+        Pair f[DEPTH];
+        asm volatile("" ::: "memory");  // the loads into LDS come first
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+            if (begin + d < end) load(f[d], begin + d, begin + d < whole);
+        if (end - begin >= DEPTH) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(DEPTH * 2 * CT) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        int k = begin;
+        const int safe = min(end, whole);
+        for (; k + 2 * DEPTH <= safe; k += DEPTH)
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                compute(acc, f[d], k + d, true);
+                load(f[d], k + d + DEPTH, true);
+                // Loads stay where they are asked for: moved together by the compiler they would come in bursts.
+                __builtin_amdgcn_sched_barrier(0x38F);
+            }
+        for (; k < end; k += DEPTH)
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                if (k + d < end) compute(acc, f[d], k + d, k + d < whole);
+                if (k + d + DEPTH < end) load(f[d], k + d + DEPTH, k + d + DEPTH < whole);
+            }
+        __syncthreads();
+    }
+};
+
+// Rows `rows` of X and the scales of `groups` times 16 rows into LDS, all waves in turn; row(r, term) and group(g) tell where they begin.
+template <class Op, class Row, class Group>
+__device__ __forceinline__ void ask_for(uint8_t *lds, int K, int rows, int groups, int wave, Row row, Group group)
+{
+    const int per_row = (K * 2 + 1023) >> 10, per_group = (K / 2 + 1023) >> 10;
+    const int xs = rows * Op::kTerms * per_row;
+    for (int u = wave; u < xs; u += kWaves) {
+        const int r = u / per_row, i = u - r * per_row;
+        kib_to_lds(row(Op::kTerms == 2 ? r % rows : r, Op::kTerms == 2 ? r / rows : 0), (uint32_t)K * 2u, i, lds + (uint32_t)r * x_row(K));
+    }
+    uint8_t *const s = lds + (uint32_t)(rows * Op::kTerms) * x_row(K);
+    for (int u = wave; u < groups * per_group; u += kWaves) {
+        const int g = u / per_group, i = u - g * per_group;
+        kib_to_lds(group(g), (uint32_t)K / 2u, i, s + (uint32_t)g * scale_group(K));
+    }
+}
+
+// The workgroup's expert and its run of pairs; false: none.
+struct Job {
+    int e, begin, end;
+};
+__device__ __forceinline__ bool find_job(Lists &l, const MoeArgs &a, int t0, Job *j)
+{
+    make_lists(l, a.ids + (size_t)t0 * a.top_k, min(kBlockTokens, a.T - t0) * a.top_k, a.E);
+    if ((int)blockIdx.y >= l.actives) return false;
+    j->e = __builtin_amdgcn_readfirstlane(l.active[blockIdx.y]);
+    j->begin = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y]);
+    j->end = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y + 1]);
+    return true;
+}
+
+// What the kernels are launched with.
+struct Geometry {
+    int parts;  // shares of K; kWaves / parts runs of CT tiles side by side
+    int pass;   // rows of an expert at a time
+};
+
+template <class Op, bool WHOLE, int DEPTH>
+__global__ __launch_bounds__(64 * kWaves, 4) void moe_gate_up_kernel(MoeArgs a, Geometry geo)
 {
     __shared__ Lists l;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const int t0 = (int)blockIdx.z * kBlockTokens, tokens = min(kBlockTokens, a.T - t0);
-    make_lists(l, a.ids + (size_t)t0 * a.top_k, tokens * a.top_k, a.E);
-    if ((int)blockIdx.y >= l.actives) return;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int t0 = (int)blockIdx.z * kBlockTokens;
+    Job job;
+    if (!find_job(l, a, t0, &job)) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int col = lane & 15, p16 = lane >> 4;
-    const int tiles = kWaves / parts, tile = wave / parts, part = wave - tile * parts;
-    const int e = __builtin_amdgcn_readfirstlane(l.active[blockIdx.y]);
-    const int begin = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y]), end = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y + 1]);
-    const int blocks = a.H / kMxBlock, steps = (blocks + kMxStepBlocks - 1) / kMxStepBlocks;
-    const uint32_t row_w = (uint32_t)a.H / 2;
+    const int tiles = kWaves / geo.parts, tile = wave / geo.parts, part = wave - tile * geo.parts;
     const int i0 = (int)blockIdx.x * tiles * 16;
-    const size_t pairs = (size_t)a.T * (size_t)a.top_k;
+    const uint32_t row_w = (uint32_t)a.H / 2, row_s = (uint32_t)a.H / kMxBlock;
+    const size_t expert_row = (size_t)job.e * 2 * (size_t)a.I;
+    auto tile_row = [&](int t) { return min(i0 + 16 * t, a.I - 16); };  // (a tile past the end repeats the last one; not stored)
+    const int pairs = ((int)row_s + 7) / 8;
 
-    MxWeights<2> o;
-    const size_t row0 = (size_t)e * 2 * (size_t)a.I + (size_t)min(i0 + 16 * tile, a.I - 16);  // (a tile past the end repeats the last one; not stored)
-    o.w = a.codes13 + row0 * row_w;
-    o.s = a.scales13 + row0 * (uint32_t)blocks;
+    Stream<Op, 2, WHOLE, DEPTH> st;
+    st.blocks = (int)row_s;
+    st.w = a.codes13 + (expert_row + (size_t)tile_row(tile)) * row_w;
+    st.second = 0;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-        const uint32_t r = (uint32_t)(t * a.I + col);
-        o.wo[t] = r * row_w + (uint32_t)p16 * 16;
-        o.so[t] = r * (uint32_t)blocks;
+        st.wo[t] = (uint32_t)(t * a.I + col) * row_w + (uint32_t)p16 * 16;
+        st.so[t] = (uint32_t)(2 * tile + t) * scale_group(a.H) + (uint32_t)col * row_s;
     }
-    const uint8_t *const x = static_cast<const uint8_t *>(a.X) + (size_t)t0 * (size_t)a.ldx * 2;
     float *const red = reinterpret_cast<float *>(lds);
-    for (int r0 = begin; r0 < end; r0 += kMxRows) {
-        const int rows = min(kMxRows, end - r0);
+    for (int r0 = job.begin; r0 < job.end; r0 += geo.pass) {
+        const int rows = min(geo.pass, job.end - r0);
+        ask_for<Op>(lds, a.H, rows, 2 * tiles, wave,
+                    [&](int r, int) {
+                        const int t = __builtin_amdgcn_readfirstlane(l.order[r0 + r]) / a.top_k;
+                        return static_cast<const uint8_t *>(a.X) + (size_t)(t0 + t) * (size_t)a.ldx * 2;
+                    },
+                    [&](int g) { return a.scales13 + (expert_row + (size_t)(g & 1) * (size_t)a.I + (size_t)tile_row(g >> 1)) * row_s; });
+        st.x = lds;
+        st.xo = (uint32_t)min(col, rows - 1) * x_row(a.H) + (uint32_t)p16 * 16;
+        st.s = lds + (uint32_t)rows * x_row(a.H);
         float4_t acc[2] = {(float4_t){0.f, 0.f, 0.f, 0.f}, (float4_t){0.f, 0.f, 0.f, 0.f}};
-        mx_stream<Op, 2, NI, SCALES4, MULTI, DEPTH>(acc, o, blocks, part, parts, expert_chunk<Op>(steps, rows), rows, lds,
-                                                    [&](int r, int) { return x + (size_t)(l.order[r0 + r] / a.top_k) * (size_t)a.ldx * 2; }, [&](int) { return x; });
+        st.run(acc, pairs * part / geo.parts, pairs * (part + 1) / geo.parts);
 #pragma unroll
         for (int t = 0; t < 2; ++t) *reinterpret_cast<float4_t *>(red + (wave * 2 + t) * 256 + lane * 4) = acc[t];
         __syncthreads();
         for (int q = (int)threadIdx.x; q < 16 * tiles * rows; q += 64 * kWaves) {
             const int r = q / (16 * tiles), c = q - r * 16 * tiles, at = (((r >> 2) << 4) | (c & 15)) * 4 + (r & 3);
-            const float *const from = red + (c >> 4) * parts * 512 + at;
+            const float *const from = red + (c >> 4) * geo.parts * 512 + at;
             float g = 0.f, u = 0.f;
-            for (int w = 0; w < parts; ++w) {
+            for (int w = 0; w < geo.parts; ++w) {
                 g += from[w * 512];
                 u += from[w * 512 + 256];
             }
@@ -136,60 +297,65 @@ __global__ __launch_bounds__(64 * kWaves) void moe_gate_up_kernel(MoeArgs a, int
                 const float low = h - __builtin_bit_cast(float, (uint32_t)hi << 16);
                 uint16_t *const to = a.hidden + ((size_t)t0 * a.top_k + l.order[r0 + r]) * (size_t)a.I + (size_t)(i0 + c);
                 to[0] = hi;
-                to[pairs * (size_t)a.I] = to_16bit(low, 1);
+                to[(size_t)a.T * (size_t)a.top_k * (size_t)a.I] = to_16bit(low, 1);
             }
         }
         __syncthreads();
     }
 }
 
-template <int CT, bool SCALES4, bool MULTI, int DEPTH>
-__global__ __launch_bounds__(64 * kWaves) void moe_down_kernel(MoeArgs a, int parts)
+template <int CT, bool WHOLE, int DEPTH>
+__global__ __launch_bounds__(64 * kWaves, 4) void moe_down_kernel(MoeArgs a, Geometry geo)
 {
     __shared__ Lists l;
-    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
-    const int t0 = (int)blockIdx.z * kBlockTokens, tokens = min(kBlockTokens, a.T - t0);
-    make_lists(l, a.ids + (size_t)t0 * a.top_k, tokens * a.top_k, a.E);
-    if ((int)blockIdx.y >= l.actives) return;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int t0 = (int)blockIdx.z * kBlockTokens;
+    Job job;
+    if (!find_job(l, a, t0, &job)) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int col = lane & 15, p16 = lane >> 4;
-    const int tiles = kWaves / parts, tile = wave / parts, part = wave - tile * parts;
-    const int e = __builtin_amdgcn_readfirstlane(l.active[blockIdx.y]);
-    const int begin = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y]), end = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y + 1]);
-    const int blocks = a.I / kMxBlock, steps = (blocks + kMxStepBlocks - 1) / kMxStepBlocks;
-    const uint32_t row_w = (uint32_t)a.I / 2;
-    const int n0 = (int)blockIdx.x * tiles * 16 * CT, base = min(n0 + 16 * CT * tile, a.H - 16);
-    const size_t pairs = (size_t)a.T * (size_t)a.top_k;
+    const int runs = kWaves / geo.parts, run = wave / geo.parts, part = wave - run * geo.parts;
+    const int n0 = (int)blockIdx.x * runs * CT * 16;
+    const uint32_t row_w = (uint32_t)a.I / 2, row_s = (uint32_t)a.I / kMxBlock;
+    const size_t expert_row = (size_t)job.e * (size_t)a.H;
+    auto tile_row = [&](int t) { return min(n0 + 16 * t, a.H - 16); };
+    const int pairs = ((int)row_s + 7) / 8;
 
-    MxWeights<CT> o;
-    const size_t row0 = (size_t)e * (size_t)a.H + (size_t)base;
-    o.w = a.codes2 + row0 * row_w;
-    o.s = a.scales2 + row0 * (uint32_t)blocks;
+    Stream<MxBF16Pair, CT, WHOLE, DEPTH> st;
+    st.blocks = (int)row_s;
+    st.w = a.codes2 + (expert_row + (size_t)tile_row(run * CT)) * row_w;
 #pragma unroll
     for (int t = 0; t < CT; ++t) {
-        const uint32_t r = (uint32_t)(min(base + 16 * t, a.H - 16) - base + col);
-        o.wo[t] = r * row_w + (uint32_t)p16 * 16;
-        o.so[t] = r * (uint32_t)blocks;
+        st.wo[t] = (uint32_t)(tile_row(run * CT + t) - tile_row(run * CT) + col) * row_w + (uint32_t)p16 * 16;
+        st.so[t] = (uint32_t)(run * CT + t) * scale_group(a.I) + (uint32_t)col * row_s;
     }
-    const uint8_t *const x = reinterpret_cast<const uint8_t *>(a.hidden + (size_t)t0 * a.top_k * (size_t)a.I);
-    const size_t second = pairs * (size_t)a.I * 2;
+    const size_t second = (size_t)a.T * (size_t)a.top_k * (size_t)a.I;
     float *const red = reinterpret_cast<float *>(lds);
-    for (int r0 = begin; r0 < end; r0 += kMxRows) {
-        const int rows = min(kMxRows, end - r0);
+    for (int r0 = job.begin; r0 < job.end; r0 += geo.pass) {
+        const int rows = min(geo.pass, job.end - r0);
+        ask_for<MxBF16Pair>(lds, a.I, rows, CT * runs, wave,
+                            [&](int r, int term) {
+                                const size_t p = (size_t)t0 * a.top_k + (size_t)__builtin_amdgcn_readfirstlane(l.order[r0 + r]);
+                                return reinterpret_cast<const uint8_t *>(a.hidden + p * (size_t)a.I + (term ? second : 0));
+                            },
+                            [&](int g) { return a.scales2 + (expert_row + (size_t)tile_row(g)) * row_s; });
+        st.x = lds;
+        st.xo = (uint32_t)min(col, rows - 1) * x_row(a.I) + (uint32_t)p16 * 16;
+        st.second = (uint32_t)rows * x_row(a.I);
+        st.s = lds + 2u * st.second;
         float4_t acc[CT];
 #pragma unroll
         for (int t = 0; t < CT; ++t) acc[t] = (float4_t){0.f, 0.f, 0.f, 0.f};
-        mx_stream<MxBF16Pair, CT, 4, SCALES4, MULTI, DEPTH>(acc, o, blocks, part, parts, expert_chunk<MxBF16Pair>(steps, rows), rows, lds,
-                                                            [&](int r, int term) { return x + (size_t)l.order[r0 + r] * (size_t)a.I * 2 + (term ? second : 0); }, [&](int) { return x; });
+        st.run(acc, pairs * part / geo.parts, pairs * (part + 1) / geo.parts);
 #pragma unroll
         for (int t = 0; t < CT; ++t) *reinterpret_cast<float4_t *>(red + (wave * CT + t) * 256 + lane * 4) = acc[t];
         __syncthreads();
-        const int width = 16 * CT * tiles;
+        const int width = 16 * CT * runs;
         for (int q = (int)threadIdx.x; q < width * rows; q += 64 * kWaves) {
             const int r = q / width, c = q - r * width, at = (((r >> 2) << 4) | (c & 15)) * 4 + (r & 3);
-            const float *const from = red + ((c / (16 * CT)) * parts * CT + (c >> 4) % CT) * 256 + at;
+            const float *const from = red + ((c / (16 * CT)) * geo.parts * CT + (c >> 4) % CT) * 256 + at;
             float v = 0.f;
-            for (int w = 0; w < parts; ++w) v += from[w * CT * 256];
+            for (int w = 0; w < geo.parts; ++w) v += from[w * CT * 256];
             if (n0 + c < a.H) {
                 const size_t p = (size_t)t0 * a.top_k + l.order[r0 + r];
                 a.partial[p * (size_t)a.H + (size_t)(n0 + c)] = a.weights[p] * v;
@@ -221,71 +387,76 @@ __global__ __launch_bounds__(256) void moe_combine_kernel(MoeArgs a)
     for (int i = 0; i < 4; ++i) y[i] = to_16bit(v[i], a.type == kTypeBF16);
 }
 
-// Shares of K per tile: about sixteen waves to a compute unit, a pair of steps to each.
-int shares(long long tiles, int steps)
+// How many shares K has, and how many rows of an expert go through a workgroup at a time: as many as LDS holds with two workgroups to a compute unit, or
+// with one, if that is too few for an expert's average.  An expert with more rows reads its weights again, from the caches.
+constexpr size_t kLds = 163840, kListsLds = (sizeof(Lists) + 1023) & ~(size_t)1023;
+struct Pass {
+    Geometry geo;
+    size_t lds;
+};
+template <class Op>
+Pass choose_pass(const MoeArgs &a, int K, int runs, int ct, int slots, int tokens)
 {
-    int parts = 1;
-    while (parts < kWaves && parts * tiles < 4096 && parts * 4 <= steps) parts *= 2;
-    return parts;
+    const int pairs = (K + 2 * kMxStep - 1) / (2 * kMxStep), most = tokens * a.top_k < kPassRows ? tokens * a.top_k : kPassRows;
+    Pass p;
+    p.geo.parts = 1;
+    while (p.geo.parts < kWaves && (long long)p.geo.parts * runs * slots < 4096 && p.geo.parts * 2 <= pairs) p.geo.parts *= 2;  // about sixteen waves to a compute unit
+    auto fit = [&](size_t limit) {
+        int rows = 0;
+        while (rows < most && pass_lds<Op>(K, rows + 1, ct * (kWaves / p.geo.parts)) <= limit) ++rows;
+        return rows;
+    };
+    p.geo.pass = fit(kLds / 2 - kListsLds);
+    if (p.geo.pass < most && (long long)p.geo.pass * a.E < 2ll * tokens * a.top_k) p.geo.pass = fit(kLds - kListsLds);
+    while (p.geo.pass == 0 && p.geo.parts < kWaves) {  // the longest rows
+        p.geo.parts *= 2;
+        p.geo.pass = fit(kLds - kListsLds);
+    }
+    p.lds = pass_lds<Op>(K, p.geo.pass, ct * (kWaves / p.geo.parts));
+    const size_t sums = (size_t)kWaves * ct * 1024;
+    if (p.lds < sums) p.lds = sums;
+    return p;
 }
 
 template <class Kernel>
-hipError_t enqueue(Kernel kernel, dim3 grid, size_t lds, hipStream_t stream, const MoeArgs &a, int parts)
+hipError_t enqueue(Kernel kernel, int outputs, int width, int slots, int token_blocks, const Pass &p, const MoeArgs &a, hipStream_t stream)
 {
-    if (lds > 49152) {  // beside the lists
-        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (p.geo.pass < 1) return hipErrorInvalidValue;
+    if (p.lds + kListsLds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds);
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(kernel, grid, dim3(64 * kWaves), lds, stream, a, parts);
+    const int per = kWaves / p.geo.parts * width;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((outputs + per - 1) / per), (unsigned)slots, (unsigned)token_blocks), dim3(64 * kWaves), p.lds, stream, a, p.geo);
     return hipGetLastError();
 }
 
-// LDS for up to `rows` rows of an expert.
+constexpr int kDownTiles = 2, kDepth = 2;
+
 template <class Op>
-size_t chunk_lds(int steps, int rows, size_t sums)
+hipError_t launch_gate_up(const MoeArgs &a, int slots, int token_blocks, int tokens, hipStream_t stream)
 {
-    size_t most = sums;
-    for (int r = 1; r <= rows; ++r) {
-        const size_t b = mx_chunk_bytes<Op>(expert_chunk<Op>(steps, r), r);
-        if (b > most) most = b;
-    }
-    return most;
+    const Pass p = choose_pass<Op>(a, a.H, a.I / 16, 2, slots, tokens);
+    return a.H % kMxStep == 0 ? enqueue(&moe_gate_up_kernel<Op, true, kDepth>, a.I, 16, slots, token_blocks, p, a, stream)
+                              : enqueue(&moe_gate_up_kernel<Op, false, kDepth>, a.I, 16, slots, token_blocks, p, a, stream);
 }
 
-template <class Op, int NI, bool MULTI>
-hipError_t launch_gate_up(const MoeArgs &a, int slots, unsigned token_blocks, int rows, hipStream_t stream)
+hipError_t launch_down(const MoeArgs &a, int slots, int token_blocks, int tokens, hipStream_t stream)
 {
-    const int steps = (a.H + kMxStep - 1) / kMxStep, parts = shares((long long)a.I / 16 * slots, steps), per = kWaves / parts * 16;
-    const dim3 grid((unsigned)((a.I + per - 1) / per), (unsigned)slots, token_blocks);
-    const size_t lds = chunk_lds<Op>(steps, rows, kWaves * 2048);
-    const bool scales4 = a.H % kMxStep == 0 && (reinterpret_cast<uintptr_t>(a.scales13) & 3u) == 0;
-    return scales4 ? enqueue(&moe_gate_up_kernel<Op, NI, true, MULTI, 2>, grid, lds, stream, a, parts)
-                   : enqueue(&moe_gate_up_kernel<Op, NI, false, MULTI, 2>, grid, lds, stream, a, parts);
-}
-
-template <int CT, bool MULTI>
-hipError_t launch_down(const MoeArgs &a, int slots, unsigned token_blocks, int rows, hipStream_t stream)
-{
-    const int steps = (a.I + kMxStep - 1) / kMxStep, parts = shares((long long)a.H / (16 * CT) * slots, steps), per = kWaves / parts * 16 * CT;
-    const dim3 grid((unsigned)((a.H + per - 1) / per), (unsigned)slots, token_blocks);
-    const size_t lds = chunk_lds<MxBF16Pair>(steps, rows, kWaves * CT * 1024);
-    const bool scales4 = a.I % kMxStep == 0 && (reinterpret_cast<uintptr_t>(a.scales2) & 3u) == 0;
-    return scales4 ? enqueue(&moe_down_kernel<CT, true, MULTI, 2>, grid, lds, stream, a, parts)
-                   : enqueue(&moe_down_kernel<CT, false, MULTI, 2>, grid, lds, stream, a, parts);
+    const Pass p = choose_pass<MxBF16Pair>(a, a.I, (a.H + 16 * kDownTiles - 1) / (16 * kDownTiles), kDownTiles, slots, tokens);
+    return a.I % kMxStep == 0 ? enqueue(&moe_down_kernel<kDownTiles, true, kDepth>, a.H, 16 * kDownTiles, slots, token_blocks, p, a, stream)
+                              : enqueue(&moe_down_kernel<kDownTiles, false, kDepth>, a.H, 16 * kDownTiles, slots, token_blocks, p, a, stream);
 }
 
 }  // namespace
 
 hipError_t launch_moe_experts(const MoeArgs &a, hipStream_t stream)
 {
-    const unsigned token_blocks = (unsigned)((a.T + kBlockTokens - 1) / kBlockTokens);
-    const int tokens = a.T < kBlockTokens ? a.T : kBlockTokens;
+    const int token_blocks = (a.T + kBlockTokens - 1) / kBlockTokens, tokens = a.T < kBlockTokens ? a.T : kBlockTokens;
     const int slots = a.E < tokens * a.top_k ? a.E : tokens * a.top_k;  // experts that a block can have chosen
-    const int rows = tokens * a.top_k < kMxRows ? tokens * a.top_k : kMxRows;
-    const bool bf16 = a.type == kTypeBF16;
-    hipError_t e = bf16 ? launch_gate_up<MxBF16, 4, true>(a, slots, token_blocks, rows, stream) : launch_gate_up<MxF16, 4, true>(a, slots, token_blocks, rows, stream);
+    hipError_t e = a.type == kTypeBF16 ? launch_gate_up<MxBF16>(a, slots, token_blocks, tokens, stream) : launch_gate_up<MxF16>(a, slots, token_blocks, tokens, stream);
     if (e != hipSuccess) return e;
-    e = launch_down<2, true>(a, slots, token_blocks, rows, stream);
+    e = launch_down(a, slots, token_blocks, tokens, stream);
     if (e != hipSuccess) return e;
     const unsigned long long quads = (unsigned long long)a.T * (unsigned)(a.H / 4);
     hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream, a);

@@ -16,13 +16,14 @@ bool bad_k(int K) { return K < kMxBlock || K % kMxBlock != 0; }
 // Rows of 16 bytes' alignment: `per` values of the type are 16 bytes.
 bool bad_rows(long long rows, int K, long long ld, int per) { return rows > 1 && (ld < K || ld % per != 0); }
 
-// 32-bit offsets inside a tile of 64 rows.
+// 32-bit offsets inside a tile of rows; rows of scales, and an expert's rows of X, in LDS.
 constexpr long long kMaxLd = 1ll << 23;
+constexpr int kMaxK = 1 << 17, kMaxExpertK = 1 << 15;
 
 int check_gemm(int M, int N, int K, int dtype, long long ldy)
 {
     if (M < 0 || N < 1 || bad_k(K) || !type_16bit(dtype) || (M > 1 && ldy < N)) return W4A16_ERR_SHAPE;
-    if (K > kMaxLd) return W4A16_ERR_UNSUPPORTED;
+    if (K > kMaxK) return W4A16_ERR_UNSUPPORTED;
     return W4A16_OK;
 }
 
@@ -109,11 +110,12 @@ int w4a16_moe_experts(const void *X, int dtype, long long ldx, const int32_t *id
     if (T == 0) return W4A16_OK;
     if (!X || !ids || !weights || !codes13 || !scales13 || !codes2 || !scales2 || !Y || !workspace) return W4A16_ERR_NULL;
     if (T > 1 && (ldx < H || ldy < H)) return W4A16_ERR_SHAPE;
-    if (!aligned(X, 16) || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(codes13, 16) || !aligned(codes2, 16) || !aligned(Y, 2) ||
+    if (!aligned(X, 16) || !aligned(ids, 4) || !aligned(weights, 4) || !aligned(codes13, 16) || !aligned(codes2, 16) || !aligned(scales13, 16) ||
+        !aligned(scales2, 16) || !aligned(Y, 2) ||
         !aligned(workspace, 256) || bad_rows(T, H, ldx, 8))
         return W4A16_ERR_ALIGN;
     // 32-bit offsets inside an expert's matrices and a block of tokens; blocks of tokens in a grid's second and third dimension
-    if ((long long)H * I > (1ll << 31) || H > kMaxLd || I > (1 << 18) || (T > 1 && ldx > kMaxLd) || T > (1 << 21)) return W4A16_ERR_UNSUPPORTED;
+    if (H > kMaxExpertK || I > kMaxExpertK || (T > 1 && ldx > kMaxLd) || T > (1 << 21)) return W4A16_ERR_UNSUPPORTED;
     if (workspace_bytes < w4a16_moe_workspace_bytes(T, top_k, H, I)) return W4A16_ERR_WORKSPACE;
     const MoeArgs a = {X, ids, weights, codes13, scales13, codes2, scales2, Y, static_cast<uint16_t *>(workspace),
                        reinterpret_cast<float *>(static_cast<uint16_t *>(workspace) + 2 * (size_t)T * (size_t)top_k * (size_t)I), T > 1 ? ldx : H, T > 1 ? ldy : H,

@@ -99,7 +99,7 @@ def test_argument_checks_need_no_gpu(moe):
     for bad in (dict(X=24), dict(ids=18), dict(c13=24), dict(c2=20), dict(Y=17), dict(ws=128), dict(ldx=68)):
         assert experts(**bad) == b.ERR_ALIGN, bad
     assert experts(ws_bytes=2 * 2 * 96 * 4 - 1) == b.ERR_WORKSPACE
-    assert experts(H=1 << 17, ldx=1 << 17, ldy=1 << 17, I=1 << 15, ws_bytes=1 << 40) == b.ERR_UNSUPPORTED
+    assert experts(H=1 << 16, ldx=1 << 16, ldy=1 << 16, ws_bytes=1 << 40) == b.ERR_UNSUPPORTED
     assert moe.workspace_bytes(2, 2, 64, 32) == 1536 and moe.workspace_bytes(0, 2, 64, 32) == 0
 
 

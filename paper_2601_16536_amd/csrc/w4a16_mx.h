@@ -25,7 +25,15 @@ struct MxGemmArgs {
     int M, N, K;
     int type;                // of Y, and of a 16-bit X
 };
+// w4a16_mx_rows.hip: few rows of X, weights read once per sixteen of them; w4a16_mx_tile.hip (K >= 128): the rest.  What a call would take, us.
+float estimate_mx_rows(const MxGemmArgs &a);
 hipError_t launch_mx_rows(const MxGemmArgs &a, hipStream_t stream);
+struct MxTilePlan {
+    int form;
+    float us;
+};
+MxTilePlan plan_mx_tile(const MxGemmArgs &a);
+hipError_t launch_mx_tile(const MxGemmArgs &a, int form, hipStream_t stream);
 
 constexpr int kMoeMaxExperts = 1024, kMoeMaxTopK = 32;
 hipError_t launch_moe_route(const void *logits, int type, int T, int E, long long ld, int top_k, bool sigmoid, bool renormalize, float factor,

@@ -20,6 +20,14 @@ bool bad_rows(long long rows, int K, long long ld, int per) { return rows > 1 &&
 constexpr long long kMaxLd = 1ll << 23;
 constexpr int kMaxK = 1 << 17, kMaxExpertK = 1 << 15;
 
+// The kernel whose time for the shape is estimated lower; both answer every shape (the tile kernel from K = 128 on) to the same accuracy.
+hipError_t launch_product(const MxGemmArgs &a, hipStream_t stream)
+{
+    if (a.K < kMxStep) return launch_mx_rows(a, stream);
+    const MxTilePlan p = plan_mx_tile(a);
+    return estimate_mx_rows(a) <= p.us ? launch_mx_rows(a, stream) : launch_mx_tile(a, p.form, stream);
+}
+
 int check_gemm(int M, int N, int K, int dtype, long long ldy)
 {
     if (M < 0 || N < 1 || bad_k(K) || !type_16bit(dtype) || (M > 1 && ldy < N)) return W4A16_ERR_SHAPE;
@@ -64,7 +72,7 @@ int w4a16_mx_gemm(const void *X, int dtype, long long ldx, const uint8_t *codes,
     if (!aligned(X, 16) || !aligned(codes, 16) || !aligned(Y, 2) || bad_rows(M, K, ldx, 8)) return W4A16_ERR_ALIGN;
     if (M > 1 && ldx > kMaxLd) return W4A16_ERR_UNSUPPORTED;
     const MxGemmArgs a = {X, nullptr, codes, scales, Y, M > 1 ? ldx : K, M > 1 ? ldy : N, M, N, K, dtype};
-    return hip_status(launch_mx_rows(a, static_cast<hipStream_t>(stream)));
+    return hip_status(launch_product(a, static_cast<hipStream_t>(stream)));
 }
 
 int w4a16_mx_gemm_mx(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *codes, const uint8_t *scales, int M, int N, int K,
@@ -76,7 +84,7 @@ int w4a16_mx_gemm_mx(const uint8_t *x_codes, const uint8_t *x_scales, const uint
     if (!x_codes || !x_scales || !codes || !scales || !Y) return W4A16_ERR_NULL;
     if (!aligned(x_codes, 16) || !aligned(codes, 16) || !aligned(Y, 2)) return W4A16_ERR_ALIGN;
     const MxGemmArgs a = {x_codes, x_scales, codes, scales, Y, K, M > 1 ? ldy : N, M, N, K, dtype};
-    return hip_status(launch_mx_rows(a, static_cast<hipStream_t>(stream)));
+    return hip_status(launch_product(a, static_cast<hipStream_t>(stream)));
 }
 
 int w4a16_moe_route(const void *logits, int dtype, int T, int E, long long ld, int top_k, int scoring, int renormalize, float factor,

@@ -59,6 +59,7 @@ __device__ __forceinline__ void blocks_to_words(uint4_t &w)
 // MXFP4 X: one MFMA per step that takes both operands' codes and scales as they are stored.
 struct MxBF16 {
     static constexpr bool kMx = false;
+    static constexpr bool kScaled = true;  // the scale is in the operand
     static constexpr int kTerms = 1;
     static __device__ __forceinline__ uint4_t operand(uint32_t w, uint32_t s) { return words_bf16(w, scale_operand(s)); }
     template <int NI>
@@ -72,12 +73,17 @@ struct MxBF16Pair : MxBF16 {  // X is the sum of two BF16 matrices: sixteen bits
 };
 struct MxF16 {
     static constexpr bool kMx = false;
+    static constexpr bool kScaled = false;
     static constexpr int kTerms = 1;
     static __device__ __forceinline__ uint4_t operand(uint32_t w, uint32_t) { return words_f16(w, 1.0f); }
+    static __device__ __forceinline__ float4_t product(uint4_t x, uint4_t b)
+    {
+        return ActF16::mfma(ActF16::x_operand(x), ActF16::x_operand(b), (float4_t){0.f, 0.f, 0.f, 0.f});
+    }
     template <int NI>
     static __device__ __forceinline__ float4_t multiply(uint4_t x, uint4_t b, uint32_t s, float4_t acc)
     {
-        const float4_t p = ActF16::mfma(ActF16::x_operand(x), ActF16::x_operand(b), (float4_t){0.f, 0.f, 0.f, 0.f});
+        const float4_t p = product(x, b);
         const float f = scale_value(s);
 #pragma unroll
         for (int i = 0; i < NI; ++i) acc[i] = __builtin_fmaf(f, p[i], acc[i]);

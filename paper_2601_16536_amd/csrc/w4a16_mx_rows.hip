@@ -18,7 +18,7 @@ namespace {
 // serves, and a step has four of X to one of W.
 //
 // Scales go through LDS too, whole rows of them at the start: read where they are used, eight bytes of sixteen rows at a time, they would be
-// as many requests to L2 as half the codes.  (K = 28672, N = 8192, one row of FP16: SCALES_BEFORE us so, SCALES_AFTER through LDS.)
+// as many requests to L2 as half the codes.  (K = 28672, N = 8192, one row of FP16: 29.8 us so, 26.9 through LDS.)
 constexpr int kMxRows = 16;        // rows of X per workgroup
 constexpr int kMxXUnits = 8;       // 16-byte units of X that a thread stages per chunk
 constexpr int kMxScaleUnits = 4;   // of scales, in flight
@@ -430,6 +430,17 @@ hipError_t launch_rows(const MxGemmArgs &a, hipStream_t stream)
 }
 
 }  // namespace
+
+// Codes and scales at the rate of memory (those of further row blocks of the caches), X once per tile at what such reads reach; not less than a workgroup takes
+// for what it reads.  Measured for 1 to 49 rows, K from 1600 to 28672, N from 129 to 11008: within a fifth where it is near the other kernel's time.
+float estimate_mx_rows(const MxGemmArgs &a)
+{
+    const float w = (float)a.N * (float)a.K * 0.53125f, tiles = (float)((a.N + 15) / 16), blocks = (float)((a.M + kMxRows - 1) / kMxRows);
+    const float row = (float)a.K * (a.xs ? 0.7f : 2.0f);
+    const float all = w / 6.2e6f + (blocks - 1.0f) * w / 12.0e6f + (float)a.M * row * tiles / 7.5e6f;
+    const float one = (8.5f * (float)a.K + (float)(a.M < kMxRows ? a.M : kMxRows) * row) / 26.0e3f;
+    return 3.0f + (all > one ? all : one);
+}
 
 hipError_t launch_mx_rows(const MxGemmArgs &a, hipStream_t stream)
 {

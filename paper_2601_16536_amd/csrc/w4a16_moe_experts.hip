@@ -7,7 +7,7 @@
 // the kernels h is kept as the sum of two BF16 numbers, sixteen bits of its FP32 fraction: its rounding (2^-17) stays below the result's; z is FP32, and a token's
 // sum is in the order of its places, so results do not depend on the schedule.
 #include "w4a16_mx.h"
-#include "w4a16_mx_device.h"
+#include "w4a16_mx_stage.h"
 
 namespace w4a16 {
 namespace {
@@ -74,6 +74,16 @@ __device__ __forceinline__ float activate(float g, int activation)
     return 0.5f * g * (1.0f + tanhf(0.7978845608f * (g + 0.044715f * g * g * g)));
 }
 
+// h of pair p as the sum of two BF16 numbers.
+__device__ __forceinline__ void store_hidden(const MoeArgs &a, size_t p, int i, float h)
+{
+    const uint16_t hi = to_16bit(h, 1);
+    const float rest = h - __builtin_bit_cast(float, (uint32_t)hi << 16);
+    uint16_t *const to = a.hidden + p * (size_t)a.I + (size_t)i;
+    to[0] = hi;
+    to[(size_t)a.T * (size_t)a.top_k * (size_t)a.I] = to_16bit(rest, 1);
+}
+
 constexpr int kWaves = 8;
 constexpr int kPassRows = 16;  // of an expert's tokens at a time
 
@@ -88,8 +98,6 @@ __host__ __device__ inline uint32_t x_row(int K) { return (((uint32_t)K * 2u + 1
 __host__ __device__ inline uint32_t scale_group(int K) { return ((uint32_t)K / 2u + 1023u) & ~1023u; }
 template <class Op>
 __host__ __device__ inline uint32_t pass_lds(int K, int rows, int groups) { return (uint32_t)(rows * Op::kTerms) * x_row(K) + (uint32_t)groups * scale_group(K); }
-
-typedef __attribute__((address_space(3))) void *lds_ptr_t;
 
 // KiB `i` of `bytes` bytes at `from` to LDS; zeros past them.
 __device__ __forceinline__ void kib_to_lds(const uint8_t *from, uint32_t bytes, int i, uint8_t *to)
@@ -220,18 +228,48 @@ __device__ __forceinline__ void ask_for(uint8_t *lds, int K, int rows, int group
     }
 }
 
-// The workgroup's expert and its run of pairs; false: none.
+// The workgroup's expert and its run of pairs; false: none.  Up to 64 pairs: every wave finds them by itself, a pair to a lane, the experts in
+// the order of their first pairs; no barrier (gate and down kernel, one token: 17.2 and 12.0 us with the lists in LDS, 15.8 and 11.5 so).
 struct Job {
     int e, begin, end;
+    unsigned long long pairs;  // of up to 64: this expert's
 };
 __device__ __forceinline__ bool find_job(Lists &l, const MoeArgs &a, int t0, Job *j)
 {
-    make_lists(l, a.ids + (size_t)t0 * a.top_k, min(kBlockTokens, a.T - t0) * a.top_k, a.E);
+    const int pairs = min(kBlockTokens, a.T - t0) * a.top_k;
+    const int32_t *const ids = a.ids + (size_t)t0 * a.top_k;
+    if (pairs <= 64) {
+        const int lane = (int)threadIdx.x & 63, e = lane < pairs ? ids[lane] : -1;
+        unsigned long long left = __ballot(e >= 0 && e < a.E), mine = 0;
+        for (int s = 0; s <= (int)blockIdx.y; ++s) {
+            if (left == 0) return false;
+            j->e = __builtin_amdgcn_readlane(e, __builtin_ctzll(left));
+            mine = __ballot(e == j->e);
+            left &= ~mine;
+        }
+        j->pairs = mine;
+        j->begin = 0;
+        j->end = __popcll(mine);
+        if (threadIdx.x < 64 && (mine >> lane & 1)) l.order[__popcll(mine & ((1ull << lane) - 1ull))] = (uint16_t)lane;  // for behind the first barrier
+        return true;
+    }
+    make_lists(l, ids, pairs, a.E);
     if ((int)blockIdx.y >= l.actives) return false;
+    j->pairs = 0;
     j->e = __builtin_amdgcn_readfirstlane(l.active[blockIdx.y]);
     j->begin = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y]);
     j->end = __builtin_amdgcn_readfirstlane(l.begin[blockIdx.y + 1]);
     return true;
+}
+// The pair of row r of the run, the same in every lane.
+__device__ __forceinline__ int pair_of(const Lists &l, const Job &j, int r)
+{
+    if (j.pairs) {
+        unsigned long long m = j.pairs;
+        for (int i = 0; i < r; ++i) m &= m - 1;
+        return __builtin_ctzll(m);
+    }
+    return __builtin_amdgcn_readfirstlane(l.order[r]);
 }
 
 // What the kernels are launched with.
@@ -271,7 +309,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_gate_up_kernel(MoeArgs a, 
         const int rows = min(geo.pass, job.end - r0);
         ask_for<Op>(lds, a.H, rows, 2 * tiles, wave,
                     [&](int r, int) {
-                        const int t = __builtin_amdgcn_readfirstlane(l.order[r0 + r]) / a.top_k;
+                        const int t = pair_of(l, job, r0 + r) / a.top_k;
                         return static_cast<const uint8_t *>(a.X) + (size_t)(t0 + t) * (size_t)a.ldx * 2;
                     },
                     [&](int g) { return a.scales13 + (expert_row + (size_t)(g & 1) * (size_t)a.I + (size_t)tile_row(g >> 1)) * row_s; });
@@ -292,12 +330,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_gate_up_kernel(MoeArgs a, 
                 u += from[w * 512 + 256];
             }
             if (i0 + c < a.I) {
-                const float h = activate(g, a.activation) * u;
-                const uint16_t hi = to_16bit(h, 1);
-                const float low = h - __builtin_bit_cast(float, (uint32_t)hi << 16);
-                uint16_t *const to = a.hidden + ((size_t)t0 * a.top_k + l.order[r0 + r]) * (size_t)a.I + (size_t)(i0 + c);
-                to[0] = hi;
-                to[(size_t)a.T * (size_t)a.top_k * (size_t)a.I] = to_16bit(low, 1);
+                store_hidden(a, (size_t)t0 * a.top_k + l.order[r0 + r], i0 + c, activate(g, a.activation) * u);
             }
         }
         __syncthreads();
@@ -335,7 +368,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_down_kernel(MoeArgs a, Geo
         const int rows = min(geo.pass, job.end - r0);
         ask_for<MxBF16Pair>(lds, a.I, rows, CT * runs, wave,
                             [&](int r, int term) {
-                                const size_t p = (size_t)t0 * a.top_k + (size_t)__builtin_amdgcn_readfirstlane(l.order[r0 + r]);
+                                const size_t p = (size_t)t0 * a.top_k + (size_t)pair_of(l, job, r0 + r);
                                 return reinterpret_cast<const uint8_t *>(a.hidden + p * (size_t)a.I + (term ? second : 0));
                             },
                             [&](int g) { return a.scales2 + (expert_row + (size_t)tile_row(g)) * row_s; });
@@ -365,22 +398,151 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_down_kernel(MoeArgs a, Geo
     }
 }
 
-// Four outputs of a token per thread.
-__global__ __launch_bounds__(256) void moe_combine_kernel(MoeArgs a)
+// ---- experts with many tokens ----
+//
+// With eight tokens to an expert and more, rows of X no longer fit LDS whole beside each other, and reading the weights again for every
+// few of them costs more than they do: the loop of w4a16_mx_stage.h, 16 MT rows at a time.  BF16, us, as above / 16 / 32 rows: 16 tokens to an expert, E = 8, H = I = 4096
+// 133 / 88 / 63; E = 16, H = 7168, I = 2048 206 / 150 / 132; eight, E = 32, H = 2048, I = 1024, four blocks of tokens 137 / 109 / 140; E = 32, H = 4096, I = 2048 113 / 117 / 136;
+// four, E = 128 376 / 401 / 495.
+constexpr int kTileRows = 8, kTileRows2 = 12;  // tokens to an expert, on average: from here on 16 rows at a time, 32 rows
+
+template <class Op, int MT, int WC, int WK, int DEPTH>
+__global__ __launch_bounds__(64 * WC * WK) void moe_gate_up_tile_kernel(MoeArgs a)
 {
-    const long long q = (long long)blockIdx.x * 256 + threadIdx.x;
-    const int quads = a.H / 4;
-    const long long t = q / quads;
-    if (t >= a.T) return;
-    const int h = (int)(q - t * quads) * 4;
-    float4_t v = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < a.top_k; ++j) {
-        const size_t p = (size_t)t * (size_t)a.top_k + (size_t)j;
-        const int e = a.ids[p];
-        if (e < 0 || e >= a.E) continue;
-        const float4_t z = *reinterpret_cast<const float4_t *>(a.partial + p * (size_t)a.H + (size_t)h);
+    using Sh = StageShape<Op, MT, 2, WC, WK, 1, DEPTH>;
+    __shared__ Lists l;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int t0 = (int)blockIdx.z * kBlockTokens;
+    Job job;
+    if (!find_job(l, a, t0, &job)) return;
+    __syncthreads();
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int c = lane & 15, p = lane >> 4, kg = wave / WC, wc = wave - kg * WC;
+    const int i0 = (int)blockIdx.x * 16 * WC;
+    const uint32_t row_w = (uint32_t)a.H / 2, row_s = (uint32_t)a.H / kMxBlock;
+    const size_t expert_row = (size_t)job.e * 2 * (size_t)a.I;
+    auto tile_row = [&](int t) { return min(i0 + 16 * t, a.I - 16); };  // (a tile past the end repeats the last one; not stored)
+
+    StageSource<2> src;
+    src.x = src.x2 = rows_buffer(static_cast<const uint8_t *>(a.X) + (size_t)t0 * (size_t)a.ldx * 2);
+    src.w = a.codes13 + (expert_row + (size_t)tile_row(wc)) * row_w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] += z[i];
+    for (int t = 0; t < 2; ++t) src.wo[t] = (uint32_t)(t * a.I + c) * row_w + (uint32_t)p * 16;
+    const int q = ((int)threadIdx.x - kg * WC * 64) % Sh::kCols;  // row of scales: of wave q / 32 the gate's sixteen, then the up's
+    src.ws = a.scales13 + expert_row * row_s;
+    src.wrow = (uint32_t)((q >> 4 & 1) * a.I + tile_row(q >> 5) + (q & 15)) * row_s;
+    src.xs = nullptr;
+    src.xrow = 0;
+    float4_t *const red = reinterpret_cast<float4_t *>(lds);
+    for (int r0 = job.begin; r0 < job.end; r0 += Sh::kRows) {
+        const int rows = min(Sh::kRows, job.end - r0);
+        uint32_t xo[Sh::kLoads];
+#pragma unroll
+        for (int i = 0; i < Sh::kLoads; ++i) {
+            const int r = Sh::row_of(wc, lane) + i * WC * Sh::kLoadRows;
+            xo[i] = r < rows ? (uint32_t)(l.order[r0 + r] / a.top_k) * (uint32_t)(a.ldx * 2) : kOutOfRange;
+        }
+        float4_t acc[2][MT];
+        stage_product<Op, MT, 2, WC, WK, 1, DEPTH>(acc, src, a.H, kg, wc, lds, [&](int i) { return xo[i]; });
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) red[((kg * WC + wc) * 2 * MT + t * MT + m) * 64 + lane] = acc[t][m];
+        __syncthreads();
+        for (int x = (int)threadIdx.x; x < 16 * WC * rows; x += 64 * WC * WK) {
+            const int r = x / (16 * WC), col = x - r * 16 * WC, at = (((r & 15) >> 2) << 4 | (col & 15)) * 4 + (r & 3);
+            float g = 0.f, u = 0.f;
+            for (int k = 0; k < WK; ++k) {
+                const float *const from = reinterpret_cast<const float *>(red + ((k * WC + (col >> 4)) * 2 * MT + (r >> 4)) * 64) + at;
+                g += from[0];
+                u += from[MT * 256];
+            }
+            if (i0 + col < a.I) store_hidden(a, (size_t)t0 * a.top_k + l.order[r0 + r], i0 + col, activate(g, a.activation) * u);
+        }
+        __syncthreads();
+    }
+}
+
+template <int MT, int CT, int WC, int WK, int DEPTH>
+__global__ __launch_bounds__(64 * WC * WK) void moe_down_tile_kernel(MoeArgs a)
+{
+    using Sh = StageShape<MxBF16Pair, MT, CT, WC, WK, 1, DEPTH>;
+    __shared__ Lists l;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int t0 = (int)blockIdx.z * kBlockTokens;
+    Job job;
+    if (!find_job(l, a, t0, &job)) return;
+    __syncthreads();
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int c = lane & 15, p = lane >> 4, kg = wave / WC, wc = wave - kg * WC;
+    const int n0 = (int)blockIdx.x * Sh::kCols;
+    const uint32_t row_w = (uint32_t)a.I / 2, row_s = (uint32_t)a.I / kMxBlock;
+    const size_t expert_row = (size_t)job.e * (size_t)a.H, first = (size_t)t0 * (size_t)a.top_k;
+    auto tile_row = [&](int t) { return min(n0 + 16 * t, a.H - 16); };
+
+    StageSource<CT> src;
+    src.x = rows_buffer(a.hidden + first * (size_t)a.I);
+    src.x2 = rows_buffer(a.hidden + ((size_t)a.T * (size_t)a.top_k + first) * (size_t)a.I);
+    src.w = a.codes2 + (expert_row + (size_t)tile_row(wc * CT)) * row_w;
+#pragma unroll
+    for (int t = 0; t < CT; ++t) src.wo[t] = (uint32_t)(tile_row(wc * CT + t) - tile_row(wc * CT) + c) * row_w + (uint32_t)p * 16;
+    const int q = ((int)threadIdx.x - kg * WC * 64) % Sh::kCols;
+    src.ws = a.scales2 + expert_row * row_s;
+    src.wrow = (uint32_t)(tile_row(q >> 4) + (q & 15)) * row_s;
+    src.xs = nullptr;
+    src.xrow = 0;
+    float4_t *const red = reinterpret_cast<float4_t *>(lds);
+    for (int r0 = job.begin; r0 < job.end; r0 += Sh::kRows) {
+        const int rows = min(Sh::kRows, job.end - r0);
+        uint32_t xo[Sh::kLoads];
+#pragma unroll
+        for (int i = 0; i < Sh::kLoads; ++i) {
+            const int r = Sh::row_of(wc, lane) + i * WC * Sh::kLoadRows;
+            xo[i] = r < rows ? (uint32_t)l.order[r0 + r] * (uint32_t)a.I * 2 : kOutOfRange;
+        }
+        float4_t acc[CT][MT];
+        stage_product<MxBF16Pair, MT, CT, WC, WK, 1, DEPTH>(acc, src, a.I, kg, wc, lds, [&](int i) { return xo[i]; });
+#pragma unroll
+        for (int t = 0; t < CT; ++t)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) red[((kg * WC + wc) * CT * MT + t * MT + m) * 64 + lane] = acc[t][m];
+        __syncthreads();
+        for (int x = (int)threadIdx.x; x < Sh::kCols * rows; x += 64 * WC * WK) {
+            const int r = x / Sh::kCols, col = x - r * Sh::kCols, at = (((r & 15) >> 2) << 4 | (col & 15)) * 4 + (r & 3);
+            float v = 0.f;
+            for (int k = 0; k < WK; ++k)
+                v += reinterpret_cast<const float *>(red + ((k * WC + col / (16 * CT)) * CT * MT + (col >> 4) % CT * MT + (r >> 4)) * 64)[at];
+            if (n0 + col < a.H) {
+                const size_t pair = first + l.order[r0 + r];
+                a.partial[pair * (size_t)a.H + (size_t)(n0 + col)] = a.weights[pair] * v;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Four outputs of a token per thread; its places' ids first, then their results, eight at a time on their way (one after the other: 5 us instead of 2 for one token).
+__global__ __launch_bounds__(128) void moe_combine_kernel(MoeArgs a)
+{
+    const int h = ((int)blockIdx.x * 128 + (int)threadIdx.x) * 4, t = (int)blockIdx.y;
+    if (h >= a.H) return;
+    const int32_t *const ids = a.ids + (size_t)t * (size_t)a.top_k;
+    const float *const from = a.partial + (size_t)t * (size_t)a.top_k * (size_t)a.H + (size_t)h;
+    float4_t v = {0.f, 0.f, 0.f, 0.f};
+    for (int j0 = 0; j0 < a.top_k; j0 += 8) {
+        float4_t z[8];
+        bool have[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int e = ids[min(j0 + j, a.top_k - 1)];
+            have[j] = j0 + j < a.top_k && e >= 0 && e < a.E;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = *reinterpret_cast<const float4_t *>(from + (size_t)min(j0 + j, a.top_k - 1) * (size_t)a.H);  // (a place without expert: whatever is there)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] += have[j] ? z[j][i] : 0.f;
     }
     uint16_t *const y = static_cast<uint16_t *>(a.Y) + (size_t)t * (size_t)a.ldy + (size_t)h;
 #pragma unroll
@@ -448,18 +610,59 @@ hipError_t launch_down(const MoeArgs &a, int slots, int token_blocks, int tokens
                               : enqueue(&moe_down_kernel<kDownTiles, false, kDepth>, a.H, 16 * kDownTiles, slots, token_blocks, p, a, stream);
 }
 
+// Tiles: four waves side by side, two shares of K.
+constexpr int kTileWC = 4, kTileWK = 2, kTileDepth = 2, kTileCT = 2;
+template <class Sh, class Kernel>
+hipError_t enqueue_tiles(Kernel kernel, int outputs, int width, int slots, int token_blocks, const MoeArgs &a, hipStream_t stream)
+{
+    if (Sh::kLds + kListsLds > 65536) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((outputs + width - 1) / width), (unsigned)slots, (unsigned)token_blocks), dim3(64 * Sh::kWaves), Sh::kLds, stream, a);
+    return hipGetLastError();
+}
+template <class Op, int MT>
+hipError_t launch_gate_up_tiles(const MoeArgs &a, int slots, int token_blocks, hipStream_t stream)
+{
+    return enqueue_tiles<StageShape<Op, MT, 2, kTileWC, kTileWK, 1, kTileDepth>>(&moe_gate_up_tile_kernel<Op, MT, kTileWC, kTileWK, kTileDepth>, a.I, 16 * kTileWC, slots, token_blocks,
+                                                                                 a, stream);
+}
+template <int MT>
+hipError_t launch_down_tiles(const MoeArgs &a, int slots, int token_blocks, hipStream_t stream)
+{
+    using Sh = StageShape<MxBF16Pair, MT, kTileCT, kTileWC, kTileWK, 1, kTileDepth>;
+    return enqueue_tiles<Sh>(&moe_down_tile_kernel<MT, kTileCT, kTileWC, kTileWK, kTileDepth>, a.H, Sh::kCols, slots, token_blocks, a, stream);
+}
+
 }  // namespace
 
 hipError_t launch_moe_experts(const MoeArgs &a, hipStream_t stream)
 {
     const int token_blocks = (a.T + kBlockTokens - 1) / kBlockTokens, tokens = a.T < kBlockTokens ? a.T : kBlockTokens;
     const int slots = a.E < tokens * a.top_k ? a.E : tokens * a.top_k;  // experts that a block can have chosen
-    hipError_t e = a.type == kTypeBF16 ? launch_gate_up<MxBF16>(a, slots, token_blocks, tokens, stream) : launch_gate_up<MxF16>(a, slots, token_blocks, tokens, stream);
+    // Rows that an expert has on average decide; tiles that would leave compute units without one do not count.
+    const int average = tokens * a.top_k / a.E;
+    const bool bf16 = a.type == kTypeBF16;
+    hipError_t e;
+    if (average < kTileRows || (long long)(a.I / (16 * kTileWC)) * slots * token_blocks < 256)
+        e = bf16 ? launch_gate_up<MxBF16>(a, slots, token_blocks, tokens, stream) : launch_gate_up<MxF16>(a, slots, token_blocks, tokens, stream);
+    else if (average < kTileRows2)
+        e = bf16 ? launch_gate_up_tiles<MxBF16, 1>(a, slots, token_blocks, stream) : launch_gate_up_tiles<MxF16, 1>(a, slots, token_blocks, stream);
+    else
+        e = bf16 ? launch_gate_up_tiles<MxBF16, 2>(a, slots, token_blocks, stream) : launch_gate_up_tiles<MxF16, 2>(a, slots, token_blocks, stream);
     if (e != hipSuccess) return e;
-    e = launch_down(a, slots, token_blocks, tokens, stream);
+    if (average < kTileRows || (long long)(a.H / (16 * kTileCT * kTileWC)) * slots * token_blocks < 256) e = launch_down(a, slots, token_blocks, tokens, stream);
+    else e = average < kTileRows2 ? launch_down_tiles<1>(a, slots, token_blocks, stream) : launch_down_tiles<2>(a, slots, token_blocks, stream);
     if (e != hipSuccess) return e;
-    const unsigned long long quads = (unsigned long long)a.T * (unsigned)(a.H / 4);
-    hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)((quads + 255) / 256)), dim3(256), 0, stream, a);
+    for (int t = 0; t < a.T; t += 65535) {  // tokens in a grid's second dimension
+        MoeArgs part = a;
+        part.T = a.T - t < 65535 ? a.T - t : 65535;
+        part.ids = a.ids + (size_t)t * (size_t)a.top_k;
+        part.partial = a.partial + (size_t)t * (size_t)a.top_k * (size_t)a.H;
+        part.Y = static_cast<uint16_t *>(a.Y) + (size_t)t * (size_t)a.ldy;
+        hipLaunchKernelGGL(moe_combine_kernel, dim3((unsigned)((a.H + 511) / 512), (unsigned)part.T), dim3(128), 0, stream, part);
+    }
     return hipGetLastError();
 }
 

@@ -54,6 +54,10 @@ int w4a16_mx_gemm(const void *X, int dtype, long long ldx, const uint8_t *codes,
 int w4a16_mx_gemm_mx(const uint8_t *x_codes, const uint8_t *x_scales, const uint8_t *codes, const uint8_t *scales, int M, int N, int K,
                      void *Y, int dtype, long long ldy, void *stream);
 
+/* What the library runs for a product of this shape: the rows of X and the columns of Y that a workgroup takes (16 columns: the kernel for few rows,
+ * which reads the weights once per 16 rows of X; its workgroups take several times 16).  `x_mx` nonzero: w4a16_mx_gemm_mx. */
+int w4a16_mx_query_tile(int M, int N, int K, int dtype, int x_mx, int *tile_m, int *tile_n);
+
 /*
  * A mixture-of-experts router's choice.  For every token t: the `top_k` experts of the largest logits[t, :] (type `dtype`: FP16, BF16
  * or FP32; rows ld values apart), in descending order, equal ones by ascending index, and their weights:

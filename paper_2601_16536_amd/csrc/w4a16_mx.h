@@ -29,7 +29,7 @@ struct MxGemmArgs {
 float estimate_mx_rows(const MxGemmArgs &a);
 hipError_t launch_mx_rows(const MxGemmArgs &a, hipStream_t stream);
 struct MxTilePlan {
-    int form;
+    int form, tile_m, tile_n;
     float us;
 };
 MxTilePlan plan_mx_tile(const MxGemmArgs &a);

@@ -20,12 +20,19 @@ bool bad_rows(long long rows, int K, long long ld, int per) { return rows > 1 &&
 constexpr long long kMaxLd = 1ll << 23;
 constexpr int kMaxK = 1 << 17, kMaxExpertK = 1 << 15;
 
-// The kernel whose time for the shape is estimated lower; both answer every shape (the tile kernel from K = 128 on) to the same accuracy.
+// The kernel whose time for the shape is estimated lower; both answer every shape (the tile kernel from K = 128 on) to the same accuracy.  tile_n = 16: the
+// one for few rows.
+MxTilePlan plan_product(const MxGemmArgs &a)
+{
+    const MxTilePlan rows = {0, 16, 16, estimate_mx_rows(a)};
+    if (a.K < kMxStep) return rows;
+    const MxTilePlan tiles = plan_mx_tile(a);
+    return rows.us <= tiles.us ? rows : tiles;
+}
 hipError_t launch_product(const MxGemmArgs &a, hipStream_t stream)
 {
-    if (a.K < kMxStep) return launch_mx_rows(a, stream);
-    const MxTilePlan p = plan_mx_tile(a);
-    return estimate_mx_rows(a) <= p.us ? launch_mx_rows(a, stream) : launch_mx_tile(a, p.form, stream);
+    const MxTilePlan p = plan_product(a);
+    return p.tile_n == 16 ? launch_mx_rows(a, stream) : launch_mx_tile(a, p.form, stream);
 }
 
 int check_gemm(int M, int N, int K, int dtype, long long ldy)
@@ -85,6 +92,25 @@ int w4a16_mx_gemm_mx(const uint8_t *x_codes, const uint8_t *x_scales, const uint
     if (!aligned(x_codes, 16) || !aligned(codes, 16) || !aligned(Y, 2)) return W4A16_ERR_ALIGN;
     const MxGemmArgs a = {x_codes, x_scales, codes, scales, Y, K, M > 1 ? ldy : N, M, N, K, dtype};
     return hip_status(launch_product(a, static_cast<hipStream_t>(stream)));
+}
+
+int w4a16_mx_query_tile(int M, int N, int K, int dtype, int x_mx, int *tile_m, int *tile_n)
+{
+    clear_hip_error();
+    const int rc = check_gemm(M, N, K, dtype, N);
+    if (rc) return rc;
+    if (M < 1) return W4A16_ERR_SHAPE;
+    if (!tile_m || !tile_n) return W4A16_ERR_NULL;
+    MxGemmArgs a = {};
+    a.xs = x_mx ? reinterpret_cast<const uint8_t *>(tile_m) : nullptr;  // (asked about, not read)
+    a.M = M;
+    a.N = N;
+    a.K = K;
+    a.type = dtype;
+    const MxTilePlan p = plan_product(a);
+    *tile_m = p.tile_m;
+    *tile_n = p.tile_n;
+    return W4A16_OK;
 }
 
 int w4a16_moe_route(const void *logits, int dtype, int T, int E, long long ld, int top_k, int scoring, int renormalize, float factor,

@@ -131,12 +131,12 @@ hipError_t launch_form(const MxGemmArgs &a, int form, hipStream_t stream)
 MxTilePlan plan_mx_tile(const MxGemmArgs &a)
 {
     const int type = a.xs ? 2 : a.type == kTypeBF16 ? 0 : 1;
-    MxTilePlan best = {0, 0.f};
+    MxTilePlan best = {0, 0, 0, 0.f};
     for (int i = 0; i < kFormCount; ++i) {
         const Form &f = kForms[i];
         const long long tiles = (long long)((a.M + f.rows - 1) / f.rows) * ((a.N + f.cols - 1) / f.cols);
         const float us = kFixed + (float)a.K / 8192.0f * (tiles <= 256 ? f.one[type] : (float)((tiles + 255) / 256) * f.more[type]);
-        if (i == 0 || us < best.us) best = {i, us};
+        if (i == 0 || us < best.us) best = {i, f.rows, f.cols, us};
     }
     return best;
 }

@@ -52,8 +52,8 @@ def route(logits, top_k: int, scoring: str = "softmax", renormalize: bool = True
     if not 1 <= top_k <= min(E, 32) or E > 1024:
         raise ValueError("1 <= top_k <= 32, top_k <= E <= 1024 wanted, not top_k %d of %d" % (top_k, E))
     if out is None:
-        ids = torch.empty((T, top_k), dtype=torch.int32, device=logits.device)
-        weights = torch.empty((T, top_k), dtype=torch.float32, device=logits.device)
+        ids = logits.new_empty((T, top_k), dtype=torch.int32)
+        weights = logits.new_empty((T, top_k), dtype=torch.float32)
     else:
         ids, weights = out
         _check_choice(ids, weights, T)

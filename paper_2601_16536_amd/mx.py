@@ -18,15 +18,16 @@ from .binding import W4A16Error, _stream
 
 F16, BF16, F32 = 0, 1, 2
 
-EXPORTS = ("w4a16_mx_quantize", "w4a16_mx_dequantize", "w4a16_mx_gemm", "w4a16_mx_gemm_mx")
+EXPORTS = ("w4a16_mx_quantize", "w4a16_mx_dequantize", "w4a16_mx_gemm", "w4a16_mx_gemm_mx", "w4a16_mx_query_tile")
 
 _lib = None
 _types = None
+_u8 = None
 
 
 def lib():
     """The loaded library with this module's functions declared."""
-    global _lib, _types
+    global _lib, _types, _u8
     if _lib is None:
         import torch
         L = binding.lib()
@@ -35,7 +36,10 @@ def lib():
         L.w4a16_mx_dequantize.argtypes = [vp, vp, ll, ci, vp, ci, ll, vp]
         L.w4a16_mx_gemm.argtypes = [vp, ci, ll, vp, vp, ci, ci, ci, vp, ll, vp]
         L.w4a16_mx_gemm_mx.argtypes = [vp, vp, vp, vp, ci, ci, ci, vp, ci, ll, vp]
+        ip = ctypes.POINTER(ci)
+        L.w4a16_mx_query_tile.argtypes = [ci, ci, ci, ci, ci, ip, ip]
         _types = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
+        _u8 = torch.uint8
         _lib = L
     return _lib
 
@@ -47,7 +51,8 @@ def _check(rc: int, where: str) -> None:
 
 def type_code(dtype, wide: bool) -> int:
     """The library's number of a torch dtype; `wide`: float32 is allowed too."""
-    lib()
+    if _lib is None:
+        lib()
     code = _types.get(dtype)
     if code is None or (code == F32 and not wide):
         raise TypeError("float16%s or bfloat16 wanted, not %s" % (", float32" if wide else "", dtype))
@@ -69,36 +74,44 @@ def rows_of(X, name: str):
 
 def check_mx(codes, scales, name: str):
     """(leading shape, K) of an MXFP4 pair of tensors."""
-    import torch
-    u8 = torch.uint8
-    if not (codes.is_cuda and scales.is_cuda and codes.dtype is u8 and scales.dtype is u8 and codes.is_contiguous() and scales.is_contiguous()):
+    if _u8 is None:
+        lib()
+    if not (codes.dtype is _u8 and scales.dtype is _u8 and codes.is_cuda and scales.is_cuda and codes.is_contiguous() and scales.is_contiguous()):
         raise TypeError("%s: codes and scales must be contiguous CUDA tensors of dtype torch.uint8" % name)
-    K = codes.shape[-1] * 2
-    if codes.shape[:-1] != scales.shape[:-1] or K < 32 or K % 32 or scales.shape[-1] * 32 != K:
-        raise ValueError("%s: codes %r and scales %r do not fit each other (K / 2 and K / 32 to a row)" % (name, tuple(codes.shape), tuple(scales.shape)))
-    return codes.shape[:-1], K
+    cs, ss = codes.shape, scales.shape
+    lead = cs[:-1]
+    if lead != ss[:-1] or not cs[-1] or cs[-1] != 16 * ss[-1]:
+        raise ValueError("%s: codes %r and scales %r do not fit each other (K / 2 and K / 32 to a row)" % (name, tuple(cs), tuple(ss)))
+    return lead, 2 * cs[-1]
 
 
 def _out_matrix(out, M: int, N: int, like, dtype):
     """The output [M, N] and its leading dimension: new, or `out` checked."""
     if out is None:
-        return like.new_empty((M, N), dtype=dtype), N
+        return (like.new_empty((M, N)) if like.dtype is dtype else like.new_empty((M, N), dtype=dtype)), N
     if not out.is_cuda or out.dtype is not dtype or tuple(out.shape) != (M, N) or (N > 1 and out.stride(1) != 1) or (M > 1 and out.stride(0) < N):
         raise ValueError("out must be a CUDA tensor [%d, %d] of dtype %s whose rows are contiguous" % (M, N, dtype))
     return out, (out.stride(0) if M > 1 else N)
 
 
+def query_tile(M: int, N: int, K: int, dtype=None, x_mx: bool = False) -> tuple:
+    """(rows of X, columns of Y) that a workgroup of gemm (dtype: X's), or with x_mx of gemm_mx, takes for this shape; 16 columns: the kernel for few rows."""
+    import torch
+    tm, tn = ctypes.c_int(), ctypes.c_int()
+    _check(lib().w4a16_mx_query_tile(M, N, K, type_code(dtype or torch.bfloat16, False), int(x_mx), ctypes.byref(tm), ctypes.byref(tn)), "w4a16_mx_query_tile")
+    return tm.value, tn.value
+
+
 def quantize(X, out=None, stream=None):
     """X [..., K] -> (codes uint8 [..., K/2], scales uint8 [..., K/32]).  A matrix may have a row stride.  `out`: the pair to fill."""
-    import torch
     code = type_code(X.dtype, True)
     rows, K, ld = rows_of(X, "X")
     if K < 32 or K % 32:
         raise ValueError("the last dimension must be a multiple of 32, not %d" % K)
     lead = X.shape[:-1]
     if out is None:
-        codes = torch.empty((*lead, K // 2), dtype=torch.uint8, device=X.device)
-        scales = torch.empty((*lead, K // 32), dtype=torch.uint8, device=X.device)
+        codes = X.new_empty((*lead, K // 2), dtype=_u8)
+        scales = X.new_empty((*lead, K // 32), dtype=_u8)
     else:
         codes, scales = out
         if check_mx(codes, scales, "out") != (lead, K):

@@ -407,7 +407,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_down_kernel(MoeArgs a, Geo
 constexpr int kTileRows = 8, kTileRows2 = 12;  // tokens to an expert, on average: from here on 16 rows at a time, 32 rows
 
 template <class Op, int MT, int WC, int WK, int DEPTH>
-__global__ __launch_bounds__(64 * WC * WK) void moe_gate_up_tile_kernel(MoeArgs a)
+__global__ __launch_bounds__(64 * WC * WK, 4) void moe_gate_up_tile_kernel(MoeArgs a)
 {
     using Sh = StageShape<Op, MT, 2, WC, WK, 1, DEPTH>;
     __shared__ Lists l;
@@ -428,7 +428,7 @@ __global__ __launch_bounds__(64 * WC * WK) void moe_gate_up_tile_kernel(MoeArgs 
     src.w = a.codes13 + (expert_row + (size_t)tile_row(wc)) * row_w;
 #pragma unroll
     for (int t = 0; t < 2; ++t) src.wo[t] = (uint32_t)(t * a.I + c) * row_w + (uint32_t)p * 16;
-    const int q = ((int)threadIdx.x - kg * WC * 64) % Sh::kCols;  // row of scales: of wave q / 32 the gate's sixteen, then the up's
+    const int q = Sh::scale_w_row();  // row of scales: of wave q / 32 the gate's sixteen, then the up's
     src.ws = a.scales13 + expert_row * row_s;
     src.wrow = (uint32_t)((q >> 4 & 1) * a.I + tile_row(q >> 5) + (q & 15)) * row_s;
     src.xs = nullptr;
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(64 * WC * WK) void moe_gate_up_tile_kernel(MoeArgs 
         uint32_t xo[Sh::kLoads];
 #pragma unroll
         for (int i = 0; i < Sh::kLoads; ++i) {
-            const int r = Sh::row_of(wc, lane) + i * WC * Sh::kLoadRows;
+            const int r = Sh::load_row(wave, i) + Sh::lane_row(lane);
             xo[i] = r < rows ? (uint32_t)(l.order[r0 + r] / a.top_k) * (uint32_t)(a.ldx * 2) : kOutOfRange;
         }
         float4_t acc[2][MT];
@@ -464,7 +464,7 @@ __global__ __launch_bounds__(64 * WC * WK) void moe_gate_up_tile_kernel(MoeArgs 
 }
 
 template <int MT, int CT, int WC, int WK, int DEPTH>
-__global__ __launch_bounds__(64 * WC * WK) void moe_down_tile_kernel(MoeArgs a)
+__global__ __launch_bounds__(64 * WC * WK, 4) void moe_down_tile_kernel(MoeArgs a)
 {
     using Sh = StageShape<MxBF16Pair, MT, CT, WC, WK, 1, DEPTH>;
     __shared__ Lists l;
@@ -486,7 +486,7 @@ __global__ __launch_bounds__(64 * WC * WK) void moe_down_tile_kernel(MoeArgs a)
     src.w = a.codes2 + (expert_row + (size_t)tile_row(wc * CT)) * row_w;
 #pragma unroll
     for (int t = 0; t < CT; ++t) src.wo[t] = (uint32_t)(tile_row(wc * CT + t) - tile_row(wc * CT) + c) * row_w + (uint32_t)p * 16;
-    const int q = ((int)threadIdx.x - kg * WC * 64) % Sh::kCols;
+    const int q = Sh::scale_w_row();
     src.ws = a.scales2 + expert_row * row_s;
     src.wrow = (uint32_t)(tile_row(q >> 4) + (q & 15)) * row_s;
     src.xs = nullptr;
@@ -497,7 +497,7 @@ __global__ __launch_bounds__(64 * WC * WK) void moe_down_tile_kernel(MoeArgs a)
         uint32_t xo[Sh::kLoads];
 #pragma unroll
         for (int i = 0; i < Sh::kLoads; ++i) {
-            const int r = Sh::row_of(wc, lane) + i * WC * Sh::kLoadRows;
+            const int r = Sh::load_row(wave, i) + Sh::lane_row(lane);
             xo[i] = r < rows ? (uint32_t)l.order[r0 + r] * (uint32_t)a.I * 2 : kOutOfRange;
         }
         float4_t acc[CT][MT];

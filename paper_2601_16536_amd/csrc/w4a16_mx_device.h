@@ -92,6 +92,7 @@ struct MxF16 {
 };
 struct MxFP4 {
     static constexpr bool kMx = true;
+    static constexpr bool kScaled = true;
     static constexpr int kTerms = 1;
     static __device__ __forceinline__ float4_t multiply(uint4_t x, uint32_t xs, uint4_t w, uint32_t ws, float4_t acc)
     {

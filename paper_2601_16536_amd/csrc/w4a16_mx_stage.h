@@ -2,13 +2,16 @@
 // wave that multiplies them: many rows of X (w4a16_mx_tile.hip), experts with many tokens (w4a16_moe_experts.hip).
 //
 // A workgroup owns 16 MT rows of X and 16 CT WC rows of W: WC waves side by side, each with MT x CT tiles of sums, and WK such groups that
-// have a share of K each.  K goes by stages of 128 STEPS values; a stage's X (loads into LDS) and codes (loads into registers) are asked for
-// DEPTH - 1 stages ahead, one barrier per stage.  Every group has as many whole stages; what is left, WK - 1 whole ones at
-// most and one that K ends in, follows in a round of its own, so that nothing in the loop depends on how far K goes: a load, a wait or a shift
-// under a condition there has the compiler wait for everything that is on its way.
+// share K: a stage is 128 STEPS values for each group, one group's behind the other's.  A stage's X (loads into LDS) and codes (loads into registers) are
+// asked for DEPTH - 1 stages ahead, one barrier per stage.  What K has beyond whole stages follows in a round of its own, so that nothing in the loop
+// depends on how far K goes: a load, a wait or a shift under a condition there has the compiler wait for everything that is on its way.
 //
-// X in LDS: rows of 256 STEPS (64 STEPS) bytes, in which the 16-byte piece q of row r lies at place q ^ (r mod the pieces of a row), so that sixteen rows of a step use all
-// banks evenly.
+// The memory pipeline takes a load's lines one by one: a KiB of one row 23 cycles, of four rows 43, of sixteen (the codes, 64 bytes of a row) about 100.  So the
+// groups' parts of a stage lie side by side: with four groups X comes in whole KiB of a row, and a row's codes are four waves' at the same time.  (Each group in a
+// quarter of K of its own, 32 x 64 tiles, M = 37, K = 10240, N = 4608, BF16: 21.7 us, 18.6 so; 16 x 32 tiles, M = 16, K = 28672, N = 8192 34.4 and 26.1.)
+//
+// X in LDS: a group's part of a row, 256 STEPS (64 STEPS) bytes, has the 16-byte piece q of row r at place q ^ (r mod the part's pieces), so that sixteen rows of a step
+// use all banks evenly.
 #pragma once
 #include "w4a16_mx_device.h"
 #include <type_traits>
@@ -23,24 +26,30 @@ struct StageShape {
     static constexpr int kStage = STEPS * kMxStep;
     static constexpr int kRowBytes = STEPS * (Op::kMx ? 64 : 256);  // of X per stage
     static constexpr int kPieces = kRowBytes / 16;
-    static constexpr int kLoadRows = 64 / kPieces;             // of one wave's load
-    static constexpr int kLoads = kRows / (WC * kLoadRows);    // of a wave per stage
-    static constexpr int kXBytes = kRows * kRowBytes, kBuffer = Op::kTerms * kXBytes;
-    static constexpr int kWindow = 4 / STEPS;                  // stages that sixteen scales of a row last
-    static constexpr int kScaleRows = kCols + (Op::kMx ? kRows : 0), kScaleBytes = kScaleRows * 16;
-    static constexpr int kGroup = DEPTH * kBuffer + 2 * kScaleBytes;  // LDS of a group
+    static constexpr int kRow = WK * kRowBytes;                // of all groups
+    static constexpr int kLoads = kRows * kRow / (1024 * kWaves);  // of a wave per stage, a KiB each
+    static constexpr int kXBytes = kRows * kRow, kBuffer = Op::kTerms * kXBytes;
+    static constexpr int kWindow = 4 / STEPS;                  // stages that a window of scales lasts: sixteen of a row for each group
+    static constexpr int kScaleRows = kCols + (Op::kMx ? kRows : 0), kScaleRow = 16 * WK, kScaleBytes = kScaleRows * kScaleRow;
     static constexpr int kRound = DEPTH % kWindow == 0 ? DEPTH : kWindow % DEPTH == 0 ? kWindow : DEPTH * kWindow;  // stages of the unrolled loop
-    static constexpr int kSums = WK > 1 ? kWaves * CT * MT * 1024 : 0;
-    static constexpr int kLds = WK * kGroup > kSums ? WK * kGroup : kSums;
+    static constexpr int kSums = WK > 1 ? kWaves * CT * MT * 1024 : 0, kStages = DEPTH * kBuffer + 2 * kScaleBytes;
+    static constexpr int kLds = kStages > kSums ? kStages : kSums;
     static constexpr int kPerStage = Op::kTerms * kLoads + CT * STEPS;      // loads that a wave asks for, scales aside
-    static_assert(kRows % (WC * kLoadRows) == 0 && kRows <= 64 * WC, "whole loads");
-    static constexpr int kPlaces = kPieces > WC * kLoadRows ? kPieces / (WC * kLoadRows) : 1;  // of a lane's piece, in loads that follow each other
-    static_assert((WC * kLoadRows) % kPieces == 0 || kPieces % (WC * kLoadRows) == 0, "places repeat");
-    static_assert(kRound % DEPTH == 0 && kRound % kWindow == 0 && kCols <= 64 * WC, "static places");
-    // A lane's part in the loads of X: load i brings row rows_of(wave of the group, lane) + i WC kLoadRows, of it piece piece_of(..., i mod kPlaces).
+    static_assert(kRows * kRow % (1024 * kWaves) == 0 && (kRow % 1024 == 0 || 1024 % kRow == 0), "whole loads");
+    static_assert(kRound % DEPTH == 0 && kRound % kWindow == 0, "static places");
+    static_assert(kCols <= 64 * WC && kRows <= 64 * WC, "a thread brings a row's sixteen scales of a group");
     static __device__ __forceinline__ int place(int piece, int row) { return kPieces > 4 ? piece ^ (row % kPieces) : piece; }  // (rows of 64 bytes: sixteen of them are all banks four times)
-    static __device__ __forceinline__ int row_of(int wc, int lane) { return wc * kLoadRows + lane / kPieces; }
-    static __device__ __forceinline__ int piece_of(int wc, int lane, int v) { return place(lane % kPieces, row_of(wc, lane) + v * WC * kLoadRows); }
+    // Load i of a wave brings row load_row + lane_row, of it the 16 bytes from load_byte on.
+    static __device__ __forceinline__ int load_row(int wave, int i) { return kRow >= 1024 ? (i * kWaves + wave) / (kRow / 1024 > 0 ? kRow / 1024 : 1) : (i * kWaves + wave) * (1024 / kRow); }
+    static __device__ __forceinline__ int lane_row(int lane) { return lane * 16 / (kRow < 1024 ? kRow : 1024); }
+    static __device__ __forceinline__ int load_byte(int wave, int lane, int i)
+    {
+        const int in_row = kRow >= 1024 ? (i * kWaves + wave) * 1024 % kRow + lane * 16 : lane * 16 % kRow;
+        return in_row / kRowBytes * kRowBytes + place(in_row % kRowBytes / 16, load_row(wave, i) + lane_row(lane)) * 16;
+    }
+    // The row of W and of X whose scales a thread brings (past the last: those of others again).
+    static __device__ __forceinline__ int scale_w_row() { return (int)threadIdx.x / WK % kCols; }
+    static __device__ __forceinline__ int scale_x_row() { return (int)threadIdx.x / WK % kRows; }
     static_assert(kPerStage * (DEPTH - 2) < 64, "what s_waitcnt counts");
 };
 
@@ -50,17 +59,18 @@ __device__ __forceinline__ void to_lds(__amdgpu_buffer_rsrc_t r, uint32_t offset
     __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr_t)to, 16, offset, base, 0, 0);
 }
 
-// Sixteen bytes of a row of `blocks` scales from place `at` on, as far as they are there (zeros past the end).  Rows begin at any byte.
-__device__ __forceinline__ uint4_t scale_window(const uint8_t *from, uint32_t row, int at, int blocks)
+// Sixteen of a window's `span` bytes of a row of `blocks` scales: the window begins at place `at`, the sixteen `part` bytes on (in `row` too); as far as they are
+// there (zeros past the end).  Rows begin at any byte.
+__device__ __forceinline__ uint4_t scale_window(const uint8_t *from, uint32_t row, int at, int part, int span, int blocks)
 {
     uint4_t v = {0u, 0u, 0u, 0u};
-    if (at + 16 <= blocks) {
+    if (at + span <= blocks) {
         const uint8_t *const here = from + at;
         __builtin_memcpy(&v, here + row, 16);
     } else
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-            if (at + j < blocks) v[j >> 2] |= (uint32_t)(from + at + j)[row] << (8 * (j & 3));
+            if (at + part + j < blocks) v[j >> 2] |= (uint32_t)(from + at + j)[row] << (8 * (j & 3));
     return v;
 }
 
@@ -73,49 +83,50 @@ struct StageSource {
     __amdgpu_buffer_rsrc_t x, x2;  // X; its second term (kTerms = 2)
     const uint8_t *w;              // codes; wo: the lane's row (row lane mod 16 of tile t) and 16 (lane / 16) bytes
     uint32_t wo[CT];
-    const uint8_t *ws, *xs;        // scales of W's rows, of X's (MXFP4 X): the thread's rows begin wrow and xrow bytes on (thread mod the rows there are)
+    const uint8_t *ws, *xs;        // scales of W's rows, of X's (MXFP4 X): rows scale_w_row and scale_x_row begin wrow and xrow bytes on
     uint32_t wrow, xrow;
 };
 
 // acc = X W^T over the share of group kg; acc as the 16 x 16 MFMAs have it.  row(i): where the lane's row of load i begins in x, kOutOfRange if there is
-// none.  lds: WK kGroup bytes.  Every thread of the workgroup has to call this.
+// none.  lds: kLds bytes.  Every thread of the workgroup has to call this.
 template <class Op, int MT, int CT, int WC, int WK, int STEPS, int DEPTH, class Row>
 __device__ __forceinline__ void stage_product(float4_t (&acc)[CT][MT], const StageSource<CT> &src, int K, int kg, int wc, uint8_t *lds, Row row)
 {
     using Sh = StageShape<Op, MT, CT, WC, WK, STEPS, DEPTH>;
     const int lane = (int)threadIdx.x & 63, c = lane & 15, p = lane >> 4;
     const int blocks = K / kMxBlock, stages = (K + Sh::kStage - 1) / Sh::kStage;
-    const int share = K / Sh::kStage / WK, s0 = kg * share;  // a group's whole stages, and its first
+    const int share = K / (Sh::kStage * WK), wave = kg * WC + wc;  // whole stages
 
     // ---- X ----
-    uint8_t *const xs = lds + kg * Sh::kGroup;
-    auto fetch_x = [&](int s, int buf, bool last) {
+    // (stages are numbered group by group: the groups' parts of stage i are i WK .. i WK + WK - 1)
+    auto fetch_x = [&](int i0, int buf, bool last) {
 #pragma unroll
         for (int h = 0; h < Op::kTerms; ++h)
 #pragma unroll
             for (int i = 0; i < Sh::kLoads; ++i) {
-                uint32_t o = row(i) + (uint32_t)Sh::piece_of(wc, lane, i % Sh::kPlaces) * 16;
-                if (last && s * Sh::kStage + Sh::piece_of(wc, lane, i % Sh::kPlaces) * (Op::kMx ? 32 : 8) >= K) o = kOutOfRange;  // past the rows' end
-                to_lds(h ? src.x2 : src.x, o, s * Sh::kRowBytes, xs + buf * Sh::kBuffer + h * Sh::kXBytes + (i * WC + wc) * 1024);
+                const int byte = Sh::load_byte(wave, lane, i);
+                uint32_t o = row(i) + (uint32_t)byte;
+                if (last && i0 * WK * Sh::kStage + byte * (Op::kMx ? 2 : 1) / (Op::kMx ? 1 : 2) >= K) o = kOutOfRange;  // past the rows' end
+                to_lds(h ? src.x2 : src.x, o, i0 * Sh::kRow, lds + buf * Sh::kBuffer + h * Sh::kXBytes + (i * Sh::kWaves + wave) * 1024);
             }
     };
 
     // ---- scales ----
-    // Sixteen of a row last for 512 values of K: asked for a window ahead, a row to a thread, and from there through LDS.  (A word per step and
+    // Sixteen of a row and group last for 512 values of its K: asked for a window ahead, and from there through LDS.  (A word per step and
     // tile, read where it is used, is sixteen requests to L2 for 64 bytes of use: M = 2048, K = N = 8192, BF16 220 us so, 195 through LDS; MXFP4 X 190 and 92.)
-    uint8_t *const sc = xs + DEPTH * Sh::kBuffer;
-    const int in_group = (int)threadIdx.x - kg * WC * 64;
+    uint8_t *const sc = lds + DEPTH * Sh::kBuffer;
+    const int part = (int)threadIdx.x % WK * 16;
     struct Window {
         uint4_t w, x;
     };
     auto fetch_scales = [&](Window &v, int at) {  // from block `at`
-        if (wc * 64 < Sh::kCols) v.w = scale_window(src.ws, src.wrow, at, blocks);
-        if (Op::kMx && wc * 64 < Sh::kRows) v.x = scale_window(src.xs, src.xrow, at, blocks);
+        if (wave * 64 < Sh::kCols * WK) v.w = scale_window(src.ws, src.wrow + (uint32_t)part, at, part, Sh::kScaleRow, blocks);
+        if (Op::kMx && wave * 64 < Sh::kRows * WK) v.x = scale_window(src.xs, src.xrow + (uint32_t)part, at, part, Sh::kScaleRow, blocks);
     };
     auto store_scales = [&](const Window &v, int buf) {
         uint8_t *const to = sc + buf * Sh::kScaleBytes;
-        if (wc * 64 < Sh::kCols) *reinterpret_cast<uint4_t *>(to + (in_group % Sh::kCols) * 16) = v.w;
-        if (Op::kMx && wc * 64 < Sh::kRows) *reinterpret_cast<uint4_t *>(to + (Sh::kCols + in_group % Sh::kRows) * 16) = v.x;
+        if (wave * 64 < Sh::kCols * WK) *reinterpret_cast<uint4_t *>(to + Sh::scale_w_row() * Sh::kScaleRow + part) = v.w;
+        if (Op::kMx && wave * 64 < Sh::kRows * WK) *reinterpret_cast<uint4_t *>(to + (Sh::kCols + Sh::scale_x_row()) * Sh::kScaleRow + part) = v.x;
     };
 
     // ---- W ----
@@ -139,12 +150,12 @@ __device__ __forceinline__ void stage_product(float4_t (&acc)[CT][MT], const Sta
         for (int m = 0; m < MT; ++m) acc[t][m] = (float4_t){0.f, 0.f, 0.f, 0.f};
 
     auto compute = [&](Weights &f, int s, int buf, int sbuf, int splace, bool last) {  // scales: buffer and the stage's place in the window
-        const uint8_t *const x = xs + buf * Sh::kBuffer, *const from = sc + sbuf * Sh::kScaleBytes + splace * STEPS * 4;
+        const uint8_t *const x = lds + buf * Sh::kBuffer + kg * Sh::kRowBytes, *const from = sc + sbuf * Sh::kScaleBytes + (splace * WK + kg) * STEPS * 4;
         uint32_t wsc[CT][STEPS];
 #pragma unroll
         for (int t = 0; t < CT; ++t)
 #pragma unroll
-            for (int h = 0; h < STEPS; ++h) wsc[t][h] = *reinterpret_cast<const uint32_t *>(from + ((wc * CT + t) * 16 + c) * 16 + h * 4);
+            for (int h = 0; h < STEPS; ++h) wsc[t][h] = *reinterpret_cast<const uint32_t *>(from + ((wc * CT + t) * 16 + c) * Sh::kScaleRow + h * 4);
         if constexpr (Op::kMx) {
             // Rows of X by fours (by twos), the next ones on their way while these are multiplied; no further ahead, for the registers.
             constexpr int kRun = MT < 4 ? MT : 4, kRuns = STEPS * MT / kRun;
@@ -154,8 +165,8 @@ __device__ __forceinline__ void stage_product(float4_t (&acc)[CT][MT], const Sta
                 const int h = r / (MT / kRun), m0 = r % (MT / kRun) * kRun;
 #pragma unroll
                 for (int m = 0; m < kRun; ++m) {
-                    xa[r & 1][m] = *reinterpret_cast<const uint4_t *>(x + ((m0 + m) * 16 + c) * Sh::kRowBytes + Sh::place(h * 4 + p, c) * 16);
-                    sx[r & 1][m] = *reinterpret_cast<const uint32_t *>(from + (Sh::kCols + (m0 + m) * 16 + c) * 16 + h * 4) >> (8 * p);
+                    xa[r & 1][m] = *reinterpret_cast<const uint4_t *>(x + ((m0 + m) * 16 + c) * Sh::kRow + Sh::place(h * 4 + p, c) * 16);
+                    sx[r & 1][m] = *reinterpret_cast<const uint32_t *>(from + (Sh::kCols + (m0 + m) * 16 + c) * Sh::kScaleRow + h * 4) >> (8 * p);
                 }
             };
             read(0);
@@ -180,7 +191,7 @@ __device__ __forceinline__ void stage_product(float4_t (&acc)[CT][MT], const Sta
 #pragma unroll
                 for (int h = 0; h < Op::kTerms; ++h)
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) xa[h][m] = *reinterpret_cast<const uint4_t *>(x + h * Sh::kXBytes + (m * 16 + c) * Sh::kRowBytes + Sh::place(j * 4 + p, c) * 16);
+                    for (int m = 0; m < MT; ++m) xa[h][m] = *reinterpret_cast<const uint4_t *>(x + h * Sh::kXBytes + (m * 16 + c) * Sh::kRow + Sh::place(j * 4 + p, c) * 16);
                 if constexpr (Op::kScaled) {
 #pragma unroll
                     for (int t = 0; t < CT; ++t) {
@@ -232,7 +243,7 @@ __device__ __forceinline__ void stage_product(float4_t (&acc)[CT][MT], const Sta
     };
     auto fetch = [&](Weights &f, int s, int buf, bool last) {
         fetch_x(s, buf, last);
-        fetch_w(f, s, last);
+        fetch_w(f, s * WK + kg, last);
     };
     // A stage is there, for every wave: all but the `later` loads asked for after it.
     auto arrive = [&](auto later) {
@@ -242,14 +253,14 @@ __device__ __forceinline__ void stage_product(float4_t (&acc)[CT][MT], const Sta
     };
     constexpr std::integral_constant<int, Sh::kPerStage *(DEPTH - 2)> kLater{};
     constexpr std::integral_constant<int, 0> kNone{};
-    auto window_at = [&](int w) { return (s0 + w * Sh::kWindow) * STEPS * kMxStepBlocks; };
+    auto window_at = [&](int w) { return w * Sh::kScaleRow; };
 
     Weights f[DEPTH];
     Window v;
     fetch_scales(v, window_at(0));
 #pragma unroll
     for (int d = 0; d < DEPTH - 1; ++d)
-        if (d < share) fetch(f[d], s0 + d, d, false);
+        if (d < share) fetch(f[d], d, d, false);
     store_scales(v, 0);
     if (share >= DEPTH - 1) arrive(kLater);
     else arrive(kNone);
@@ -260,9 +271,9 @@ __device__ __forceinline__ void stage_product(float4_t (&acc)[CT][MT], const Sta
         for (int d = 0; d < Sh::kRound; ++d) {
             const int w = (i + d) / Sh::kWindow;
             if (d % Sh::kWindow == 0) fetch_scales(v, window_at(w + 1));
-            fetch(f[(d + DEPTH - 1) % DEPTH], s0 + i + d + DEPTH - 1, (d + DEPTH - 1) % DEPTH, false);
+            fetch(f[(d + DEPTH - 1) % DEPTH], i + d + DEPTH - 1, (d + DEPTH - 1) % DEPTH, false);
             __builtin_amdgcn_sched_barrier(0);
-            compute(f[d % DEPTH], s0 + i + d, d % DEPTH, w & 1, d % Sh::kWindow, false);
+            compute(f[d % DEPTH], (i + d) * WK + kg, d % DEPTH, w & 1, d % Sh::kWindow, false);
             settle();
             if (d % Sh::kWindow == Sh::kWindow - 1) store_scales(v, (w + 1) & 1);
             arrive(kLater);
@@ -273,19 +284,18 @@ __device__ __forceinline__ void stage_product(float4_t (&acc)[CT][MT], const Sta
             if (i + d < share) {
                 const int w = (i + d) / Sh::kWindow;
                 if (d % Sh::kWindow == 0) fetch_scales(v, window_at(w + 1));
-                if (i + d + DEPTH - 1 < share) fetch(f[(d + DEPTH - 1) % DEPTH], s0 + i + d + DEPTH - 1, (d + DEPTH - 1) % DEPTH, false);
-                compute(f[d % DEPTH], s0 + i + d, d % DEPTH, w & 1, d % Sh::kWindow, false);
+                if (i + d + DEPTH - 1 < share) fetch(f[(d + DEPTH - 1) % DEPTH], i + d + DEPTH - 1, (d + DEPTH - 1) % DEPTH, false);
+                compute(f[d % DEPTH], (i + d) * WK + kg, d % DEPTH, w & 1, d % Sh::kWindow, false);
                 settle();
                 if (d % Sh::kWindow == Sh::kWindow - 1) store_scales(v, (w + 1) & 1);
                 arrive(kNone);
             }
     if (share * WK < stages) {
         const int s = share * WK + kg;
-        if (s < stages) {
-            fetch_scales(v, s * STEPS * kMxStepBlocks);
-            fetch(f[0], s, 0, true);
-            store_scales(v, 0);
-        }
+        fetch_scales(v, share * WK * STEPS * kMxStepBlocks);
+        fetch_x(share, 0, true);
+        if (s < stages) fetch_w(f[0], s, true);
+        store_scales(v, 0);
         arrive(kNone);
         if (s < stages) compute(f[0], s, 0, 0, 0, true);
         __syncthreads();

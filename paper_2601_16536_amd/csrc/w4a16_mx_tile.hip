@@ -23,17 +23,17 @@ __global__ __launch_bounds__(64 * WC * WK, PER_CU) void mx_tile_kernel(MxGemmArg
     src.x = src.x2 = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(static_cast<const uint8_t *>(a.X) + (size_t)m0 * row_x), 0,
                                                        (uint32_t)(rows - 1) * row_x + (Op::kMx ? row_w : (uint32_t)a.K * 2u), kRawBuffer);
     // rows of W past the end: the last one
-    const int base = min(n0, a.N - 1), in_group = (int)threadIdx.x - kg * WC * 64;
+    const int base = min(n0, a.N - 1);
     src.w = a.codes + (size_t)base * row_w;
 #pragma unroll
     for (int t = 0; t < CT; ++t) src.wo[t] = (uint32_t)min(16 * t + c, a.N - 1 - base) * row_w + (uint32_t)p * 16;
     src.ws = a.scales + (size_t)first_n * row_s;
-    src.wrow = (uint32_t)min(in_group % Sh::kCols, a.N - 1 - first_n) * row_s;
+    src.wrow = (uint32_t)min(Sh::scale_w_row(), a.N - 1 - first_n) * row_s;
     src.xs = Op::kMx ? a.xs + (size_t)m0 * row_s : nullptr;
-    src.xrow = (uint32_t)min(in_group % Sh::kRows, rows - 1) * row_s;
-    const uint32_t xrow0 = (uint32_t)Sh::row_of(wc, lane) * row_x;
+    src.xrow = (uint32_t)min(Sh::scale_x_row(), rows - 1) * row_s;
+    const uint32_t lane_x = (uint32_t)Sh::lane_row(lane) * row_x;
     float4_t acc[CT][MT];
-    stage_product<Op, MT, CT, WC, WK, STEPS, DEPTH>(acc, src, a.K, kg, wc, lds, [&](int i) { return xrow0 + (uint32_t)(i * WC * Sh::kLoadRows) * row_x; });
+    stage_product<Op, MT, CT, WC, WK, STEPS, DEPTH>(acc, src, a.K, kg, wc, lds, [&](int i) { return lane_x + (uint32_t)Sh::load_row(wave, i) * row_x; });
 
     // ---- Y ----
     uint16_t *const y = static_cast<uint16_t *>(a.Y);
@@ -99,14 +99,15 @@ struct Form {
     int rows, cols;
     float one[3], more[3];
 };
+constexpr float kNever = 1e9f;
 constexpr Form kForms[] = {
-    {16, 32, {9.0f, 9.5f, 7.1f}, {9.0f, 9.5f, 7.1f}},            // eight shares of K
-    {32, 32, {13.5f, 14.5f, 9.5f}, {12.5f, 13.5f, 8.5f}},        // four, two workgroups to a compute unit
-    {32, 64, {18.0f, 19.0f, 15.0f}, {17.5f, 19.0f, 14.5f}},      // four
-    {64, 64, {24.0f, 25.0f, 18.0f}, {25.0f, 27.0f, 18.0f}},      // four
-    {64, 128, {36.5f, 45.0f, 28.5f}, {34.0f, 42.0f, 23.0f}},     // two
-    {128, 128, {60.0f, 90.0f, 31.0f}, {58.0f, 77.0f, 29.0f}},    // one, two workgroups to a compute unit
-    {128, 256, {97.0f, 188.0f, 56.0f}, {97.0f, 152.0f, 54.0f}},  // one, two workgroups to a compute unit
+    {16, 32, {9.7f, 10.2f, 8.8f}, {9.3f, 9.9f, 6.9f}},           // eight shares of K
+    {32, 32, {11.0f, 11.5f, 9.5f}, {11.2f, 12.3f, 6.5f}},        // four, two workgroups to a compute unit
+    {32, 64, {15.5f, 16.5f, kNever}, {15.6f, 17.5f, kNever}},    // four (MXFP4 X: 13.0 and 13.0, never less than its neighbours)
+    {64, 64, {23.0f, 24.0f, 15.0f}, {24.7f, 26.0f, 16.0f}},      // four
+    {64, 128, {36.5f, 42.5f, 25.7f}, {31.5f, 44.5f, 27.0f}},     // two
+    {128, 128, {56.0f, 88.0f, 30.0f}, {56.0f, 73.7f, 29.0f}},    // one, two workgroups to a compute unit
+    {128, 256, {92.0f, kNever, 54.0f}, {97.0f, kNever, 54.5f}},  // one, two workgroups to a compute unit (FP16, whose sums per block need the registers: 205 and 161)
 };
 constexpr int kFormCount = sizeof(kForms) / sizeof(kForms[0]);
 constexpr float kFixed = 3.0f;  // launch, first loads, last sums
@@ -115,14 +116,18 @@ template <class Op>
 hipError_t launch_form(const MxGemmArgs &a, int form, hipStream_t stream)
 {
     constexpr bool mx = Op::kMx;
-    switch (form) {
+    switch (form) {  // (a form whose time is kNever is not planned)
     case 0: return launch<Op, 1, 1, 2, 8, mx ? 4 : 1, mx ? 2 : 4, 4>(a, stream);
     case 1: return launch<Op, 2, 1, 2, 4, mx ? 4 : 1, mx ? 2 : 4, 4>(a, stream);
-    case 2: return launch<Op, 2, 1, 4, 4, mx ? 2 : 1, mx ? 2 : 4, 4>(a, stream);
-    case 3: return launch<Op, 4, 1, 4, 4, 1, 2, 4>(a, stream);
-    case 4: return launch<Op, 4, 2, 4, 2, 1, 2, 2>(a, stream);
+    case 2:
+        if constexpr (mx) return hipErrorInvalidValue;
+        else return launch<Op, 2, 1, 4, 4, 1, 4, 4>(a, stream);
+    case 3: return launch<Op, 4, 1, 4, 4, mx ? 2 : 1, 2, 4>(a, stream);
+    case 4: return launch<Op, 4, 2, 4, 2, mx ? 2 : 1, 2, 2>(a, stream);
     case 5: return launch<Op, 8, 2, 4, 1, 1, mx ? 4 : 2, 2>(a, stream);
-    default: return launch<Op, 8, 4, 4, 1, 1, 2, 2>(a, stream);
+    default:
+        if constexpr (!mx && !Op::kScaled) return hipErrorInvalidValue;
+        else return launch<Op, 8, 4, 4, 1, 1, 2, 2>(a, stream);
     }
 }
 

@@ -1,9 +1,10 @@
-// A mixture of experts' feed-forward layers for a few tokens:
+// A mixture of experts' feed-forward layers for one to some hundred tokens:
 //     h_p = act(W1_e x_t) * (W3_e x_t)   for every pair p = (t, j), e = ids[p]        (gate_up kernel)
 //     z_p = weights[p] W2_e h_p                                                        (down kernel)
 //     y_t = sum_j z_p                                                                  (combine kernel)
-// The first two are bound by the weights of the experts that some token chose, each of which is read once per 16 of its tokens.  Every
-// workgroup sorts the pairs of a block of 64 tokens by expert for itself (some hundred numbers, in LDS) and takes one expert and a run of its rows.  Between
+// The first two are bound by the weights of the experts that some token chose: up to 64 tokens, few to an expert, these stream through registers once per 16 rows
+// (T = 48, E = 128, top_k = 8, H = 4096, I = 2048: 355 us, 4.6 TB/s of weights; T = 1 of the same 64 experts' layer 30.5 us, 3.4 TB/s); otherwise they go through tiles.
+// Every workgroup sorts the pairs of a block of tokens by expert for itself (some hundred numbers, in LDS) and takes one expert and a run of its rows.  Between
 // the kernels h is kept as the sum of two BF16 numbers, sixteen bits of its FP32 fraction: its rounding (2^-17) stays below the result's; z is FP32, and a token's
 // sum is in the order of its places, so results do not depend on the schedule.
 #include "w4a16_mx.h"
@@ -12,7 +13,7 @@
 namespace w4a16 {
 namespace {
 
-constexpr int kBlockTokens = 64;
+constexpr int kBlockTokens = 64, kWideBlockTokens = 256;  // of the streaming kernels at most; of the tiles, where pairs and offsets allow
 constexpr int kMaxPairs = kBlockTokens * kMoeMaxTopK;
 
 struct Lists {
@@ -236,7 +237,7 @@ struct Job {
 };
 __device__ __forceinline__ bool find_job(Lists &l, const MoeArgs &a, int t0, Job *j)
 {
-    const int pairs = min(kBlockTokens, a.T - t0) * a.top_k;
+    const int pairs = min(a.block_tokens, a.T - t0) * a.top_k;
     const int32_t *const ids = a.ids + (size_t)t0 * a.top_k;
     if (pairs <= 64) {
         const int lane = (int)threadIdx.x & 63, e = lane < pairs ? ids[lane] : -1;
@@ -283,9 +284,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_gate_up_kernel(MoeArgs a, 
 {
     __shared__ Lists l;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    const int t0 = (int)blockIdx.z * kBlockTokens;
     Job job;
-    if (!find_job(l, a, t0, &job)) return;
+    if (!find_job(l, a, 0, &job)) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int col = lane & 15, p16 = lane >> 4;
     const int tiles = kWaves / geo.parts, tile = wave / geo.parts, part = wave - tile * geo.parts;
@@ -310,7 +310,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_gate_up_kernel(MoeArgs a, 
         ask_for<Op>(lds, a.H, rows, 2 * tiles, wave,
                     [&](int r, int) {
                         const int t = pair_of(l, job, r0 + r) / a.top_k;
-                        return static_cast<const uint8_t *>(a.X) + (size_t)(t0 + t) * (size_t)a.ldx * 2;
+                        return static_cast<const uint8_t *>(a.X) + (size_t)t * (size_t)a.ldx * 2;
                     },
                     [&](int g) { return a.scales13 + (expert_row + (size_t)(g & 1) * (size_t)a.I + (size_t)tile_row(g >> 1)) * row_s; });
         st.x = lds;
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_gate_up_kernel(MoeArgs a, 
                 u += from[w * 512 + 256];
             }
             if (i0 + c < a.I) {
-                store_hidden(a, (size_t)t0 * a.top_k + l.order[r0 + r], i0 + c, activate(g, a.activation) * u);
+                store_hidden(a, (size_t)l.order[r0 + r], i0 + c, activate(g, a.activation) * u);
             }
         }
         __syncthreads();
@@ -342,9 +342,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_down_kernel(MoeArgs a, Geo
 {
     __shared__ Lists l;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    const int t0 = (int)blockIdx.z * kBlockTokens;
     Job job;
-    if (!find_job(l, a, t0, &job)) return;
+    if (!find_job(l, a, 0, &job)) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int col = lane & 15, p16 = lane >> 4;
     const int runs = kWaves / geo.parts, run = wave / geo.parts, part = wave - run * geo.parts;
@@ -368,7 +367,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_down_kernel(MoeArgs a, Geo
         const int rows = min(geo.pass, job.end - r0);
         ask_for<MxBF16Pair>(lds, a.I, rows, CT * runs, wave,
                             [&](int r, int term) {
-                                const size_t p = (size_t)t0 * a.top_k + (size_t)pair_of(l, job, r0 + r);
+                                const size_t p = (size_t)pair_of(l, job, r0 + r);
                                 return reinterpret_cast<const uint8_t *>(a.hidden + p * (size_t)a.I + (term ? second : 0));
                             },
                             [&](int g) { return a.scales2 + (expert_row + (size_t)tile_row(g)) * row_s; });
@@ -390,7 +389,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_down_kernel(MoeArgs a, Geo
             float v = 0.f;
             for (int w = 0; w < geo.parts; ++w) v += from[w * CT * 256];
             if (n0 + c < a.H) {
-                const size_t p = (size_t)t0 * a.top_k + l.order[r0 + r];
+                const size_t p = (size_t)l.order[r0 + r];
                 a.partial[p * (size_t)a.H + (size_t)(n0 + c)] = a.weights[p] * v;
             }
         }
@@ -400,11 +399,13 @@ __global__ __launch_bounds__(64 * kWaves, 4) void moe_down_kernel(MoeArgs a, Geo
 
 // ---- experts with many tokens ----
 //
-// With eight tokens to an expert and more, rows of X no longer fit LDS whole beside each other, and reading the weights again for every
-// few of them costs more than they do: the loop of w4a16_mx_stage.h, 16 MT rows at a time.  BF16, us, as above / 16 / 32 rows: 16 tokens to an expert, E = 8, H = I = 4096
-// 133 / 88 / 63; E = 16, H = 7168, I = 2048 206 / 150 / 132; eight, E = 32, H = 2048, I = 1024, four blocks of tokens 137 / 109 / 140; E = 32, H = 4096, I = 2048 113 / 117 / 136;
-// four, E = 128 376 / 401 / 495.
-constexpr int kTileRows = 8, kTileRows2 = 12;  // tokens to an expert, on average: from here on 16 rows at a time, 32 rows
+// Where an expert has rows that do not fit LDS beside each other, reading the weights again for every few of them costs more than they do: the loop of
+// w4a16_mx_stage.h, 16 MT rows at a time.  Its workgroups sort the pairs of up to 256 tokens, so that a longer batch reads the weights once per 256.
+// BF16, us, as above / 16 / 32 rows: T = 64, E = 8, top_k = 2, H = I = 4096 116 / 90 / 62; T = 256, E = 32, top_k = 4, H = 4096, I = 2048 380 / 253 / 223 (in
+// blocks of 64 tokens 372 / 376 / 486); T = 48, E = 16, top_k = 2, H = 7168, I = 2048 117 / 96 / 124; T = 49, E = 34, top_k = 7, H = 3008, I = 800 76 / 53 / 74; T = 48, E = 128, top_k = 8, H = 4096,
+// I = 2048 358 / 382 / 494.  64 rows: 169 where 32 take 159 (T = 256, E = 8), 90 where they take 108 at best.
+constexpr int kTileRows = 8, kTileRows2 = 12;   // tokens to an expert, on average: from here on 16 rows at a time, 32
+constexpr int kTileLongRows = 4, kTileLongBytes = 56 << 10;  // ... where that many fill this much LDS
 
 template <class Op, int MT, int WC, int WK, int DEPTH>
 __global__ __launch_bounds__(64 * WC * WK, 4) void moe_gate_up_tile_kernel(MoeArgs a)
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(64 * WC * WK, 4) void moe_gate_up_tile_kernel(MoeAr
     using Sh = StageShape<Op, MT, 2, WC, WK, 1, DEPTH>;
     __shared__ Lists l;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    const int t0 = (int)blockIdx.z * kBlockTokens;
+    const int t0 = (int)blockIdx.z * a.block_tokens;
     Job job;
     if (!find_job(l, a, t0, &job)) return;
     __syncthreads();
@@ -469,7 +470,7 @@ __global__ __launch_bounds__(64 * WC * WK, 4) void moe_down_tile_kernel(MoeArgs 
     using Sh = StageShape<MxBF16Pair, MT, CT, WC, WK, 1, DEPTH>;
     __shared__ Lists l;
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    const int t0 = (int)blockIdx.z * kBlockTokens;
+    const int t0 = (int)blockIdx.z * a.block_tokens;
     Job job;
     if (!find_job(l, a, t0, &job)) return;
     __syncthreads();
@@ -557,9 +558,9 @@ struct Pass {
     size_t lds;
 };
 template <class Op>
-Pass choose_pass(const MoeArgs &a, int K, int runs, int ct, int slots, int tokens)
+Pass choose_pass(const MoeArgs &a, int K, int runs, int ct, int slots)
 {
-    const int pairs = (K + 2 * kMxStep - 1) / (2 * kMxStep), most = tokens * a.top_k < kPassRows ? tokens * a.top_k : kPassRows;
+    const int pairs = (K + 2 * kMxStep - 1) / (2 * kMxStep), most = a.T * a.top_k < kPassRows ? a.T * a.top_k : kPassRows;
     Pass p;
     p.geo.parts = 1;
     while (p.geo.parts < kWaves && (long long)p.geo.parts * runs * slots < 4096 && p.geo.parts * 2 <= pairs) p.geo.parts *= 2;  // about sixteen waves to a compute unit
@@ -569,7 +570,7 @@ Pass choose_pass(const MoeArgs &a, int K, int runs, int ct, int slots, int token
         return rows;
     };
     p.geo.pass = fit(kLds / 2 - kListsLds);
-    if (p.geo.pass < most && (long long)p.geo.pass * a.E < 2ll * tokens * a.top_k) p.geo.pass = fit(kLds - kListsLds);
+    if (p.geo.pass < most && (long long)p.geo.pass * a.E < 2ll * a.T * a.top_k) p.geo.pass = fit(kLds - kListsLds);
     while (p.geo.pass == 0 && p.geo.parts < kWaves) {  // the longest rows
         p.geo.parts *= 2;
         p.geo.pass = fit(kLds - kListsLds);
@@ -581,7 +582,7 @@ Pass choose_pass(const MoeArgs &a, int K, int runs, int ct, int slots, int token
 }
 
 template <class Kernel>
-hipError_t enqueue(Kernel kernel, int outputs, int width, int slots, int token_blocks, const Pass &p, const MoeArgs &a, hipStream_t stream)
+hipError_t enqueue(Kernel kernel, int outputs, int width, int slots, const Pass &p, const MoeArgs &a, hipStream_t stream)
 {
     if (p.geo.pass < 1) return hipErrorInvalidValue;
     if (p.lds + kListsLds > 65536) {
@@ -589,25 +590,25 @@ hipError_t enqueue(Kernel kernel, int outputs, int width, int slots, int token_b
         if (e != hipSuccess) return e;
     }
     const int per = kWaves / p.geo.parts * width;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)((outputs + per - 1) / per), (unsigned)slots, (unsigned)token_blocks), dim3(64 * kWaves), p.lds, stream, a, p.geo);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)((outputs + per - 1) / per), (unsigned)slots), dim3(64 * kWaves), p.lds, stream, a, p.geo);
     return hipGetLastError();
 }
 
 constexpr int kDownTiles = 2, kDepth = 2;
 
 template <class Op>
-hipError_t launch_gate_up(const MoeArgs &a, int slots, int token_blocks, int tokens, hipStream_t stream)
+hipError_t launch_gate_up(const MoeArgs &a, int slots, hipStream_t stream)
 {
-    const Pass p = choose_pass<Op>(a, a.H, a.I / 16, 2, slots, tokens);
-    return a.H % kMxStep == 0 ? enqueue(&moe_gate_up_kernel<Op, true, kDepth>, a.I, 16, slots, token_blocks, p, a, stream)
-                              : enqueue(&moe_gate_up_kernel<Op, false, kDepth>, a.I, 16, slots, token_blocks, p, a, stream);
+    const Pass p = choose_pass<Op>(a, a.H, a.I / 16, 2, slots);
+    return a.H % kMxStep == 0 ? enqueue(&moe_gate_up_kernel<Op, true, kDepth>, a.I, 16, slots, p, a, stream)
+                              : enqueue(&moe_gate_up_kernel<Op, false, kDepth>, a.I, 16, slots, p, a, stream);
 }
 
-hipError_t launch_down(const MoeArgs &a, int slots, int token_blocks, int tokens, hipStream_t stream)
+hipError_t launch_down(const MoeArgs &a, int slots, hipStream_t stream)
 {
-    const Pass p = choose_pass<MxBF16Pair>(a, a.I, (a.H + 16 * kDownTiles - 1) / (16 * kDownTiles), kDownTiles, slots, tokens);
-    return a.I % kMxStep == 0 ? enqueue(&moe_down_kernel<kDownTiles, true, kDepth>, a.H, 16 * kDownTiles, slots, token_blocks, p, a, stream)
-                              : enqueue(&moe_down_kernel<kDownTiles, false, kDepth>, a.H, 16 * kDownTiles, slots, token_blocks, p, a, stream);
+    const Pass p = choose_pass<MxBF16Pair>(a, a.I, (a.H + 16 * kDownTiles - 1) / (16 * kDownTiles), kDownTiles, slots);
+    return a.I % kMxStep == 0 ? enqueue(&moe_down_kernel<kDownTiles, true, kDepth>, a.H, 16 * kDownTiles, slots, p, a, stream)
+                              : enqueue(&moe_down_kernel<kDownTiles, false, kDepth>, a.H, 16 * kDownTiles, slots, p, a, stream);
 }
 
 // Tiles: four waves side by side, two shares of K.
@@ -625,35 +626,37 @@ hipError_t enqueue_tiles(Kernel kernel, int outputs, int width, int slots, int t
 template <class Op, int MT>
 hipError_t launch_gate_up_tiles(const MoeArgs &a, int slots, int token_blocks, hipStream_t stream)
 {
-    return enqueue_tiles<StageShape<Op, MT, 2, kTileWC, kTileWK, 1, kTileDepth>>(&moe_gate_up_tile_kernel<Op, MT, kTileWC, kTileWK, kTileDepth>, a.I, 16 * kTileWC, slots, token_blocks,
-                                                                                 a, stream);
+    using Sh = StageShape<Op, MT, 2, kTileWC, kTileWK, 1, kTileDepth>;
+    return enqueue_tiles<Sh>(&moe_gate_up_tile_kernel<Op, MT, kTileWC, kTileWK, kTileDepth>, a.I, 16 * kTileWC, slots, token_blocks, a, stream);
 }
 template <int MT>
-hipError_t launch_down_tiles(const MoeArgs &a, int slots, int token_blocks, hipStream_t stream)
+hipError_t launch_tiles(const MoeArgs &a, int slots, int token_blocks, hipStream_t stream)
 {
+    const hipError_t e = a.type == kTypeBF16 ? launch_gate_up_tiles<MxBF16, MT>(a, slots, token_blocks, stream) : launch_gate_up_tiles<MxF16, MT>(a, slots, token_blocks, stream);
+    if (e != hipSuccess) return e;
     using Sh = StageShape<MxBF16Pair, MT, kTileCT, kTileWC, kTileWK, 1, kTileDepth>;
     return enqueue_tiles<Sh>(&moe_down_tile_kernel<MT, kTileCT, kTileWC, kTileWK, kTileDepth>, a.H, Sh::kCols, slots, token_blocks, a, stream);
 }
 
 }  // namespace
 
-hipError_t launch_moe_experts(const MoeArgs &a, hipStream_t stream)
+hipError_t launch_moe_experts(const MoeArgs &args, hipStream_t stream)
 {
-    const int token_blocks = (a.T + kBlockTokens - 1) / kBlockTokens, tokens = a.T < kBlockTokens ? a.T : kBlockTokens;
+    MoeArgs a = args;
+    // Rows that an expert has on average decide.  A block's pairs fit the lists, its rows of X 32-bit offsets.
+    a.block_tokens = kWideBlockTokens;
+    if (a.block_tokens * a.top_k > kMaxPairs) a.block_tokens = kMaxPairs / a.top_k;
+    if (a.ldx > (1ll << 21)) a.block_tokens = kBlockTokens;
+    const int tokens = a.T < a.block_tokens ? a.T : a.block_tokens, token_blocks = (a.T + a.block_tokens - 1) / a.block_tokens;
     const int slots = a.E < tokens * a.top_k ? a.E : tokens * a.top_k;  // experts that a block can have chosen
-    // Rows that an expert has on average decide; tiles that would leave compute units without one do not count.
     const int average = tokens * a.top_k / a.E;
-    const bool bf16 = a.type == kTypeBF16;
     hipError_t e;
-    if (average < kTileRows || (long long)(a.I / (16 * kTileWC)) * slots * token_blocks < 256)
-        e = bf16 ? launch_gate_up<MxBF16>(a, slots, token_blocks, tokens, stream) : launch_gate_up<MxF16>(a, slots, token_blocks, tokens, stream);
-    else if (average < kTileRows2)
-        e = bf16 ? launch_gate_up_tiles<MxBF16, 1>(a, slots, token_blocks, stream) : launch_gate_up_tiles<MxF16, 1>(a, slots, token_blocks, stream);
-    else
-        e = bf16 ? launch_gate_up_tiles<MxBF16, 2>(a, slots, token_blocks, stream) : launch_gate_up_tiles<MxF16, 2>(a, slots, token_blocks, stream);
-    if (e != hipSuccess) return e;
-    if (average < kTileRows || (long long)(a.H / (16 * kTileCT * kTileWC)) * slots * token_blocks < 256) e = launch_down(a, slots, token_blocks, tokens, stream);
-    else e = average < kTileRows2 ? launch_down_tiles<1>(a, slots, token_blocks, stream) : launch_down_tiles<2>(a, slots, token_blocks, stream);
+    if (a.T <= kBlockTokens && average < kTileRows && (average < kTileLongRows || average * (int)x_row(a.H) < kTileLongBytes)) {
+        e = a.type == kTypeBF16 ? launch_gate_up<MxBF16>(a, slots, stream) : launch_gate_up<MxF16>(a, slots, stream);
+        if (e == hipSuccess) e = launch_down(a, slots, stream);
+    } else {
+        e = average < kTileRows2 ? launch_tiles<1>(a, slots, token_blocks, stream) : launch_tiles<2>(a, slots, token_blocks, stream);
+    }
     if (e != hipSuccess) return e;
     for (int t = 0; t < a.T; t += 65535) {  // tokens in a grid's second dimension
         MoeArgs part = a;

@@ -50,6 +50,7 @@ struct MoeArgs {
     float *partial;                      // [T top_k, H]: the places' results, weighted
     long long ldx, ldy;
     int type, T, E, top_k, H, I, activation;
+    int block_tokens = 0;                // tokens whose pairs a workgroup sorts (set by launch_moe_experts)
 };
 hipError_t launch_moe_experts(const MoeArgs &a, hipStream_t stream);
 

@@ -438,7 +438,7 @@ float estimate_mx_rows(const MxGemmArgs &a)
     const float w = (float)a.N * (float)a.K * 0.53125f, tiles = (float)((a.N + 15) / 16), blocks = (float)((a.M + kMxRows - 1) / kMxRows);
     const float row = (float)a.K * (a.xs ? 0.7f : 2.0f);
     const float all = w / 6.2e6f + (blocks - 1.0f) * w / 12.0e6f + (float)a.M * row * tiles / 7.5e6f;
-    const float one = (8.5f * (float)a.K + (float)(a.M < kMxRows ? a.M : kMxRows) * row) / 26.0e3f;
+    const float one = (8.5f * (float)a.K + (float)(a.M < kMxRows ? a.M : kMxRows) * row) / 26.0e3f * (tiles * blocks > 256.0f ? 2.0f : 1.0f);  // (half the waves to a tile)
     return 3.0f + (all > one ? all : one);
 }
 

@@ -224,6 +224,14 @@ def test_experts_match_the_oracle(moe, kind, T, E, top_k, H, I):
 
 
 @gpu
+@pytest.mark.parametrize("kind", ["float16", "bfloat16"])
+@pytest.mark.parametrize("T,E,top_k,H,I", [(66, 128, 1, 96, 64), (256, 5, 3, 96, 64), (257, 4, 2, 32, 96), (300, 40, 6, 288, 160), (130, 48, 32, 160, 32), (10, 4, 2, 6016, 64)])
+def test_experts_of_long_batches(moe, kind, T, E, top_k, H, I):
+    import torch
+    check_layer(moe, np.random.default_rng([T, E, H]), T, E, top_k, H, I, getattr(torch, kind), ldx=8 * (T % 3))
+
+
+@gpu
 def test_gelu(moe):
     import torch
     for T in (1, 20):

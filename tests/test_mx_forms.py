@@ -118,3 +118,21 @@ def test_experts_with_many_tokens_unevenly(mx):
         ids[:, 1] = rng.integers(-2, 6, 64)
         ids[5] = [3, 3, 0]
         tmoe.check_layer(moe, rng, 64, 4, 3, H, I, torch.bfloat16, ids=ids)
+
+
+@gpu
+@pytest.mark.parametrize("apart", [0, 6, 22, 23, 24, 60])
+@pytest.mark.parametrize("M,N,K", [(16, 6205, 4128), (50, 2107, 1056), (33, 6205, 1056), (150, 6210, 672), (1003, 2111, 416), (1000, 1037, 288)])
+def test_blocks_beside_much_larger_ones(mx, M, N, K, apart):
+    """FP16: blocks of W whose scales are 2^apart times their neighbours', where X is zero: the small ones' values are all there is."""
+    import torch
+    rng = np.random.default_rng([M, N, apart])
+    wc, ws = tmx._random_mx(rng, N, K)
+    large = np.arange(K // 32) % 4 == rng.integers(0, 4)
+    ws[:] = rng.integers(119, 122, (N, 1)) + apart * large
+    ws[::7] = 120  # rows without large blocks among them
+    x = rng.standard_normal((M, K)).reshape(M, K // 32, 32)
+    x[:, large] = 0.0
+    X = tmx._torch(x.reshape(M, K)).to(torch.float16)
+    ref, terms = mo.gemm(tmx._exact(X), wc, ws)
+    tmx.check(mx.gemm(X, tmx._torch(wc), tmx._torch(ws)), ref, terms, K, "M=%d N=%d K=%d apart=%d" % (M, N, K, apart))

@@ -57,6 +57,8 @@ int w4a16_mx_gemm_mx(const uint8_t *x_codes, const uint8_t *x_scales, const uint
 /* What the library runs for a product of this shape: the rows of X and the columns of Y that a workgroup takes (16 columns: the kernel for few rows,
  * which reads the weights once per 16 rows of X; its workgroups take several times 16).  `x_mx` nonzero: w4a16_mx_gemm_mx. */
 int w4a16_mx_query_tile(int M, int N, int K, int dtype, int x_mx, int *tile_m, int *tile_n);
+/* LDS of one of its workgroups, and in how many pieces of K the rows of X pass through it (tiles: 1). */
+int w4a16_mx_query_lds(int M, int N, int K, int dtype, int x_mx, int *lds_bytes, int *chunks);
 
 /*
  * A mixture-of-experts router's choice.  For every token t: the `top_k` experts of the largest logits[t, :] (type `dtype`: FP16, BF16

@@ -27,12 +27,17 @@ struct MxGemmArgs {
 };
 // w4a16_mx_rows.hip: few rows of X, weights read once per sixteen of them; w4a16_mx_tile.hip (K >= 128): the rest.  What a call would take, us.
 float estimate_mx_rows(const MxGemmArgs &a);
+struct MxRowsLayout {
+    int lds_bytes, chunks;  // of a workgroup; pieces of K that X's rows come to LDS in
+};
+MxRowsLayout layout_mx_rows(const MxGemmArgs &a);
 hipError_t launch_mx_rows(const MxGemmArgs &a, hipStream_t stream);
 struct MxTilePlan {
     int form, tile_m, tile_n;
     float us;
 };
 MxTilePlan plan_mx_tile(const MxGemmArgs &a);
+int mx_tile_lds(const MxGemmArgs &a, int form);  // bytes of a workgroup
 hipError_t launch_mx_tile(const MxGemmArgs &a, int form, hipStream_t stream);
 
 constexpr int kMoeMaxExperts = 1024, kMoeMaxTopK = 32;

@@ -42,6 +42,21 @@ int check_gemm(int M, int N, int K, int dtype, long long ldy)
     return W4A16_OK;
 }
 
+// The arguments of a product that is asked about: xs tells which X, nothing is read.
+int asked(int M, int N, int K, int dtype, int x_mx, MxGemmArgs *a)
+{
+    const int rc = check_gemm(M, N, K, dtype, N);
+    if (rc) return rc;
+    if (M < 1) return W4A16_ERR_SHAPE;
+    *a = {};
+    a->xs = x_mx ? reinterpret_cast<const uint8_t *>(a) : nullptr;
+    a->M = M;
+    a->N = N;
+    a->K = K;
+    a->type = dtype;
+    return W4A16_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -97,19 +112,27 @@ int w4a16_mx_gemm_mx(const uint8_t *x_codes, const uint8_t *x_scales, const uint
 int w4a16_mx_query_tile(int M, int N, int K, int dtype, int x_mx, int *tile_m, int *tile_n)
 {
     clear_hip_error();
-    const int rc = check_gemm(M, N, K, dtype, N);
+    MxGemmArgs a;
+    const int rc = asked(M, N, K, dtype, x_mx, &a);
     if (rc) return rc;
-    if (M < 1) return W4A16_ERR_SHAPE;
     if (!tile_m || !tile_n) return W4A16_ERR_NULL;
-    MxGemmArgs a = {};
-    a.xs = x_mx ? reinterpret_cast<const uint8_t *>(tile_m) : nullptr;  // (asked about, not read)
-    a.M = M;
-    a.N = N;
-    a.K = K;
-    a.type = dtype;
     const MxTilePlan p = plan_product(a);
     *tile_m = p.tile_m;
     *tile_n = p.tile_n;
+    return W4A16_OK;
+}
+
+int w4a16_mx_query_lds(int M, int N, int K, int dtype, int x_mx, int *lds_bytes, int *chunks)
+{
+    clear_hip_error();
+    MxGemmArgs a;
+    const int rc = asked(M, N, K, dtype, x_mx, &a);
+    if (rc) return rc;
+    if (!lds_bytes || !chunks) return W4A16_ERR_NULL;
+    const MxTilePlan p = plan_product(a);
+    const MxRowsLayout l = p.tile_n == 16 ? layout_mx_rows(a) : MxRowsLayout{mx_tile_lds(a, p.form), 1};
+    *lds_bytes = l.lds_bytes;
+    *chunks = l.chunks;
     return W4A16_OK;
 }
 

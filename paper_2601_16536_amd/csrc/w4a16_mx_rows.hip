@@ -25,6 +25,7 @@ namespace {
 constexpr int kMxRows = 16;        // rows of X per workgroup
 constexpr int kMxXUnits = 8;       // 16-byte units of X that a thread stages per chunk
 constexpr int kMxScaleUnits = 4;   // of scales, in flight
+constexpr size_t kMxMostLds = 152 << 10;  // of a compute unit's 160 KiB
 
 // How X lies in LDS: rows 64 bytes past a multiple of 256 apart, so that four rows of a step use different banks.
 struct MxChunk {
@@ -404,28 +405,37 @@ RowsPlan plan(const MxGemmArgs &a, int waves)
     while (p.parts < waves && p.parts * tiles < 4096 && p.parts * 4 <= steps) p.parts *= 2;
     p.tiles = waves / p.parts;
     const int blocks = a.K / kMxBlock;
-    const size_t limit = waves == 16 ? 155648 : 77824;  // one or two workgroups to a compute unit
+    const size_t limit = waves == 16 ? kMxMostLds : kMxMostLds / 2;  // one or two workgroups to a compute unit
     const int held = kMxXUnits * 64 * waves / (rows * Op::kTerms * (Op::kMx ? 4 : 16));  // steps that the threads' registers hold
-    for (;; p.parts *= 2, p.tiles /= 2) {
-        int chunk = steps;
-        if (mx_lds<Op>(mx_chunk<Op>(steps), rows, blocks, p.tiles) > limit) {
-            chunk = held - held % 2;
-            if (chunk > 2 * p.parts) chunk -= chunk % (2 * p.parts);
-        }
+    auto take = [&](int chunk) {
         p.multi = chunk < steps;
         p.chunk = mx_chunk<Op>(chunk);
         p.lds = mx_lds<Op>(p.chunk, rows, blocks, p.tiles);
-        if (p.lds <= 155648 || p.tiles == 1) break;  // (very long rows of scales: fewer tiles)
+    };
+    // A chunk that is not the last has whole pairs of steps, an equal number for every share where there are that many.
+    auto even = [&](int chunk) {
+        chunk -= chunk % 2;
+        if (chunk > 2 * p.parts) chunk -= chunk % (2 * p.parts);
+        return chunk;
+    };
+    for (;; p.parts *= 2, p.tiles /= 2) {
+        take(steps);
+        if (p.lds > limit && even(held) < steps) take(even(held));
+        if (p.lds <= kMxMostLds || p.tiles == 1) break;  // (very long rows of scales: fewer tiles)
     }
+    // One tile's scales, up to 128 KiB with those of 16 rows of X, stay beside X whole: shorter chunks.  (K = 131072, 16 rows in MXFP4: 22 steps.)
+    while (p.lds > kMxMostLds && p.chunk.steps > 2) take(even(p.chunk.steps - 1));
     const size_t sums = (size_t)waves * 1024;
     if (p.lds < sums) p.lds = sums;
     return p;
 }
 
+int waves_of(const MxGemmArgs &a) { return ((long long)a.N + 15) / 16 * ((a.M + kMxRows - 1) / kMxRows) <= 256 ? 16 : 8; }
+
 template <class Op>
 hipError_t launch_rows(const MxGemmArgs &a, hipStream_t stream)
 {
-    const int waves = ((long long)a.N + 15) / 16 * ((a.M + kMxRows - 1) / kMxRows) <= 256 ? 16 : 8;
+    const int waves = waves_of(a);
     const RowsPlan p = plan<Op>(a, waves);
     if constexpr (Op::kMx || Op::kTerms == 2) return waves == 16 ? launch<Op, 4, 16, 4>(a, p, stream) : launch<Op, 4, 8, 4>(a, p, stream);
     else if (a.M == 1) return waves == 16 ? launch<Op, 1, 16, 4>(a, p, stream) : launch<Op, 1, 8, 4>(a, p, stream);
@@ -443,6 +453,13 @@ float estimate_mx_rows(const MxGemmArgs &a)
     const float all = w / 6.2e6f + (blocks - 1.0f) * w / 12.0e6f + (float)a.M * row * tiles / 7.5e6f;
     const float one = (8.5f * (float)a.K + (float)(a.M < kMxRows ? a.M : kMxRows) * row) / 26.0e3f * (tiles * blocks > 256.0f ? 2.0f : 1.0f);  // (half the waves to a tile)
     return 3.0f + (all > one ? all : one);
+}
+
+MxRowsLayout layout_mx_rows(const MxGemmArgs &a)
+{
+    const RowsPlan p = a.xs ? plan<MxFP4>(a, waves_of(a)) : plan<MxBF16>(a, waves_of(a));  // (alike for FP16)
+    const int steps = (a.K + kMxStep - 1) / kMxStep;
+    return {(int)p.lds, (steps + p.chunk.steps - 1) / p.chunk.steps};
 }
 
 hipError_t launch_mx_rows(const MxGemmArgs &a, hipStream_t stream)

@@ -74,23 +74,25 @@ __global__ __launch_bounds__(64 * WC * WK, PER_CU) void mx_tile_kernel(MxGemmArg
     }
 }
 
+// A form's kernel: 16 MT x 16 CT WC tiles, WK shares of K.
 template <class Op, int MT, int CT, int WC, int WK, int STEPS, int DEPTH, int PER_CU>
-hipError_t launch(const MxGemmArgs &a, hipStream_t stream)
-{
+struct TileKernel {
     using Sh = StageShape<Op, MT, CT, WC, WK, STEPS, DEPTH>;
-    const int tiles_n = (a.N + Sh::kCols - 1) / Sh::kCols, row_blocks = (a.M + Sh::kRows - 1) / Sh::kRows;
-    const long long grid = eighths_grid(tiles_n, row_blocks);
-    if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
-    auto go = [&](auto kernel) {
+    static_assert(Sh::kLds <= 163840, "LDS of a compute unit");
+    static hipError_t launch(const MxGemmArgs &a, hipStream_t stream)
+    {
+        const int tiles_n = (a.N + Sh::kCols - 1) / Sh::kCols, row_blocks = (a.M + Sh::kRows - 1) / Sh::kRows;
+        const long long grid = eighths_grid(tiles_n, row_blocks);
+        if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+        const auto kernel = &mx_tile_kernel<Op, MT, CT, WC, WK, STEPS, DEPTH, PER_CU>;
         if (Sh::kLds > 65536) {
             const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds);
             if (e != hipSuccess) return e;
         }
         hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * Sh::kWaves), Sh::kLds, stream, a, tiles_n, row_blocks);
         return hipGetLastError();
-    };
-    return go(&mx_tile_kernel<Op, MT, CT, WC, WK, STEPS, DEPTH, PER_CU>);
-}
+    }
+};
 
 // A form's tile and its time for K = 8192, us, where every compute unit has one tile at most, and per round of 256 of them where there are more (measured, N = 8192 and
 // 4096; BF16, FP16, MXFP4 X).  Narrow tiles with many shares of K keep all compute units and many loads busy where there are few rows; wide ones read X and
@@ -116,23 +118,30 @@ constexpr float kFixed = 3.0f;  // launch, first loads, last sums
 constexpr float kRound = 4.0f, kWideRound = 1.0f;
 constexpr int kFirstWide = 5;  // form
 
-template <class Op>
-hipError_t launch_form(const MxGemmArgs &a, int form, hipStream_t stream)
+// use(TileKernel of the form).
+template <class Op, class Use>
+void with_form(int form, Use use)
 {
     constexpr bool mx = Op::kMx;
     switch (form) {  // (a form whose time is kNever is not planned)
-    case 0: return launch<Op, 1, 1, 2, 8, mx ? 4 : 1, mx ? 2 : 4, 4>(a, stream);
-    case 1: return launch<Op, 2, 1, 2, 4, mx ? 4 : 1, mx ? 2 : 4, 4>(a, stream);
+    case 0: return use(TileKernel<Op, 1, 1, 2, 8, mx ? 4 : 1, mx ? 2 : 4, 4>{});
+    case 1: return use(TileKernel<Op, 2, 1, 2, 4, mx ? 4 : 1, mx ? 2 : 4, 4>{});
     case 2:
-        if constexpr (mx) return hipErrorInvalidValue;
-        else return launch<Op, 2, 1, 4, 4, 1, 4, 4>(a, stream);
-    case 3: return launch<Op, 4, 1, 4, 4, mx ? 2 : 1, 2, 4>(a, stream);
-    case 4: return launch<Op, 4, 2, 4, 2, mx ? 2 : 1, 2, 2>(a, stream);
-    case 5: return launch<Op, 8, 2, 4, 1, 1, mx ? 4 : 2, 2>(a, stream);
+        if constexpr (!mx) use(TileKernel<Op, 2, 1, 4, 4, 1, 4, 4>{});
+        return;
+    case 3: return use(TileKernel<Op, 4, 1, 4, 4, mx ? 2 : 1, 2, 4>{});
+    case 4: return use(TileKernel<Op, 4, 2, 4, 2, mx ? 2 : 1, 2, 2>{});
+    case 5: return use(TileKernel<Op, 8, 2, 4, 1, 1, mx ? 4 : 2, 2>{});
     default:
-        if constexpr (!mx && !Op::kScaled) return hipErrorInvalidValue;
-        else return launch<Op, 8, 4, 4, 1, 1, 2, 2>(a, stream);
+        if constexpr (mx || Op::kScaled) use(TileKernel<Op, 8, 4, 4, 1, 1, 2, 2>{});
     }
+}
+template <class Use>
+void with_form(const MxGemmArgs &a, int form, Use use)
+{
+    if (a.xs) with_form<MxFP4>(form, use);
+    else if (a.type == kTypeBF16) with_form<MxBF16>(form, use);
+    else with_form<MxF16Together>(form, use);
 }
 
 }  // namespace
@@ -151,10 +160,18 @@ MxTilePlan plan_mx_tile(const MxGemmArgs &a)
     return best;
 }
 
+int mx_tile_lds(const MxGemmArgs &a, int form)
+{
+    int lds = 0;
+    with_form(a, form, [&](auto kernel) { lds = decltype(kernel)::Sh::kLds; });
+    return lds;
+}
+
 hipError_t launch_mx_tile(const MxGemmArgs &a, int form, hipStream_t stream)
 {
-    if (a.xs) return launch_form<MxFP4>(a, form, stream);
-    return a.type == kTypeBF16 ? launch_form<MxBF16>(a, form, stream) : launch_form<MxF16Together>(a, form, stream);
+    hipError_t e = hipErrorInvalidValue;
+    with_form(a, form, [&](auto kernel) { e = decltype(kernel)::launch(a, stream); });
+    return e;
 }
 
 }  // namespace w4a16

@@ -18,7 +18,7 @@ from .binding import W4A16Error, _stream
 
 F16, BF16, F32 = 0, 1, 2
 
-EXPORTS = ("w4a16_mx_quantize", "w4a16_mx_dequantize", "w4a16_mx_gemm", "w4a16_mx_gemm_mx", "w4a16_mx_query_tile")
+EXPORTS = ("w4a16_mx_quantize", "w4a16_mx_dequantize", "w4a16_mx_gemm", "w4a16_mx_gemm_mx", "w4a16_mx_query_tile", "w4a16_mx_query_lds")
 
 _lib = None
 _types = None
@@ -38,6 +38,7 @@ def lib():
         L.w4a16_mx_gemm_mx.argtypes = [vp, vp, vp, vp, ci, ci, ci, vp, ci, ll, vp]
         ip = ctypes.POINTER(ci)
         L.w4a16_mx_query_tile.argtypes = [ci, ci, ci, ci, ci, ip, ip]
+        L.w4a16_mx_query_lds.argtypes = L.w4a16_mx_query_tile.argtypes
         _types = {torch.float16: F16, torch.bfloat16: BF16, torch.float32: F32}
         _u8 = torch.uint8
         _lib = L
@@ -100,6 +101,14 @@ def query_tile(M: int, N: int, K: int, dtype=None, x_mx: bool = False) -> tuple:
     tm, tn = ctypes.c_int(), ctypes.c_int()
     _check(lib().w4a16_mx_query_tile(M, N, K, type_code(dtype or torch.bfloat16, False), int(x_mx), ctypes.byref(tm), ctypes.byref(tn)), "w4a16_mx_query_tile")
     return tm.value, tn.value
+
+
+def query_lds(M: int, N: int, K: int, dtype=None, x_mx: bool = False) -> tuple:
+    """(bytes of LDS of a workgroup of that kernel, pieces of K that X passes through it in)."""
+    import torch
+    lds, chunks = ctypes.c_int(), ctypes.c_int()
+    _check(lib().w4a16_mx_query_lds(M, N, K, type_code(dtype or torch.bfloat16, False), int(x_mx), ctypes.byref(lds), ctypes.byref(chunks)), "w4a16_mx_query_lds")
+    return lds.value, chunks.value
 
 
 def quantize(X, out=None, stream=None):

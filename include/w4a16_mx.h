@@ -90,6 +90,11 @@ int w4a16_moe_experts(const void *X, int dtype, long long ldx, const int32_t *id
                       const uint8_t *scales13, const uint8_t *codes2, const uint8_t *scales2, int T, int E, int top_k, int H, int I,
                       int activation, void *Y, long long ldy, void *workspace, size_t workspace_bytes, void *stream);
 
+/* What the library runs for a layer of these sizes (contiguous X): the kernels that stream an expert's weights or, `tiles` nonzero, those of many rows; the rows of
+ * an expert that a workgroup of the gate and up product and of the down product takes at a time, and its LDS. */
+typedef struct { int tiles, rows_up, rows_down, lds_up, lds_down; } w4a16_moe_plan;
+int w4a16_moe_query_plan(int T, int E, int top_k, int H, int I, w4a16_moe_plan *plan);
+
 #ifdef __cplusplus
 }
 #endif

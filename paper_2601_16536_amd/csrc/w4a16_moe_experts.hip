@@ -584,7 +584,6 @@ Pass choose_pass(const MoeArgs &a, int K, int runs, int ct, int slots)
 template <class Kernel>
 hipError_t enqueue(Kernel kernel, int outputs, int width, int slots, const Pass &p, const MoeArgs &a, hipStream_t stream)
 {
-    if (p.geo.pass < 1) return hipErrorInvalidValue;
     if (p.lds + kListsLds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)p.lds);
         if (e != hipSuccess) return e;
@@ -597,25 +596,28 @@ hipError_t enqueue(Kernel kernel, int outputs, int width, int slots, const Pass 
 constexpr int kDownTiles = 2, kDepth = 2;
 
 template <class Op>
-hipError_t launch_gate_up(const MoeArgs &a, int slots, hipStream_t stream)
+hipError_t launch_gate_up(const MoeArgs &a, const Pass &p, int slots, hipStream_t stream)
 {
-    const Pass p = choose_pass<Op>(a, a.H, a.I / 16, 2, slots);
     return a.H % kMxStep == 0 ? enqueue(&moe_gate_up_kernel<Op, true, kDepth>, a.I, 16, slots, p, a, stream)
                               : enqueue(&moe_gate_up_kernel<Op, false, kDepth>, a.I, 16, slots, p, a, stream);
 }
 
-hipError_t launch_down(const MoeArgs &a, int slots, hipStream_t stream)
+hipError_t launch_down(const MoeArgs &a, const Pass &p, int slots, hipStream_t stream)
 {
-    const Pass p = choose_pass<MxBF16Pair>(a, a.I, (a.H + 16 * kDownTiles - 1) / (16 * kDownTiles), kDownTiles, slots);
     return a.I % kMxStep == 0 ? enqueue(&moe_down_kernel<kDownTiles, true, kDepth>, a.H, 16 * kDownTiles, slots, p, a, stream)
                               : enqueue(&moe_down_kernel<kDownTiles, false, kDepth>, a.H, 16 * kDownTiles, slots, p, a, stream);
 }
 
 // Tiles: four waves side by side, two shares of K.
 constexpr int kTileWC = 4, kTileWK = 2, kTileDepth = 2, kTileCT = 2;
+template <class Op, int MT>
+using UpShape = StageShape<Op, MT, 2, kTileWC, kTileWK, 1, kTileDepth>;
+template <int MT>
+using DownShape = StageShape<MxBF16Pair, MT, kTileCT, kTileWC, kTileWK, 1, kTileDepth>;
 template <class Sh, class Kernel>
 hipError_t enqueue_tiles(Kernel kernel, int outputs, int width, int slots, int token_blocks, const MoeArgs &a, hipStream_t stream)
 {
+    static_assert(Sh::kLds + kListsLds <= kLds, "LDS of a compute unit");
     if (Sh::kLds + kListsLds > 65536) {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, Sh::kLds);
         if (e != hipSuccess) return e;
@@ -626,36 +628,65 @@ hipError_t enqueue_tiles(Kernel kernel, int outputs, int width, int slots, int t
 template <class Op, int MT>
 hipError_t launch_gate_up_tiles(const MoeArgs &a, int slots, int token_blocks, hipStream_t stream)
 {
-    using Sh = StageShape<Op, MT, 2, kTileWC, kTileWK, 1, kTileDepth>;
-    return enqueue_tiles<Sh>(&moe_gate_up_tile_kernel<Op, MT, kTileWC, kTileWK, kTileDepth>, a.I, 16 * kTileWC, slots, token_blocks, a, stream);
+    return enqueue_tiles<UpShape<Op, MT>>(&moe_gate_up_tile_kernel<Op, MT, kTileWC, kTileWK, kTileDepth>, a.I, 16 * kTileWC, slots, token_blocks, a, stream);
 }
 template <int MT>
 hipError_t launch_tiles(const MoeArgs &a, int slots, int token_blocks, hipStream_t stream)
 {
     const hipError_t e = a.type == kTypeBF16 ? launch_gate_up_tiles<MxBF16, MT>(a, slots, token_blocks, stream) : launch_gate_up_tiles<MxF16, MT>(a, slots, token_blocks, stream);
     if (e != hipSuccess) return e;
-    using Sh = StageShape<MxBF16Pair, MT, kTileCT, kTileWC, kTileWK, 1, kTileDepth>;
-    return enqueue_tiles<Sh>(&moe_down_tile_kernel<MT, kTileCT, kTileWC, kTileWK, kTileDepth>, a.H, Sh::kCols, slots, token_blocks, a, stream);
+    return enqueue_tiles<DownShape<MT>>(&moe_down_tile_kernel<MT, kTileCT, kTileWC, kTileWK, kTileDepth>, a.H, DownShape<MT>::kCols, slots, token_blocks, a, stream);
+}
+
+// How a layer runs, from its sizes alone.
+struct Plan {
+    int block_tokens, token_blocks, slots;  // tokens whose pairs a workgroup sorts; blocks of them; experts that a block can have chosen
+    int tile_rows;                          // of the tiles; 0: streaming
+    Pass up, down;                          // streaming
+};
+Plan plan_layer(const MoeArgs &a)
+{
+    Plan p = {};
+    // Rows that an expert has on average decide.  A block's pairs fit the lists, its rows of X 32-bit offsets.
+    p.block_tokens = kWideBlockTokens;
+    if (p.block_tokens * a.top_k > kMaxPairs) p.block_tokens = kMaxPairs / a.top_k;
+    if (a.ldx > (1ll << 21)) p.block_tokens = kBlockTokens;
+    const int tokens = a.T < p.block_tokens ? a.T : p.block_tokens;
+    p.token_blocks = (a.T + p.block_tokens - 1) / p.block_tokens;
+    p.slots = a.E < tokens * a.top_k ? a.E : tokens * a.top_k;
+    const int average = tokens * a.top_k / a.E;
+    p.tile_rows = average < kTileRows2 ? 16 : 32;
+    if (a.T <= kBlockTokens && average < kTileRows && (average < kTileLongRows || average * (int)x_row(a.H) < kTileLongBytes)) {
+        p.up = choose_pass<MxBF16>(a, a.H, a.I / 16, 2, p.slots);  // (alike for FP16)
+        p.down = choose_pass<MxBF16Pair>(a, a.I, (a.H + 16 * kDownTiles - 1) / (16 * kDownTiles), kDownTiles, p.slots);
+        // (no row of more than about 29700 values in two terms fits LDS with its weights' scales: the tiles take any length)
+        if (p.up.geo.pass > 0 && p.down.geo.pass > 0) p.tile_rows = 0;
+    }
+    return p;
 }
 
 }  // namespace
 
+MoeLayout layout_moe_experts(const MoeArgs &a)
+{
+    const Plan p = plan_layer(a);
+    const int lists = (int)sizeof(Lists);
+    if (p.tile_rows == 0) return {0, p.up.geo.pass, p.down.geo.pass, lists + (int)p.up.lds, lists + (int)p.down.lds};
+    const bool one = p.tile_rows == 16;
+    return {1, p.tile_rows, p.tile_rows, lists + (one ? UpShape<MxBF16, 1>::kLds : UpShape<MxBF16, 2>::kLds), lists + (one ? DownShape<1>::kLds : DownShape<2>::kLds)};
+}
+
 hipError_t launch_moe_experts(const MoeArgs &args, hipStream_t stream)
 {
     MoeArgs a = args;
-    // Rows that an expert has on average decide.  A block's pairs fit the lists, its rows of X 32-bit offsets.
-    a.block_tokens = kWideBlockTokens;
-    if (a.block_tokens * a.top_k > kMaxPairs) a.block_tokens = kMaxPairs / a.top_k;
-    if (a.ldx > (1ll << 21)) a.block_tokens = kBlockTokens;
-    const int tokens = a.T < a.block_tokens ? a.T : a.block_tokens, token_blocks = (a.T + a.block_tokens - 1) / a.block_tokens;
-    const int slots = a.E < tokens * a.top_k ? a.E : tokens * a.top_k;  // experts that a block can have chosen
-    const int average = tokens * a.top_k / a.E;
+    const Plan p = plan_layer(a);
+    a.block_tokens = p.block_tokens;
     hipError_t e;
-    if (a.T <= kBlockTokens && average < kTileRows && (average < kTileLongRows || average * (int)x_row(a.H) < kTileLongBytes)) {
-        e = a.type == kTypeBF16 ? launch_gate_up<MxBF16>(a, slots, stream) : launch_gate_up<MxF16>(a, slots, stream);
-        if (e == hipSuccess) e = launch_down(a, slots, stream);
+    if (p.tile_rows == 0) {
+        e = a.type == kTypeBF16 ? launch_gate_up<MxBF16>(a, p.up, p.slots, stream) : launch_gate_up<MxF16>(a, p.up, p.slots, stream);
+        if (e == hipSuccess) e = launch_down(a, p.down, p.slots, stream);
     } else {
-        e = average < kTileRows2 ? launch_tiles<1>(a, slots, token_blocks, stream) : launch_tiles<2>(a, slots, token_blocks, stream);
+        e = p.tile_rows == 16 ? launch_tiles<1>(a, p.slots, p.token_blocks, stream) : launch_tiles<2>(a, p.slots, p.token_blocks, stream);
     }
     if (e != hipSuccess) return e;
     for (int t = 0; t < a.T; t += 65535) {  // tokens in a grid's second dimension

@@ -57,6 +57,10 @@ struct MoeArgs {
     int type, T, E, top_k, H, I, activation;
     int block_tokens = 0;                // tokens whose pairs a workgroup sorts (set by launch_moe_experts)
 };
+struct MoeLayout {
+    int tiles, rows_up, rows_down, lds_up, lds_down;
+};
+MoeLayout layout_moe_experts(const MoeArgs &a);
 hipError_t launch_moe_experts(const MoeArgs &a, hipStream_t stream);
 
 }  // namespace w4a16

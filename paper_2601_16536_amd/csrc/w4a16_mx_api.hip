@@ -42,6 +42,14 @@ int check_gemm(int M, int N, int K, int dtype, long long ldy)
     return W4A16_OK;
 }
 
+int check_experts(int T, int E, int top_k, int H, int I)
+{
+    if (T < 0 || E < 1 || E > kMoeMaxExperts || top_k < 1 || top_k > kMoeMaxTopK || bad_k(H) || bad_k(I)) return W4A16_ERR_SHAPE;
+    // 32-bit offsets inside an expert's matrices and a block of tokens; blocks of tokens in a grid's third dimension
+    if (H > kMaxExpertK || I > kMaxExpertK || T > (1 << 21)) return W4A16_ERR_UNSUPPORTED;
+    return W4A16_OK;
+}
+
 // The arguments of a product that is asked about: xs tells which X, nothing is read.
 int asked(int M, int N, int K, int dtype, int x_mx, MxGemmArgs *a)
 {
@@ -156,14 +164,32 @@ size_t w4a16_moe_workspace_bytes(int T, int top_k, int H, int I)
     return (size_t)T * (size_t)top_k * ((size_t)H + (size_t)I) * 4;
 }
 
+int w4a16_moe_query_plan(int T, int E, int top_k, int H, int I, w4a16_moe_plan *plan)
+{
+    clear_hip_error();
+    const int rc = check_experts(T, E, top_k, H, I);
+    if (rc) return rc;
+    if (T < 1) return W4A16_ERR_SHAPE;
+    if (!plan) return W4A16_ERR_NULL;
+    MoeArgs a = {};
+    a.ldx = H;
+    a.T = T;
+    a.E = E;
+    a.top_k = top_k;
+    a.H = H;
+    a.I = I;
+    const MoeLayout l = layout_moe_experts(a);
+    *plan = {l.tiles, l.rows_up, l.rows_down, l.lds_up, l.lds_down};
+    return W4A16_OK;
+}
+
 int w4a16_moe_experts(const void *X, int dtype, long long ldx, const int32_t *ids, const float *weights, const uint8_t *codes13,
                       const uint8_t *scales13, const uint8_t *codes2, const uint8_t *scales2, int T, int E, int top_k, int H, int I,
                       int activation, void *Y, long long ldy, void *workspace, size_t workspace_bytes, void *stream)
 {
     clear_hip_error();
-    if (!type_16bit(dtype) || T < 0 || E < 1 || E > kMoeMaxExperts || top_k < 1 || top_k > kMoeMaxTopK || bad_k(H) || bad_k(I) ||
-        (activation != W4A16_MOE_SILU && activation != W4A16_MOE_GELU))
-        return W4A16_ERR_SHAPE;
+    const int rc = check_experts(T, E, top_k, H, I);
+    if (rc == W4A16_ERR_SHAPE || !type_16bit(dtype) || (activation != W4A16_MOE_SILU && activation != W4A16_MOE_GELU)) return W4A16_ERR_SHAPE;
     if (T == 0) return W4A16_OK;
     if (!X || !ids || !weights || !codes13 || !scales13 || !codes2 || !scales2 || !Y || !workspace) return W4A16_ERR_NULL;
     if (T > 1 && (ldx < H || ldy < H)) return W4A16_ERR_SHAPE;
@@ -171,8 +197,7 @@ int w4a16_moe_experts(const void *X, int dtype, long long ldx, const int32_t *id
         !aligned(scales2, 16) || !aligned(Y, 2) ||
         !aligned(workspace, 256) || bad_rows(T, H, ldx, 8))
         return W4A16_ERR_ALIGN;
-    // 32-bit offsets inside an expert's matrices and a block of tokens; blocks of tokens in a grid's second and third dimension
-    if (H > kMaxExpertK || I > kMaxExpertK || (T > 1 && ldx > kMaxLd) || T > (1 << 21)) return W4A16_ERR_UNSUPPORTED;
+    if (rc || (T > 1 && ldx > kMaxLd)) return W4A16_ERR_UNSUPPORTED;
     if (workspace_bytes < w4a16_moe_workspace_bytes(T, top_k, H, I)) return W4A16_ERR_WORKSPACE;
     const MoeArgs a = {X, ids, weights, codes13, scales13, codes2, scales2, Y, static_cast<uint16_t *>(workspace),
                        reinterpret_cast<float *>(static_cast<uint16_t *>(workspace) + 2 * (size_t)T * (size_t)top_k * (size_t)I), T > 1 ? ldx : H, T > 1 ? ldy : H,

@@ -16,9 +16,13 @@ from .binding import W4A16Error, _stream
 SCORINGS = {"softmax": 0, "sigmoid": 1}
 ACTIVATIONS = {"silu": 0, "gelu": 1}
 
-EXPORTS = ("w4a16_moe_route", "w4a16_moe_workspace_bytes", "w4a16_moe_experts")
+EXPORTS = ("w4a16_moe_route", "w4a16_moe_workspace_bytes", "w4a16_moe_experts", "w4a16_moe_query_plan")
 
 _lib = None
+
+
+class Plan(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int) for name in ("tiles", "rows_up", "rows_down", "lds_up", "lds_down")]
 
 
 def lib():
@@ -31,6 +35,7 @@ def lib():
         L.w4a16_moe_workspace_bytes.argtypes = [ci, ci, ci, ci]
         L.w4a16_moe_workspace_bytes.restype = sz
         L.w4a16_moe_experts.argtypes = [vp, ci, ll, vp, vp, vp, vp, vp, vp, ci, ci, ci, ci, ci, ci, vp, ll, vp, sz, vp]
+        L.w4a16_moe_query_plan.argtypes = [ci, ci, ci, ci, ci, ctypes.POINTER(Plan)]
         _lib = L
     return _lib
 
@@ -38,6 +43,16 @@ def lib():
 def workspace_bytes(T: int, top_k: int, H: int, I: int) -> int:
     """Bytes of workspace that `experts` needs."""
     return int(lib().w4a16_moe_workspace_bytes(T, top_k, H, I))
+
+
+def query_plan(T: int, E: int, top_k: int, H: int, I: int) -> dict:
+    """What `experts` runs for a layer of these sizes: `tiles` or streamed weights; rows of an expert at a time and bytes of LDS of a workgroup of the gate and up
+    product and of the down product."""
+    p = Plan()
+    rc = lib().w4a16_moe_query_plan(T, E, top_k, H, I, ctypes.byref(p))
+    if rc:
+        raise W4A16Error(rc, "w4a16_moe_query_plan")
+    return {name: getattr(p, name) for name, _ in Plan._fields_}
 
 
 def route(logits, top_k: int, scoring: str = "softmax", renormalize: bool = True, factor: float = 1.0, out=None, stream=None):

@@ -80,8 +80,8 @@ int w4a16_moe_route(const void *logits, int dtype, int T, int E, long long ld, i
  * X and Y [T, H] both FP16 or both BF16 (`dtype`); weights in MXFP4: codes13, scales13 of [E, 2 I, H] (of each expert first the I
  * rows of W1, the gate, then those of W3), codes2, scales2 of [E, H, I].  act: SiLU, g / (1 + exp(-g)), or GELU, 0.5 g (1 +
  * tanh(sqrt(2 / pi) (g + 0.044715 g^3))).  An id outside 0 .. E - 1 stands for no expert (its weight is not read); a token without
- * any gets zeros; an expert named twice counts twice.  FP32 sums; the product of the gate and up halves is rounded to 2^-17 on its way into the second
- * product.  H and I multiples of 32, at most 32768, E <= 1024, top_k <= 32.  `workspace`: device memory of w4a16_moe_workspace_bytes,
+ * any gets zeros; an expert named twice counts twice.  FP32 sums; the product of the gate and up halves (infinite beyond FP32's range) is rounded to 2^-17 on
+ * its way into the second product.  H and I multiples of 32, at most 32768, E <= 1024, top_k <= 32.  `workspace`: device memory of w4a16_moe_workspace_bytes,
  * 256-byte aligned, contents irrelevant, used by this call alone until its work on `stream` is done.
  */
 typedef enum { W4A16_MOE_SILU = 0, W4A16_MOE_GELU = 1 } w4a16_moe_activation;

@@ -75,13 +75,15 @@ __device__ __forceinline__ float activate(float g, int activation)
     return 0.5f * g * (1.0f + tanhf(0.7978845608f * (g + 0.044715f * g * g * g)));
 }
 
-// h of pair p as the sum of two BF16 numbers.
+// h of pair p as the sum of two BF16 numbers.  What is beyond the largest BF16 number has that as its upper term; an infinity is itself and 0.
 __device__ __forceinline__ void store_hidden(const MoeArgs &a, size_t p, int i, float h)
 {
-    const uint16_t hi = to_16bit(h, 1);
-    const float rest = h - __builtin_bit_cast(float, (uint32_t)hi << 16);
+    uint32_t hi = to_16bit(h, 1);
+    const bool infinite = __builtin_fabsf(h) == __builtin_inff();
+    if ((hi & 0x7FFFu) == 0x7F80u && !infinite) --hi;
+    const float rest = infinite ? 0.f : h - __builtin_bit_cast(float, hi << 16);
     uint16_t *const to = a.hidden + p * (size_t)a.I + (size_t)i;
-    to[0] = hi;
+    to[0] = (uint16_t)hi;
     to[(size_t)a.T * (size_t)a.top_k * (size_t)a.I] = to_16bit(rest, 1);
 }
 

@@ -78,13 +78,14 @@ def route(logits, top_k, sigmoid=False, renormalize=True, factor=1.0):
         if not order:
             continue
         with np.errstate(all="ignore"):
-            if sigmoid:
-                score = 1.0 / (1.0 + np.exp(-row))
+            if sigmoid:  # by its logarithm, -log(1 + e^-l): quotients of sigmoids that are themselves below the range of 64 bits
+                log = -np.logaddexp(0.0, -row[order])
+                chosen = np.exp(log - log.max() if renormalize else log)
                 total = 1.0
             else:
                 score = np.exp(row - row[order[0]])
                 total = score.sum()
-            chosen = score[order]
+                chosen = score[order]
             if renormalize:
                 total = chosen.sum()
             ids[t, :len(order)] = order

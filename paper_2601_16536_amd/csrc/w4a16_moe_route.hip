@@ -107,7 +107,13 @@ __global__ __launch_bounds__(64 * kTokens) void moe_route_kernel(const void *__r
         }
     }
     float w = 0.f;
-    if (id >= 0) w = sigmoid ? 1.0f / (1.0f + expf(-value_of(mine))) : expf(value_of(mine) - value_of(first));
+    if (id >= 0) {
+        const float l = value_of(mine), top = value_of(first);
+        if (!sigmoid) w = expf(l - top);
+        // To be divided by their sum, which is 0 where all sigmoids are below FP32's range: with negative logits 1 / (1 + e^-l) = e^l / (1 + e^l), all times e^-top.
+        else if (renormalize && top < 0.f) w = expf(l - top) / (1.0f + expf(l));
+        else w = 1.0f / (1.0f + expf(-l));
+    }
     if (renormalize) all = across(w, sum);
     else if (sigmoid) all = 1.0f;
     if (lane < top_k) {

@@ -110,3 +110,43 @@ def test_infinite_x(moe, T):
     ids = rng.integers(0, E, (T, 1))
     Y = _run(moe, tmoe._torch(x).to(torch.bfloat16), ids, np.ones((T, 1), np.float32), c13, s13, c2, s2)
     assert np.array_equal(Y, np.sign(mo.values(c2, s2)[ids[:, 0], :, 0]) * np.inf)
+
+
+# ---- routing: sigmoids below FP32's range ----
+
+def test_oracle_divides_sigmoids_that_vanish():
+    for l in (0.0, -50.0, -89.0, -800.0, -1e30):
+        _, w = mo.route([[l] * 8], 4, sigmoid=True)
+        assert np.allclose(w, 0.25, rtol=1e-12)
+    _, w = mo.route([[-800.0, -801.0, -802.0]], 2, sigmoid=True)
+    assert np.allclose(w, [[1 / (1 + np.exp(-1.0)), 1 / (1 + np.exp(1.0))]], rtol=1e-12)
+    rng = np.random.default_rng(1)
+    l = rng.standard_normal((5, 9)) * 3
+    ids, w = mo.route(l, 3, sigmoid=True)
+    s = np.take_along_axis(1 / (1 + np.exp(-l)), ids, 1)
+    assert np.allclose(w, s / s.sum(1, keepdims=True), rtol=1e-12)
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["float32", "float16", "bfloat16"])
+@pytest.mark.parametrize("E", [8, 130, 700])
+def test_renormalized_sigmoids_of_very_negative_logits(moe, kind, E):
+    """The tolerance of test_moe.py: at most 32 terms of 2 roundings each in a sum, and l - top rounded: |l - top| <= 104 where the result is an FP32 number, 52 of 2^-23;
+    below (32 / 2 + 8 + 52) 2^-23."""
+    import torch
+    rng = np.random.default_rng(E)
+    rows = np.stack([np.full(E, l) for l in (-1.0, -50.0, -88.0, -89.0, -90.0, -100.0, -104.0, -300.0, -6e4)])
+    near = -rng.uniform(80, 200, (40, 1)) - rng.uniform(0, 20, (40, E))       # some beside each other, all beyond the range
+    wide = -np.exp(rng.uniform(0, 10, (40, E)))                               # of every size
+    both = rng.standard_normal((40, E)) * 60                                  # a positive one among them
+    holes = near.copy()
+    holes[rng.random((40, E)) < 0.9] = -np.inf
+    logits = tmoe._torch(np.concatenate([rows, near, wide, both, holes])).to(getattr(torch, kind))
+    for renormalize in (True, False):
+        ids, w = moe.route(logits, 8, scoring="sigmoid", renormalize=renormalize, factor=2.5)
+        want, ww = mo.route(tmoe._exact(logits), 8, True, renormalize, 2.5)
+        assert np.array_equal(ids.cpu().numpy(), want)
+        got = tmoe._exact(w)
+        assert np.all(np.abs(got - ww) <= (32 / 2 + 8 + 52) * 2.0 ** -23 * ww + 2.5 * 2.0 ** -126)
+        if renormalize:
+            assert np.allclose(got[(want >= 0).any(1)].sum(1), 2.5, rtol=1e-5)

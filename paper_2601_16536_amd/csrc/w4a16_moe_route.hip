@@ -140,12 +140,23 @@ hipError_t launch(const void *logits, int T, int E, long long ld, int top_k, boo
 
 }  // namespace
 
+// A grid has fewer than 2^32 threads in a dimension (what goes beyond is dropped without an error): so many tokens per launch.
+constexpr int kLaunchTokens = 1 << 24;
+
 hipError_t launch_moe_route(const void *logits, int type, int T, int E, long long ld, int top_k, bool sigmoid, bool renormalize, float factor,
                             int32_t *ids, float *weights, hipStream_t stream)
 {
-    if (type == kTypeF16) return launch<kTypeF16>(logits, T, E, ld, top_k, sigmoid, renormalize, factor, ids, weights, stream);
-    if (type == kTypeBF16) return launch<kTypeBF16>(logits, T, E, ld, top_k, sigmoid, renormalize, factor, ids, weights, stream);
-    return launch<kTypeF32>(logits, T, E, ld, top_k, sigmoid, renormalize, factor, ids, weights, stream);
+    for (long long t = 0; t < T; t += kLaunchTokens) {
+        const int n = T - t < kLaunchTokens ? (int)(T - t) : kLaunchTokens;
+        const void *const from = static_cast<const uint8_t *>(logits) + t * ld * (type == kTypeF32 ? 4 : 2);
+        int32_t *const to = ids + t * top_k;
+        float *const w = weights + t * top_k;
+        const hipError_t e = type == kTypeF16    ? launch<kTypeF16>(from, n, E, ld, top_k, sigmoid, renormalize, factor, to, w, stream)
+                             : type == kTypeBF16 ? launch<kTypeBF16>(from, n, E, ld, top_k, sigmoid, renormalize, factor, to, w, stream)
+                                                 : launch<kTypeF32>(from, n, E, ld, top_k, sigmoid, renormalize, factor, to, w, stream);
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 }  // namespace w4a16

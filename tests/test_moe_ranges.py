@@ -56,3 +56,16 @@ LONG = [(1, 2, 2, 32, LONGEST), (10, 4, 2, 96, LONGEST), (3, 4, 2, 64, 29728), (
 def test_longest_rows_match_the_oracle(moe, kind, T, E, top_k, H, I):
     import torch
     tmoe.check_layer(moe, np.random.default_rng([T, E, H]), T, E, top_k, H, I, getattr(torch, kind), ldx=8 * (T % 3))
+
+
+@gpu
+def test_more_tokens_than_one_grid_has_threads_for(moe):
+    """Four tokens to 256 threads: 2^26 tokens are 2^32 threads.  Two experts, the larger logit's one wanted."""
+    import torch
+    T = 2 ** 26 + 5
+    logits = torch.zeros(T, 2, dtype=torch.bfloat16, device="cuda")
+    logits[::3, 1] = 1
+    ids = torch.full((T, 1), 7, dtype=torch.int32, device="cuda")
+    w = torch.full((T, 1), 7.0, device="cuda")
+    moe.route(logits, 1, factor=0.5, out=(ids, w))
+    assert torch.equal(ids[:, 0], logits[:, 1].int()) and bool((w == 0.5).all())

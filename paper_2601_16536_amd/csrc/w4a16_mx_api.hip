@@ -29,10 +29,28 @@ MxTilePlan plan_product(const MxGemmArgs &a)
     const MxTilePlan tiles = plan_mx_tile(a);
     return rows.us <= tiles.us ? rows : tiles;
 }
-hipError_t launch_product(const MxGemmArgs &a, hipStream_t stream)
+// Rows and columns of Y per launch: a grid has fewer than 2^32 threads in its first dimension (a matrix of few rows takes up to 32 per column; what
+// goes beyond is dropped without an error) and at most 65535 blocks in its second.
+constexpr int kLaunchRows = 1 << 19, kLaunchColumns = 1 << 26;
+
+hipError_t launch_product(const MxGemmArgs &all, hipStream_t stream)
 {
-    const MxTilePlan p = plan_product(a);
-    return p.tile_n == 16 ? launch_mx_rows(a, stream) : launch_mx_tile(a, p.form, stream);
+    const size_t row_x = all.xs ? (size_t)all.K / 2 : (size_t)all.ldx * 2, row_w = (size_t)all.K / 2, row_s = (size_t)all.K / kMxBlock;
+    for (long long m = 0; m < all.M; m += kLaunchRows)
+        for (long long n = 0; n < all.N; n += kLaunchColumns) {
+            MxGemmArgs a = all;
+            a.M = all.M - m < kLaunchRows ? (int)(all.M - m) : kLaunchRows;
+            a.N = all.N - n < kLaunchColumns ? (int)(all.N - n) : kLaunchColumns;
+            a.X = static_cast<const uint8_t *>(all.X) + (size_t)m * row_x;
+            if (all.xs) a.xs = all.xs + (size_t)m * row_s;
+            a.codes = all.codes + (size_t)n * row_w;
+            a.scales = all.scales + (size_t)n * row_s;
+            a.Y = static_cast<uint16_t *>(all.Y) + (size_t)m * (size_t)all.ldy + (size_t)n;
+            const MxTilePlan p = plan_product(a);
+            const hipError_t e = p.tile_n == 16 ? launch_mx_rows(a, stream) : launch_mx_tile(a, p.form, stream);
+            if (e != hipSuccess) return e;
+        }
+    return hipSuccess;
 }
 
 int check_gemm(int M, int N, int K, int dtype, long long ldy)
@@ -58,8 +76,8 @@ int asked(int M, int N, int K, int dtype, int x_mx, MxGemmArgs *a)
     if (M < 1) return W4A16_ERR_SHAPE;
     *a = {};
     a->xs = x_mx ? reinterpret_cast<const uint8_t *>(a) : nullptr;
-    a->M = M;
-    a->N = N;
+    a->M = M < kLaunchRows ? M : kLaunchRows;  // the first launch
+    a->N = N < kLaunchColumns ? N : kLaunchColumns;
     a->K = K;
     a->type = dtype;
     return W4A16_OK;

@@ -66,3 +66,59 @@ def test_the_longest_rows_are_of_the_kernel_for_few_rows(mx):
 def test_longest_rows_match_the_oracle(mx, kind, M, N, K):
     Y, ref, terms = _product(mx, kind, np.random.default_rng([M, N, K]), M, N, K)
     tmx.check(Y, ref, terms, K, "M=%d N=%d K=%d %s" % (M, N, K, kind))
+
+
+@pytest.mark.parametrize("kind", ["float16", "bfloat16", "mx"])
+def test_the_largest_sizes_have_a_plan(mx, kind):
+    most = 2 ** 31 - 1
+    for M, N, K in ((most, 1, 32), (1, most, 32), (most, most, 32), (most, 1, 128), (most, 64, 1024), (16, most, 4096), (most, most, LONGEST)):
+        lds, chunks = mx.query_lds(M, N, K, **_how(kind))
+        assert 0 < lds <= LDS and chunks >= 1
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["bfloat16", "mx"])
+def test_more_columns_than_one_grid_has_threads_for(mx, kind):
+    """Four threads to a column: 2^30 columns are 2^32 threads.  x is 1 at k = 0 alone, so Y is W's first column: elements 0 .. 6 in turn, with a scale of 1 or 2."""
+    import torch
+    N, K = 2 ** 30 + 37, 32
+    codes = torch.zeros(N, K // 2, dtype=torch.uint8, device="cuda")
+    scales = torch.full((N, 1), 127, dtype=torch.uint8, device="cuda")
+    turn = torch.arange(N, dtype=torch.int32, device="cuda").remainder_(40).to(torch.uint8)
+    codes[:, 0] = turn % 8
+    scales[:, 0] += turn // 20
+    values = torch.tensor(mo.MAGNITUDES, device="cuda", dtype=torch.bfloat16)[torch.arange(40, device="cuda") % 8] * (1 + torch.arange(40, device="cuda") // 20)
+    if kind == "mx":
+        xc = torch.zeros(1, K // 2, dtype=torch.uint8, device="cuda")
+        xc[0, 0] = 2
+        Y = mx.gemm_mx(xc, torch.full((1, 1), 127, dtype=torch.uint8, device="cuda"), codes, scales)
+    else:
+        x = torch.zeros(1, K, dtype=torch.bfloat16, device="cuda")
+        x[0, 0] = 1
+        Y = mx.gemm(x, codes, scales)
+    for n in range(0, N, 2 ** 27):  # 40 divides no power of two: the pieces begin at places of their own
+        here = Y[0, n:n + 2 ** 27]
+        assert torch.equal(here, values[turn[n:n + 2 ** 27].int()])
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["float16", "bfloat16", "mx"])
+@pytest.mark.parametrize("K", [32, 160])
+def test_many_rows(mx, kind, K):
+    """More row blocks than a grid's second dimension is documented to hold, and pieces of rows: strided X and Y, every row with numbers of its own."""
+    import torch
+    M, N = 65535 * 16 + 21, 5
+    rng = np.random.default_rng(K)
+    wc, ws = tmx._random_mx(rng, N, K, 126, 129)
+    W = torch.from_numpy(mo.values(wc, ws)).float().cuda()
+    out = torch.full((M, N + 2), 9.0, dtype=torch.bfloat16 if kind == "mx" else getattr(torch, kind), device="cuda")
+    x = torch.randint(-2, 3, (M, K + 8), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).float()[:, :K]
+    if kind == "mx":
+        xc, xs = mx.quantize(x.contiguous())
+        mx.gemm_mx(xc, xs, tmx._torch(wc), tmx._torch(ws), out=out[:, :N])
+    else:
+        big = torch.zeros(M, K + 8, dtype=out.dtype, device="cuda")
+        big[:, :K] = x
+        mx.gemm(big[:, :K], tmx._torch(wc), tmx._torch(ws), out=out[:, :N])
+    want = torch.stack([(x * W[n]).sum(1) for n in range(N)], 1).to(out.dtype)  # whole multiples of a quarter below 2^12: exact in FP32
+    assert torch.equal(out[:, :N], want) and bool((out[:, N:] == 9.0).all())

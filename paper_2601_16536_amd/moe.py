@@ -92,7 +92,7 @@ def _check_choice(ids, weights, T: int) -> None:
 
 def experts(X, ids, weights, codes13, scales13, codes2, scales2, activation: str = "silu", out=None, workspace=None, stream=None):
     """Y [T, H]: for every token the weighted sum of its experts' W2 (act(W1 x) * (W3 x)).  X [T, H] float16 or bfloat16; codes13, scales13
-    of [E, 2 I, H], codes2, scales2 of [E, H, I] in MXFP4; activation 'silu' or 'gelu'.  `workspace`: a CUDA uint8 tensor of
+    of [E, 2 I, H], codes2, scales2 of [E, H, I] in MXFP4; activation 'silu' or 'gelu'.  `workspace`: a contiguous CUDA tensor of
     workspace_bytes(T, top_k, H, I), 256-byte aligned, this call's own until its work is done; by default one from torch's allocator
     (on the current stream: with an explicit stream bring one)."""
     import torch
@@ -112,6 +112,8 @@ def experts(X, ids, weights, codes13, scales13, codes2, scales2, activation: str
         if stream is not None:
             raise ValueError("with an explicit stream the workspace has to be brought too")
         workspace = torch.empty(need, dtype=torch.uint8, device=X.device)
+    elif not (workspace.is_cuda and workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous CUDA tensor")
     rc = lib().w4a16_moe_experts(X.data_ptr(), code, ld, ids.data_ptr(), weights.data_ptr(), codes13.data_ptr(), scales13.data_ptr(), codes2.data_ptr(),
                                  scales2.data_ptr(), T, lead13[0], top_k, H, I, ACTIVATIONS[activation], Y.data_ptr(), ldy, workspace.data_ptr(),
                                  workspace.numel() * workspace.element_size(), _stream(stream))

@@ -150,3 +150,20 @@ def test_renormalized_sigmoids_of_very_negative_logits(moe, kind, E):
         assert np.all(np.abs(got - ww) <= (32 / 2 + 8 + 52) * 2.0 ** -23 * ww + 2.5 * 2.0 ** -126)
         if renormalize:
             assert np.allclose(got[(want >= 0).any(1)].sum(1), 2.5, rtol=1e-5)
+
+
+# ---- a workspace that is none ----
+
+@gpu
+def test_workspace_on_the_host_or_with_gaps_is_refused(moe):
+    import torch
+    from paper_2601_16536_amd import mx
+    (c13, s13), (c2, s2) = mx.quantize(torch.zeros(4, 64, 64, device="cuda")), mx.quantize(torch.zeros(4, 64, 32, device="cuda"))
+    x = torch.zeros(2, 64, dtype=torch.float16, device="cuda")
+    ids, w = moe.route(torch.zeros(2, 4, device="cuda"), 2)
+    need = moe.workspace_bytes(2, 2, 64, 32)
+    for workspace in (torch.empty(need, dtype=torch.uint8), torch.empty(need, dtype=torch.uint8, pin_memory=True), torch.empty(2 * need, dtype=torch.uint8, device="cuda")[::2]):
+        with pytest.raises(TypeError):
+            moe.experts(x, ids, w, c13, s13, c2, s2, workspace=workspace)
+    flat = torch.empty(need // 4, device="cuda")  # of any type
+    assert not bool(moe.experts(x, ids, w, c13, s13, c2, s2, workspace=flat).any())

@@ -919,6 +919,7 @@ int hip_status(hipError_t e)
 {
     if (e == hipSuccess) return W4A16_OK;
     note_hip_error(e);
+    (void)hipGetLastError();  // (a call other than a launch leaves it for the next one to find)
     return W4A16_ERR_HIP;
 }
 

@@ -1,6 +1,7 @@
 """MXFP4 products over the whole range of sizes that the header names: what is planned, on the CPU, and the ends of the range on the GPU.  Tolerances
 as derived in test_mx.py (16 waves at most, K/32 + 16 + 128 roundings: whatever the pieces that K comes in, a wave's sums are one chain)."""
 import os
+import subprocess
 import sys
 
 import numpy as np
@@ -122,3 +123,25 @@ def test_many_rows(mx, kind, K):
         mx.gemm(big[:, :K], tmx._torch(wc), tmx._torch(ws), out=out[:, :N])
     want = torch.stack([(x * W[n]).sum(1) for n in range(N)], 1).to(out.dtype)  # whole multiples of a quarter below 2^12: exact in FP32
     assert torch.equal(out[:, :N], want) and bool((out[:, N:] == 9.0).all())
+
+
+def test_a_failing_call_leaves_no_error_behind(tmp_path):
+    """A runtime whose hipFuncSetAttribute fails, in a child process: the call ends there, before anything is launched, and what the runtime keeps of it must not be the
+    next caller's.  16 rows, K = N = 4096: a kernel that asks for more LDS than the default."""
+    source, shim = tmp_path / "shim.c", tmp_path / "shim.so"
+    source.write_text("static int last;\n"
+                      "int hipFuncSetAttribute(const void *f, int a, int v) { (void)f; (void)a; (void)v; return last = 1; }\n"
+                      "int hipGetLastError(void) { int e = last; last = 0; return e; }\n")
+    subprocess.check_call(["gcc", "-shared", "-fPIC", "-o", str(shim), str(source)])
+    code = """if True:
+        import ctypes, sys
+        shim = ctypes.CDLL(sys.argv[1], ctypes.RTLD_GLOBAL)
+        from paper_2601_16536_amd import binding, mx
+        assert mx.lib().w4a16_mx_gemm(256, 1, 4096, 256, 256, 16, 4096, 4096, 256, 4096, 0) == binding.ERR_HIP
+        assert "invalid argument" in binding.last_hip_error(), binding.last_hip_error()
+        assert shim.hipGetLastError() == 0
+        print("clean")
+        """
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", code, str(shim)], cwd=root, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
+    assert r.returncode == 0 and "clean" in r.stdout, r.stdout[-2000:]

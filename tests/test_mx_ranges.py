@@ -145,3 +145,20 @@ def test_a_failing_call_leaves_no_error_behind(tmp_path):
     root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
     r = subprocess.run([sys.executable, "-c", code, str(shim)], cwd=root, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=300)
     assert r.returncode == 0 and "clean" in r.stdout, r.stdout[-2000:]
+
+
+# X in several pieces of K: 16 waves and 8 (N above 4096), K of whole steps and not, one piece short of whole pairs, all three types
+CHUNKED = [("mx", 16, 100, 28672), ("mx", 16, 100, 28640), ("mx", 7, 4130, 20000), ("mx", 6, 4100, 21504), ("mx", 21, 40, 28672)]
+CHUNKED += [(kind, *sizes) for kind in ("bfloat16", "float16") for sizes in ((8, 70, 16384), (11, 70, 16416), (3, 4130, 12512), (2, 4100, 18432), (1, 4099, 32960))]
+
+
+def test_the_chunked_shapes_are_of_several_chunks(mx):
+    for kind, M, N, K in CHUNKED:
+        assert mx.query_tile(M, N, K, **_how(kind)) == (16, 16) and mx.query_lds(M, N, K, **_how(kind))[1] > 1, (kind, M, N, K)
+
+
+@gpu
+@pytest.mark.parametrize("kind,M,N,K", CHUNKED)
+def test_x_in_chunks_matches_the_oracle(mx, kind, M, N, K):
+    Y, ref, terms = _product(mx, kind, np.random.default_rng([M, N, K]), M, N, K)
+    tmx.check(Y, ref, terms, K, "M=%d N=%d K=%d %s" % (M, N, K, kind))

@@ -13,7 +13,7 @@ namespace {
 
 // ---- products with up to sixteen rows of X: weights streamed from memory, X through LDS ----
 //
-// A wave holds one MFMA tile of sums per matrix of W that it multiplies (CT of them, 16 rows of W each) and walks its steps of K (128 values): 16 bytes
+// A wave holds one MFMA tile of sums (16 rows of W) and walks its steps of K (128 values): 16 bytes
 // per lane of codes and a word of scales from memory, DEPTH steps in flight, X from LDS.  The waves of a workgroup are `parts` shares of K
 // times tiles of W; X, which all of them read, is staged in chunks of K, the next chunk on its way while the present one is used.
 //
@@ -45,12 +45,11 @@ __host__ __device__ inline MxChunk mx_chunk(int steps)
 // Rows of scales: an odd multiple of eight bytes apart.
 __host__ __device__ inline uint32_t mx_scale_row(int blocks) { return (((uint32_t)blocks + 7u) / 8u | 1u) * 8u; }
 // LDS of a workgroup: X, the scales of 16 `groups` rows of W, those of X.
-template <class Op>
-__host__ __device__ inline uint32_t mx_lds_x(const MxChunk &c, int rows) { return (uint32_t)rows * c.row * Op::kTerms; }
+__host__ __device__ inline uint32_t mx_lds_x(const MxChunk &c, int rows) { return (uint32_t)rows * c.row; }
 template <class Op>
 __host__ __device__ inline uint32_t mx_lds(const MxChunk &c, int rows, int blocks, int groups)
 {
-    return mx_lds_x<Op>(c, rows) + ((uint32_t)groups * 16u + (Op::kMx ? (uint32_t)rows : 0u)) * mx_scale_row(blocks);
+    return mx_lds_x(c, rows) + ((uint32_t)groups * 16u + (Op::kMx ? (uint32_t)rows : 0u)) * mx_scale_row(blocks);
 }
 
 // The pairs of steps (128 bytes of W's rows, a line) of chunk q that share `part` of `parts` takes.  A chunk that is not the last has whole pairs.
@@ -63,12 +62,11 @@ __device__ __forceinline__ MxRange mx_range(int chunk_steps, int total, int q, i
     return {first / 2 + pairs * part / parts, first / 2 + pairs * (part + 1) / parts};
 }
 
-// W's codes as a wave reads them: a pointer that is the same in every lane, and the lane's 32-bit offsets: its row of W (row lane mod 16 of a tile)
+// W's codes as a wave reads them: a pointer that is the same in every lane, and the lane's 32-bit offset: its row of W (row lane mod 16 of the tile)
 // plus 16 (lane / 16) bytes.  `row`: the row of scales in LDS that goes with it.
-template <int CT>
 struct MxWeights {
     const uint8_t *w;
-    uint32_t wo[CT], row[CT];
+    uint32_t wo, row;
 };
 // Rows of scales, one after the other in memory.
 struct MxScales {
@@ -76,24 +74,24 @@ struct MxScales {
     uint32_t bytes;
 };
 
-// acc[t] += X W_t^T over this wave's share of K = 32 blocks values; acc as the 16 x 16 MFMAs have it: lane (c, p) holds column c, rows 4 p .. 4 p + 3.
-// X: `rows` rows; row(r, term) gives where row r begins; x_scales (MXFP4): their scales.  `groups` times 16 rows of W: scales(g).  NI: of a lane's four
+// acc += X W^T over this wave's share of K = 32 blocks values; acc as the 16 x 16 MFMAs have it: lane (c, p) holds column c, rows 4 p .. 4 p + 3.
+// X: `rows` rows; row(r) gives where row r begins; x_scales (MXFP4): their scales.  `groups` times 16 rows of W: scales(g).  NI: of a lane's four
 // rows, those that are wanted (rows <= NI, or NI = 4).  WHOLE: K is whole steps.  MULTI: more than one chunk.  `lds`: mx_lds.  Every thread of the
 // workgroup has to call this; a barrier ends it.
-template <class Op, int CT, int NI, bool WHOLE, bool MULTI, int DEPTH, class Row, class Scales>
-__device__ __forceinline__ void mx_stream(float4_t (&acc)[CT], const MxWeights<CT> &o, int blocks, int part, int parts, const MxChunk &ch, int rows, int groups,
+template <class Op, int NI, bool WHOLE, bool MULTI, int DEPTH, class Row, class Scales>
+__device__ __forceinline__ void mx_stream(float4_t &acc, const MxWeights &o, int blocks, int part, int parts, const MxChunk &ch, int rows, int groups,
                                           uint8_t *lds, Row row, MxScales x_scales, Scales scales)
 {
     struct Pair {
-        uint4_t w[2][CT];
+        uint4_t w[2];
     };
     const int tid = (int)threadIdx.x, threads = (int)blockDim.x, lane = tid & 63, col = lane & 15, p16 = lane >> 4;
     const int total = (blocks + kMxStepBlocks - 1) / kMxStepBlocks, chunks = MULTI ? (total + ch.steps - 1) / ch.steps : 1;
-    uint8_t *const lds_s = lds + mx_lds_x<Op>(ch, rows);
+    uint8_t *const lds_s = lds + mx_lds_x(ch, rows);
     const uint32_t srow = mx_scale_row(blocks);
 
     // ---- X ----
-    // Unit u of a chunk is 16 bytes: `units` to a row, rows in order, the rows of a second term after those of the first.
+    // Unit u of a chunk is 16 bytes: `units` to a row, rows in order.
     constexpr int kStepUnits = Op::kMx ? 4 : 16;
     const int row_units = blocks * (Op::kMx ? 1 : 4);
     uint4_t stage[kMxXUnits];
@@ -102,9 +100,9 @@ __device__ __forceinline__ void mx_stream(float4_t (&acc)[CT], const MxWeights<C
 #pragma unroll
         for (int i = 0; i < kMxXUnits; ++i) {
             const int u = from + tid + i * threads;
-            if (u < units * rows * Op::kTerms) {
+            if (u < units * rows) {
                 const int r = u / units;
-                stage[i] = *reinterpret_cast<const uint4_t *>(row(Op::kTerms == 2 ? r % rows : r, Op::kTerms == 2 ? r / rows : 0) + ((size_t)q * (uint32_t)(ch.steps * kStepUnits) + (uint32_t)(u - r * units)) * 16);
+                stage[i] = *reinterpret_cast<const uint4_t *>(row(r) + ((size_t)q * (uint32_t)(ch.steps * kStepUnits) + (uint32_t)(u - r * units)) * 16);
             }
         }
     };
@@ -113,7 +111,7 @@ __device__ __forceinline__ void mx_stream(float4_t (&acc)[CT], const MxWeights<C
 #pragma unroll
         for (int i = 0; i < kMxXUnits; ++i) {
             const int u = from + tid + i * threads;
-            if (u < units * rows * Op::kTerms) {
+            if (u < units * rows) {
                 const int r = u / units;
                 *reinterpret_cast<uint4_t *>(lds + (uint32_t)r * ch.row + (uint32_t)(u - r * units) * 16) = stage[i];
             }
@@ -188,64 +186,43 @@ __device__ __forceinline__ void mx_stream(float4_t (&acc)[CT], const MxWeights<C
             back0 = (uint32_t)max(p16 - last, 0) * 16;
             back1 = (uint32_t)max(p16 + kMxStepBlocks - last, 0) * 16;
         }
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-            f.w[0][t] = *reinterpret_cast<const uint4_t *>(w + (o.wo[t] - back0));
-            f.w[1][t] = *reinterpret_cast<const uint4_t *>(w + (o.wo[t] + 64 - back1));
-        }
+        f.w[0] = *reinterpret_cast<const uint4_t *>(w + (o.wo - back0));
+        f.w[1] = *reinterpret_cast<const uint4_t *>(w + (o.wo + 64 - back1));
     };
     const uint32_t xo = (uint32_t)min(col, rows - 1) * ch.row + (uint32_t)p16 * 16, xso = (uint32_t)(groups * 16 + min(col, rows - 1)) * srow;
-    uint32_t so[CT];
-#pragma unroll
-    for (int t = 0; t < CT; ++t) so[t] = o.row[t] * srow;
-    auto step = [&](uint4_t (&w)[CT], const uint32_t (&ws)[CT], uint32_t xs, int at, int have) {  // `at`: the step's place in the chunk; `have`: its blocks
+    const uint32_t so = o.row * srow;
+    auto step = [&](uint4_t &w, uint32_t ws, uint32_t xs, int at, int have) {  // `at`: the step's place in the chunk; `have`: its blocks
         const uint8_t *const x = lds + xo + (uint32_t)at * (Op::kMx ? 64u : 256u);
         if constexpr (Op::kMx) {
             uint4_t xv = *reinterpret_cast<const uint4_t *>(x);
             xs >>= 8 * p16;
+            uint32_t s = ws >> (8 * p16);
             if (!WHOLE && p16 >= have) {  // zeros
                 xv = (uint4_t){0u, 0u, 0u, 0u};
                 xs = 127u;
+                s = 127u;
             }
-#pragma unroll
-            for (int t = 0; t < CT; ++t) {
-                uint32_t s = ws[t] >> (8 * p16);
-                if (!WHOLE && p16 >= have) s = 127u;
-                acc[t] = Op::multiply(xv, xs, w[t], s, acc[t]);
-            }
+            acc = Op::multiply(xv, xs, w, s, acc);
         } else {
-            uint4_t xv[Op::kTerms][kMxStepBlocks];
+            uint4_t xv[kMxStepBlocks];
 #pragma unroll
-            for (int h = 0; h < Op::kTerms; ++h)
+            for (int j = 0; j < kMxStepBlocks; ++j) xv[j] = *reinterpret_cast<const uint4_t *>(x + j * 64);
+            blocks_to_words(w);
 #pragma unroll
-                for (int j = 0; j < kMxStepBlocks; ++j) xv[h][j] = *reinterpret_cast<const uint4_t *>(x + (uint32_t)h * (uint32_t)rows * ch.row + j * 64);
-#pragma unroll
-            for (int t = 0; t < CT; ++t) {
-                blocks_to_words(w[t]);
-#pragma unroll
-                for (int j = 0; j < kMxStepBlocks; ++j) {
-                    if (!WHOLE && j >= have) break;
-                    const uint32_t s = (ws[t] >> (8 * j)) & 0xFFu;
-                    const uint4_t b = Op::operand(w[t][j], s);
-#pragma unroll
-                    for (int h = 0; h < Op::kTerms; ++h) acc[t] = Op::template multiply<NI>(xv[h][j], b, s, acc[t]);
-                }
+            for (int j = 0; j < kMxStepBlocks; ++j) {
+                if (!WHOLE && j >= have) break;
+                const uint32_t s = (ws >> (8 * j)) & 0xFFu;
+                acc = Op::template multiply<NI>(xv[j], Op::operand(w[j], s), s, acc);
             }
         }
     };
     auto compute = [&](Pair &f, int k, int q, bool full) {
         const int at = 2 * k - q * ch.steps, left = blocks - 2 * k * kMxStepBlocks;
-        uint32_t s0[CT], s1[CT];
-#pragma unroll
-        for (int t = 0; t < CT; ++t) {
-            const uint2_t v = *reinterpret_cast<const uint2_t *>(lds_s + so[t] + (uint32_t)k * 8);
-            s0[t] = v[0];
-            s1[t] = v[1];
-        }
+        const uint2_t s = *reinterpret_cast<const uint2_t *>(lds_s + so + (uint32_t)k * 8);
         uint2_t xs = {0u, 0u};
         if constexpr (Op::kMx) xs = *reinterpret_cast<const uint2_t *>(lds_s + xso + (uint32_t)k * 8);
-        step(f.w[0], s0, xs[0], at, full ? kMxStepBlocks : min(left, kMxStepBlocks));
-        if (full || left > kMxStepBlocks) step(f.w[1], s1, xs[1], at + 1, full ? kMxStepBlocks : min(left - kMxStepBlocks, kMxStepBlocks));
+        step(f.w[0], s[0], xs[0], at, full ? kMxStepBlocks : min(left, kMxStepBlocks));
+        if (full || left > kMxStepBlocks) step(f.w[1], s[1], xs[1], at + 1, full ? kMxStepBlocks : min(left - kMxStepBlocks, kMxStepBlocks));
     };
     // Loads stay where they are asked for: moved together by the compiler they would come in bursts between which nothing is in flight.
     auto keep_loads = [] { __builtin_amdgcn_sched_barrier(0x38F); };
@@ -272,7 +249,7 @@ __device__ __forceinline__ void mx_stream(float4_t (&acc)[CT], const MxWeights<C
     for (int d = 0; d < DEPTH; ++d) load_next(f[d]);
     store_x(0, 0);
     store_scales(0);
-    for (int from = kMxXUnits * threads; from < min(ch.steps * kStepUnits, row_units) * rows * Op::kTerms; from += kMxXUnits * threads) {  // (a single chunk may be larger)
+    for (int from = kMxXUnits * threads; from < min(ch.steps * kStepUnits, row_units) * rows; from += kMxXUnits * threads) {  // (a single chunk may be larger)
         fetch_x(0, from);
         store_x(0, from);
     }
@@ -347,24 +324,24 @@ __global__ __launch_bounds__(64 * WAVES) void mx_rows_kernel(MxGemmArgs a, MxChu
     const uint32_t row_w = (uint32_t)a.K / 2;
 
     // Rows of W past the end read the last one; what comes of them is not stored.
-    MxWeights<1> o;
+    MxWeights o;
     const int base = min(n0, a.N - 1);
     const uint32_t n = (uint32_t)min(col, a.N - 1 - base);
     o.w = a.codes + (size_t)base * row_w;
-    o.wo[0] = n * row_w + (uint32_t)p16 * 16;
-    o.row[0] = (uint32_t)(16 * tile) + n;
+    o.wo = n * row_w + (uint32_t)p16 * 16;
+    o.row = (uint32_t)(16 * tile) + n;
     const size_t row_x = Op::kMx ? (size_t)row_w : (size_t)a.ldx * 2;
     const uint8_t *const x = static_cast<const uint8_t *>(a.X) + (size_t)m0 * row_x;
     const MxScales xs = {Op::kMx ? a.xs + (size_t)m0 * (uint32_t)blocks : nullptr, (uint32_t)rows * (uint32_t)blocks};
 
-    float4_t acc[1] = {(float4_t){0.f, 0.f, 0.f, 0.f}};
-    mx_stream<Op, 1, NI, WHOLE, MULTI, DEPTH>(acc, o, blocks, part, parts, chunk, rows, tiles, lds, [&](int r, int) { return x + (size_t)r * row_x; }, xs, [&](int g) {
+    float4_t acc = {0.f, 0.f, 0.f, 0.f};
+    mx_stream<Op, NI, WHOLE, MULTI, DEPTH>(acc, o, blocks, part, parts, chunk, rows, tiles, lds, [&](int r) { return x + (size_t)r * row_x; }, xs, [&](int g) {
         const int first = min(((int)blockIdx.x * tiles + g) * 16, a.N - 1);
         return MxScales{a.scales + (size_t)first * (uint32_t)blocks, (uint32_t)min(16, a.N - first) * (uint32_t)blocks};
     });
 
     float *const red = reinterpret_cast<float *>(lds);
-    *reinterpret_cast<float4_t *>(red + wave * 256 + lane * 4) = acc[0];
+    *reinterpret_cast<float4_t *>(red + wave * 256 + lane * 4) = acc;
     __syncthreads();
     // Output e of the workgroup: row e / (16 tiles), column e mod (16 tiles); lane 16 (row / 4) + column mod 16 held number row mod 4 of it.
     const int width = 16 * tiles, c0 = (int)blockIdx.x * width;
@@ -406,7 +383,7 @@ RowsPlan plan(const MxGemmArgs &a, int waves)
     p.tiles = waves / p.parts;
     const int blocks = a.K / kMxBlock;
     const size_t limit = waves == 16 ? kMxMostLds : kMxMostLds / 2;  // one or two workgroups to a compute unit
-    const int held = kMxXUnits * 64 * waves / (rows * Op::kTerms * (Op::kMx ? 4 : 16));  // steps that the threads' registers hold
+    const int held = kMxXUnits * 64 * waves / (rows * (Op::kMx ? 4 : 16));  // steps that the threads' registers hold
     auto take = [&](int chunk) {
         p.multi = chunk < steps;
         p.chunk = mx_chunk<Op>(chunk);
@@ -437,7 +414,7 @@ hipError_t launch_rows(const MxGemmArgs &a, hipStream_t stream)
 {
     const int waves = waves_of(a);
     const RowsPlan p = plan<Op>(a, waves);
-    if constexpr (Op::kMx || Op::kTerms == 2) return waves == 16 ? launch<Op, 4, 16, 4>(a, p, stream) : launch<Op, 4, 8, 4>(a, p, stream);
+    if constexpr (Op::kMx) return waves == 16 ? launch<Op, 4, 16, 4>(a, p, stream) : launch<Op, 4, 8, 4>(a, p, stream);
     else if (a.M == 1) return waves == 16 ? launch<Op, 1, 16, 4>(a, p, stream) : launch<Op, 1, 8, 4>(a, p, stream);
     else return waves == 16 ? launch<Op, 4, 16, 4>(a, p, stream) : launch<Op, 4, 8, 4>(a, p, stream);
 }

@@ -45,7 +45,8 @@ int w4a16_mx_dequantize(const uint8_t *codes, const uint8_t *scales, long long r
 
 /*
  * Y[M, N] = X[M, K] W[N, K]^T, W in MXFP4, X and Y both FP16 or both BF16 (`dtype`); FP32 sums, one rounding.  X's elements
- * and the weights enter the products exactly.
+ * and the weights enter the products exactly; but beside BF16 X, and in the experts' layer, a weight that is no FP32 number (+-4 and +-6 with s = 253, +-2 to
+ * +-6 with s = 254; w4a16_mx_quantize makes none) is infinite, as w4a16_mx_dequantize has it.
  */
 int w4a16_mx_gemm(const void *X, int dtype, long long ldx, const uint8_t *codes, const uint8_t *scales, int M, int N, int K, void *Y,
                   long long ldy, void *stream);

@@ -162,3 +162,37 @@ def test_the_chunked_shapes_are_of_several_chunks(mx):
 def test_x_in_chunks_matches_the_oracle(mx, kind, M, N, K):
     Y, ref, terms = _product(mx, kind, np.random.default_rng([M, N, K]), M, N, K)
     tmx.check(Y, ref, terms, K, "M=%d N=%d K=%d %s" % (M, N, K, kind))
+
+
+@gpu
+@pytest.mark.parametrize("kind", ["float16", "bfloat16", "mx"])
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_weights_beyond_fp32(mx, kind, M):
+    """Rows 3 and 30 of W hold 6 2^126 and 2 2^127 in their first block, which no FP32 number is.  x is 2^-20, -2^-20 there, and the sum of the two 0; FP16 and MXFP4 X have
+    that, and row 30's third value beside; with BF16 X such a weight is infinite, and the rows' outputs are no numbers.  The other outputs are as ever."""
+    import torch
+    N, K = 70, 288
+    rng = np.random.default_rng(M)
+    wc, ws = tmx._random_mx(rng, N, K)
+    wc[[3, 30]] = 0
+    ws[3, 0], ws[30, 0] = 253, 254
+    wc[3, 0], wc[30, 0] = 0x77, 0x44
+    wc[30, 16] = 2                                   # 1 at k = 32
+    ws[30, 1] = 127
+    xq = rng.integers(0, 16, (M, K)).astype(np.uint8)
+    xq[:, 0], xq[:, 1], xq[:, 32] = 2, 10, 6         # 1, -1, 4, times the scale
+    xc = xq[:, 0::2] | (xq[:, 1::2] << 4)
+    xs = np.full((M, K // 32), 107, np.uint8)
+    x = mo.values(xc, xs)
+    if kind == "mx":
+        Y = mx.gemm_mx(tmx._torch(xc), tmx._torch(xs), tmx._torch(wc), tmx._torch(ws))
+    else:
+        Y = mx.gemm(tmx._torch(x).to(getattr(torch, kind)), tmx._torch(wc), tmx._torch(ws))
+    y = tmx._exact(Y)
+    others = np.setdiff1d(np.arange(N), [3, 30])
+    ref, terms = mo.gemm(x, wc[others], ws[others])
+    tmx.check(Y[:, torch.from_numpy(others).cuda()], ref, terms, K, "beside weights beyond FP32")
+    if kind == "bfloat16":
+        assert not np.isfinite(y[:, [3, 30]]).any()
+    else:
+        assert not y[:, 3].any() and np.all(y[:, 30] == 4 * 2.0 ** -20)

@@ -9,7 +9,7 @@
  *   codes   uint8 [rows, K/2]   the code of an even k is the low nibble; bit 3 of a code is the sign
  *   scales  uint8 [rows, K/32]  s stands for 2^(s - 127); s = 255: the block's values are NaN
  *
- * K is a multiple of 32 (in products at most 131072); rows may be any number.
+ * K is a multiple of 32 (in products at most 131072); rows may be any number.  Rows of a 16-bit X of the products and the experts are at most 2^23 values apart.
  *
  * All data pointers are DEVICE pointers owned by the caller.  Codes, X and Y of the quantizer and X of the products are
  * 16-byte aligned, and so are every row of an X with a leading dimension (ld: values from a row to the next) and the experts'
@@ -74,7 +74,8 @@ int w4a16_moe_route(const void *logits, int dtype, int T, int E, long long ld, i
                     int32_t *ids, float *weights, void *stream);
 
 /*
- * A mixture of experts' gated feed-forward layers, for a few tokens (any number works; weights are read once per 64):
+ * A mixture of experts' gated feed-forward layers, for a few tokens (up to 2^21 work; an expert's weights come from memory once
+ * per 256 of them, or per 2048 / top_k, if that is less):
  *
  *   Y[t] = sum over j of weights[t, j] W2_e (act(W1_e X[t]) * (W3_e X[t])),  e = ids[t, j],
  *

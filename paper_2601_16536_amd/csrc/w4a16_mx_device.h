@@ -1,5 +1,5 @@
-// Device-side pieces shared by the kernels on microscaled 4-bit weights (MXFP4): the format's conversions and the step of the
-// products that a wave makes by itself.
+// Device-side pieces shared by the kernels on microscaled 4-bit weights (MXFP4): the format's conversions, the exchange among lanes that makes
+// operands of codes, and the multiplication for each format of X.
 //
 // Format: 32 values of a row of K are a block; an element is e2m1 (sign, two exponent bits, one fraction bit: 0, 0.5, 1, 1.5, 2, 3,
 // 4, 6), a block's scale e8m0 (2^(s - 127); 255: the block is not a number).  Codes [rows, K/2] bytes, the even k in the low nibble;

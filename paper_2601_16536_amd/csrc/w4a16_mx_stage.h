@@ -6,7 +6,8 @@
 // asked for DEPTH - 1 stages ahead, one barrier per stage.  What K has beyond whole stages follows in a round of its own, so that nothing in the loop
 // depends on how far K goes: a load, a wait or a shift under a condition there has the compiler wait for everything that is on its way.
 //
-// The memory pipeline takes a load's lines one by one: a KiB of one row 23 cycles, of four rows 43, of sixteen (the codes, 64 bytes of a row) about 100.  So the
+// The memory pipeline takes a load's lines one by one: a KiB from L2 that is one row's takes a compute unit 18 cycles, four rows' 22, sixteen rows' (the codes, 64 bytes of a row) 44,
+// and 64 where the rows are a power of two apart (from memory, with all compute units at it, 80, 82 and 89: there the rate of memory counts).  So the
 // groups' parts of a stage lie side by side: with four groups X comes in whole KiB of a row, and a row's codes are four waves' at the same time.  (Each group in a
 // quarter of K of its own, 32 x 64 tiles, M = 37, K = 10240, N = 4608, BF16: 21.7 us, 18.6 so; 16 x 32 tiles, M = 16, K = 28672, N = 8192 34.4 and 26.1.)
 //

@@ -9,7 +9,7 @@ Submodules are imported on demand so that the seeded input generators
 """
 import importlib
 
-__all__ = ["binding", "moe", "moe_block", "mx", "workloads", "build"]
+__all__ = ["binding", "grouped", "lora", "moe", "moe_block", "mx", "workloads", "build"]
 
 
 def __getattr__(name):

@@ -1,0 +1,255 @@
+// Device-side pieces of the products of rows in groups: which rows a workgroup has, tiles of 16-bit operands in LDS, and the loop over them.
+//
+// A product's operands come in two orders: along (the values to be summed over are neighbours in memory) and across (they are a row apart).  A
+// stage is 64 such values.  Both orders come to LDS by loads that pass no register; MFMA operands, eight neighbours along the sum per lane, are read
+// from an along tile as they are and from an across tile by gfx950's transposing reads:
+//   along   rows of 64 values (128 bytes); 16-byte piece q of row r is at place q ^ (r mod 8)
+//   across  64 rows of SPAN values; the 32 bytes of columns 16 j .. 16 j + 15 of row k are at place j ^ f(k), f(k) = k mod 4 + 4 (k / 8 mod 4)
+// so that the sixteen rows that a read takes lie on all banks evenly.
+#pragma once
+#include "w4a16_mx_device.h"
+#include "w4a16_group.h"
+#include <type_traits>
+
+namespace w4a16 {
+
+typedef __attribute__((address_space(3))) void *lds_ptr_t;
+typedef const __attribute__((address_space(1))) void *global_ptr_t;
+typedef short short4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) short4_t *lds_short4_t;
+
+constexpr int kGroupStage = 64;
+__device__ const uint4_t kGroupZeros[1] = {{0u, 0u, 0u, 0u}};  // what a load reads that has nothing to read
+
+template <int TYPE>
+struct ActOf;
+template <>
+struct ActOf<kTypeF16> {
+    typedef ActF16 type;
+};
+template <>
+struct ActOf<kTypeBF16> {
+    typedef ActBF16 type;
+};
+
+template <int TYPE>
+__device__ __forceinline__ float from_16bit(uint16_t v)
+{
+    if constexpr (TYPE == kTypeBF16) return __builtin_bit_cast(float, (uint32_t)v << 16);
+    else return (float)__builtin_bit_cast(_Float16, v);
+}
+
+__device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
+
+// The rows of group g; E: those behind the last group, E + 1: those ahead of the first.
+__device__ __forceinline__ void group_range(const int32_t *offsets, int E, int count, int g, int *begin, int *end)
+{
+    const int b = g <= E ? clamp_to(offsets[g], 0, count) : 0;
+    *begin = b;
+    *end = g == E ? count : clamp_to(offsets[g < E ? g + 1 : 0], b, count);
+}
+
+// Which row tile of which group this workgroup has.  Row tiles are numbered group by group; how many there are only the device knows, so the launch has as many
+// workgroups as there could be, and those past the last tile have none.  XCD x (workgroup mod 8) takes the x-th eighth of the (row tile, column tile)
+// pairs that there are, in order: neighbours read the same rows and weights through one L2.
+struct RowTile {
+    int group, row0, end;  // rows row0 .. min(end, row0 + tile) - 1
+    int col;               // column tile
+};
+template <int THREADS>
+__device__ __forceinline__ bool find_row_tile(const int32_t *offsets, int E, int groups, int count, int tile_rows, int cols, RowTile *found)
+{
+    constexpr int kWaves = THREADS / 64;
+    __shared__ int s[kWaves + 3];
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (groups + THREADS - 1) / THREADS;
+    int tiles = 0;
+    for (int i = 0; i < per; ++i) {
+        const int g = tid * per + i;
+        if (g < groups) {
+            int b, e;
+            group_range(offsets, E, count, g, &b, &e);
+            tiles += (e - b + tile_rows - 1) / tile_rows;
+        }
+    }
+    int upto = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int v = __shfl_up(upto, d, 64);
+        if (lane >= d) upto += v;
+    }
+    if (lane == 63) s[wave] = upto;
+    __syncthreads();
+    int before = 0, total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+        if (w < wave) before += s[w];
+        total += s[w];
+    }
+    const long long pairs = (long long)total * cols, eighth = (pairs + kPlaceXcds - 1) / kPlaceXcds;
+    const long long in = blockIdx.x / kPlaceXcds, id = (long long)(blockIdx.x % kPlaceXcds) * eighth + in;
+    if (in >= eighth || id >= pairs) return false;
+    const int tile = (int)(id / cols);
+    int at = before + upto - tiles;
+    if (tile >= at && tile < at + tiles)
+        for (int i = 0; i < per; ++i) {
+            const int g = tid * per + i;
+            if (g >= groups) break;
+            int b, e;
+            group_range(offsets, E, count, g, &b, &e);
+            const int n = (e - b + tile_rows - 1) / tile_rows;
+            if (tile < at + n) {
+                s[kWaves] = g;
+                s[kWaves + 1] = b + (tile - at) * tile_rows;
+                s[kWaves + 2] = e;
+                break;
+            }
+            at += n;
+        }
+    __syncthreads();
+    found->group = __builtin_amdgcn_readfirstlane(s[kWaves]);
+    found->row0 = __builtin_amdgcn_readfirstlane(s[kWaves + 1]);
+    found->end = __builtin_amdgcn_readfirstlane(s[kWaves + 2]);
+    found->col = (int)(id - (long long)tile * cols);
+    return true;
+}
+// At most so many row tiles.
+inline long long most_row_tiles(long long groups, long long count, int tile_rows)
+{
+    if (groups > count) groups = count;
+    return (count + groups * (tile_rows - 1)) / tile_rows;
+}
+
+__device__ __forceinline__ void load_to_lds(const uint8_t *from, uint8_t *to)
+{
+    __builtin_amdgcn_global_load_lds((global_ptr_t)from, (lds_ptr_t)to, 16, 0, 0);
+}
+
+// ---- tiles ----
+//
+// Each of WAVES waves asks for kLoads KiB of a stage (where there are fewer KiB than waves, some ask for the same one).
+
+template <int ROWS, int WAVES>
+struct AlongTile {
+    static constexpr int kBytes = ROWS * 128, kKibs = kBytes / 1024, kLoads = (kKibs + WAVES - 1) / WAVES;
+    static_assert(ROWS % 16 == 0 && (kKibs % WAVES == 0 || WAVES % kKibs == 0), "whole loads");
+    static __device__ __forceinline__ int kib(int wave, int i) { return (i * WAVES + wave) % kKibs; }
+    // The row of the tile that a lane brings in load i, and where in a row of the stage it reads: a piece of eight values.
+    static __device__ __forceinline__ int row(int wave, int lane, int i) { return kib(wave, i) * 8 + (lane >> 3); }
+    static __device__ __forceinline__ int piece(int lane) { return (lane & 7) ^ (lane >> 3); }
+    // Operand of rows first .. first + 15, values 32 step .. + 31 of the stage.
+    static __device__ __forceinline__ uint4_t read(const uint8_t *tile, int lane, int first, int step)
+    {
+        const int c = lane & 15, p = lane >> 4;
+        return *reinterpret_cast<const uint4_t *>(tile + (first + c) * 128 + ((step * 4 + p) ^ (c & 7)) * 16);
+    }
+};
+
+template <int SPAN, int WAVES>
+struct AcrossTile {
+    static constexpr int kBytes = SPAN * 128, kKibs = kBytes / 1024, kLoads = (kKibs + WAVES - 1) / WAVES, kPieces = SPAN / 8;
+    static_assert(SPAN % 64 == 0 && (kKibs % WAVES == 0 || WAVES % kKibs == 0), "whole loads");
+    static __device__ __forceinline__ int kib(int wave, int i) { return (i * WAVES + wave) % kKibs; }
+    static __device__ __forceinline__ int turn(int k) { return ((k & 3) | ((k >> 3) & 3) << 2) & (SPAN / 16 - 1); }
+    // The row of the stage (of its 64) that a lane brings in load i, and the eight columns that it reads of it.
+    static __device__ __forceinline__ int row(int wave, int lane, int i) { return (kib(wave, i) * 64 + lane) / kPieces; }
+    static __device__ __forceinline__ int column(int wave, int lane, int i)
+    {
+        const int q = lane % kPieces;
+        return ((((q >> 1) ^ turn(row(wave, lane, i))) << 1) | (q & 1)) * 8;
+    }
+    // Operand of columns first .. first + 15, rows 32 step .. + 31 of the stage.  A transposing read takes four rows of sixteen columns per sixteen lanes.
+    static __device__ __forceinline__ uint4_t read(const uint8_t *tile, int lane, int first, int step)
+    {
+        const int j = lane & 15, p = lane >> 4, k = step * 32 + p * 8 + (j >> 2);
+        const uint8_t *const at = tile + k * (SPAN * 2) + ((first >> 4) ^ turn(k)) * 32 + (j & 3) * 8;
+        union {
+            short4_t s[2];
+            uint4_t u;
+        } v;
+        v.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)at);
+        v.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(at + 4 * SPAN * 2));
+        return v.u;
+    }
+};
+
+// ---- the loop ----
+//
+// acc[i][j] = sum over the stages of P's operand i times Q's operand j: MFMAs of 16 x 16 x 32; the result's four values per lane are neighbours along P, its sixteen
+// columns are Q's.  fetch(stage, buffer, last): this wave's kLoads loads of a stage into a buffer; with last the stage may reach past the sum's end and brings zeros there.
+// DEPTH buffers; the last operands of a stage are in registers before the barrier after which its buffer is filled again, and multiplied behind it.
+// p_at, q_at: the wave's part of either tile.
+template <class Act, class PTile, class QTile, int PI, int QI, int DEPTH, class Fetch>
+__device__ __forceinline__ void group_product(float4_t (&acc)[PI][QI], uint8_t *lds, int p_at, int q_at, int stages, int whole, Fetch fetch)
+{
+    constexpr int kBuffer = PTile::kBytes + QTile::kBytes, kLoads = PTile::kLoads + QTile::kLoads;
+    static_assert((DEPTH - 1) * kLoads < 64, "what s_waitcnt counts");
+    const int lane = (int)threadIdx.x & 63;
+    uint4_t p[2][PI], q[2][QI];
+    auto read = [&](auto step, int buf) {
+        constexpr int kStep = decltype(step)::value;
+        const uint8_t *const tile = lds + buf * kBuffer;
+#pragma unroll
+        for (int i = 0; i < PI; ++i) p[kStep][i] = PTile::read(tile, lane, p_at + 16 * i, kStep);
+#pragma unroll
+        for (int j = 0; j < QI; ++j) q[kStep][j] = QTile::read(tile + PTile::kBytes, lane, q_at + 16 * j, kStep);
+    };
+    auto multiply = [&](auto step) {
+        constexpr int kStep = decltype(step)::value;
+#pragma unroll
+        for (int i = 0; i < PI; ++i)
+#pragma unroll
+            for (int j = 0; j < QI; ++j) acc[i][j] = Act::mfma(Act::x_operand(p[kStep][i]), Act::x_operand(q[kStep][j]), acc[i][j]);
+    };
+    // All but the `later` loads asked for last have arrived, for every wave, and every wave has its operands of the stage before.
+    auto arrive = [&](auto later) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(later)::value) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    constexpr std::integral_constant<int, 0> kFirst{};
+    constexpr std::integral_constant<int, 1> kSecond{};
+    constexpr std::integral_constant<int, kLoads *(DEPTH - 2)> kLater{};
+    constexpr std::integral_constant<int, kLoads *(DEPTH - 1)> kStart{};
+    constexpr std::integral_constant<int, 0> kNone{};
+
+#pragma unroll
+    for (int i = 0; i < PI; ++i)
+#pragma unroll
+        for (int j = 0; j < QI; ++j) acc[i][j] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    if (stages == 0) return;
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (d < stages) fetch(d, d, d >= whole);
+    if (stages >= DEPTH) arrive(kStart);
+    else arrive(kNone);
+    read(kFirst, 0);
+    int i = 0, buf = 0;
+    for (; i + DEPTH < whole; ++i) {
+        const int next = buf + 1 == DEPTH ? 0 : buf + 1;
+        read(kSecond, buf);
+        multiply(kFirst);
+        arrive(kLater);
+        fetch(i + DEPTH, buf, false);
+        read(kFirst, next);
+        multiply(kSecond);
+        buf = next;
+    }
+    for (; i < stages; ++i) {
+        const int next = buf + 1 == DEPTH ? 0 : buf + 1;
+        read(kSecond, buf);
+        multiply(kFirst);
+        if (i + 1 < stages) {
+            arrive(kNone);
+            if (i + DEPTH < stages) fetch(i + DEPTH, buf, i + DEPTH >= whole);
+            read(kFirst, next);
+        }
+        multiply(kSecond);
+        buf = next;
+    }
+}
+
+// Four FP32 results to a 16-bit type, 8 bytes.
+template <class Act>
+__device__ __forceinline__ uint2_t to_16bit4(float4_t v) { return (uint2_t){Act::pack2(v[0], v[1]), Act::pack2(v[2], v[3])}; }
+
+}  // namespace w4a16

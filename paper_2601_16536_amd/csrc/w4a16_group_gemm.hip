@@ -1,0 +1,145 @@
+// Y[i] = W_e X[r(i)] for ragged groups of rows: experts on 16-bit weights.
+#include "w4a16_group_device.h"
+#include <type_traits>
+
+namespace w4a16 {
+namespace {
+
+// TP columns of Y (rows of W, or its columns where it is transposed) by TQ rows, of PW x QW waves.
+template <int TYPE, bool ACROSS, bool GATHER, int TP, int TQ, int PW, int QW, int DEPTH, int PER_CU>
+__global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_gemm_kernel(GroupGemmArgs a, int groups, int cols)
+{
+    typedef typename ActOf<TYPE>::type Act;
+    constexpr int kWaves = PW * QW, PI = TP / PW / 16, QI = TQ / QW / 16;
+    typedef std::conditional_t<ACROSS, AcrossTile<TP, kWaves>, AlongTile<TP, kWaves>> PTile;
+    typedef AlongTile<TQ, kWaves> QTile;
+    constexpr int kBuffer = PTile::kBytes + QTile::kBytes;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    RowTile t;
+    if (!find_row_tile<64 * kWaves>(a.offsets, a.E, groups, a.count, TQ, cols, &t)) return;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int pw = wave / QW, qw = wave - pw * QW, c = lane & 15, p4 = (lane >> 4) * 4;
+    const int n0 = t.col * TP, rows = min(TQ, t.end - t.row0);
+    const size_t row_x = (size_t)a.ldx * 2, row_w = (size_t)a.ldw * 2;
+
+    // The lane's rows of X: 64-bit addresses where they are gathered, else offsets from the tile's first.  A row that there is not: zeros in the end.
+    const uint8_t *const x = static_cast<const uint8_t *>(a.X) + (GATHER ? 0 : (size_t)t.row0 * row_x);
+    const uint8_t *xp[GATHER ? QTile::kLoads : 1];
+    uint32_t xo[GATHER ? 1 : QTile::kLoads];
+#pragma unroll
+    for (int i = 0; i < QTile::kLoads; ++i) {
+        const int r = min(QTile::row(wave, lane, i), rows - 1), piece = QTile::piece(lane) * 16;
+        if constexpr (GATHER) {
+            const int from = a.rows[t.row0 + r] / a.top_k;
+            xp[i] = x + (size_t)clamp_to(from, 0, a.x_rows - 1) * row_x + piece;
+        } else {
+            xo[i] = (uint32_t)r * (uint32_t)row_x + (uint32_t)piece;
+        }
+    }
+    const bool product = t.group < a.E;
+    const uint8_t *const w = static_cast<const uint8_t *>(a.W) + (product ? (size_t)t.group * (size_t)a.stride_w * 2 : 0) + (ACROSS ? (size_t)n0 * 2 : (size_t)n0 * row_w);
+    uint32_t wo[PTile::kLoads];
+#pragma unroll
+    for (int i = 0; i < PTile::kLoads; ++i) {
+        if constexpr (ACROSS)  // columns past the last: those ahead of it again
+            wo[i] = (uint32_t)PTile::row(wave, lane, i) * (uint32_t)row_w + (uint32_t)min(PTile::column(wave, lane, i), a.N - 8 - n0) * 2u;
+        else wo[i] = (uint32_t)min(PTile::row(wave, lane, i), a.N - 1 - n0) * (uint32_t)row_w + (uint32_t)PTile::piece(lane) * 16u;
+    }
+    const uint8_t *const zeros = reinterpret_cast<const uint8_t *>(kGroupZeros);
+    auto fetch = [&](int stage, int buf, bool last) {
+        uint8_t *const to = lds + buf * kBuffer;
+        const int k0 = stage * kGroupStage;
+        const uint8_t *const wk = w + (ACROSS ? (size_t)k0 * row_w : (size_t)k0 * 2), *const xk = x + (size_t)k0 * 2;
+#pragma unroll
+        for (int i = 0; i < PTile::kLoads; ++i) {
+            const uint8_t *from = wk + wo[i];
+            if (last && k0 + (ACROSS ? PTile::row(wave, lane, i) : QTile::piece(lane) * 8) >= a.K) from = zeros;
+            load_to_lds(from, to + PTile::kib(wave, i) * 1024);
+        }
+#pragma unroll
+        for (int i = 0; i < QTile::kLoads; ++i) {
+            const uint8_t *from;
+            if constexpr (GATHER) from = xp[i] + (size_t)k0 * 2;
+            else from = xk + xo[i];
+            if (last && k0 + QTile::piece(lane) * 8 >= a.K) from = zeros;
+            load_to_lds(from, to + PTile::kBytes + QTile::kib(wave, i) * 1024);
+        }
+    };
+    float4_t acc[PI][QI];
+    group_product<Act, PTile, QTile, PI, QI, DEPTH>(acc, lds, pw * PI * 16, qw * QI * 16, product ? (a.K + kGroupStage - 1) / kGroupStage : 0, a.K / kGroupStage, fetch);
+
+    uint16_t *const y = static_cast<uint16_t *>(a.Y);
+#pragma unroll
+    for (int j = 0; j < QI; ++j) {
+        const int r = qw * QI * 16 + 16 * j + c;
+        if (r >= rows) continue;
+        bool there = true;
+        if constexpr (GATHER) {
+            const int from = a.rows[t.row0 + r];
+            there = from >= 0 && from / a.top_k < a.x_rows;
+        }
+        uint16_t *const to = y + (size_t)(t.row0 + r) * (size_t)a.ldy;
+#pragma unroll
+        for (int i = 0; i < PI; ++i) {
+            const int n = n0 + pw * PI * 16 + 16 * i + p4;
+            if (n < a.N) *reinterpret_cast<uint2_t *>(to + n) = there ? to_16bit4<Act>(acc[i][j]) : (uint2_t){0u, 0u};
+        }
+    }
+}
+
+template <int TP, int TQ, int PW, int QW, int DEPTH, int PER_CU>
+struct Form {
+    static constexpr int kRows = TQ, kCols = TP, kLds = DEPTH * (TP + TQ) * 128;
+    static_assert(kLds + 1024 <= 163840, "LDS of a compute unit");
+    template <int TYPE, bool ACROSS, bool GATHER>
+    static hipError_t go(const GroupGemmArgs &a, hipStream_t stream)
+    {
+        const auto kernel = &group_gemm_kernel<TYPE, ACROSS, GATHER, TP, TQ, PW, QW, DEPTH, PER_CU>;
+        if (kLds > 65536 - 1024) {
+            const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+            if (e != hipSuccess) return e;
+        }
+        const int groups = a.fill ? a.E + 2 : a.E, cols = (a.N + TP - 1) / TP;
+        const long long grid = (most_row_tiles(groups, a.count, TQ) * cols + kPlaceXcds - 1) / kPlaceXcds * kPlaceXcds;
+        if (grid * 64 * PW * QW > 0xFFFFFFFFll) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * PW * QW), kLds, stream, a, groups, cols);
+        return hipGetLastError();
+    }
+    static hipError_t launch(const GroupGemmArgs &a, hipStream_t stream)
+    {
+        auto typed = [&](auto type) {
+            constexpr int T = decltype(type)::value;
+            if (a.transposed) return a.rows ? go<T, true, true>(a, stream) : go<T, true, false>(a, stream);
+            return a.rows ? go<T, false, true>(a, stream) : go<T, false, false>(a, stream);
+        };
+        return a.type == kTypeBF16 ? typed(std::integral_constant<int, kTypeBF16>{}) : typed(std::integral_constant<int, kTypeF16>{});
+    }
+};
+
+template <class Use>
+auto with_form(int form, Use use)
+{
+    switch (form) {
+    case 0: return use(Form<128, 16, 4, 1, 4, 2>{});
+    case 1: return use(Form<128, 64, 4, 1, 3, 2>{});
+    default: return use(Form<128, 128, 2, 2, 2, 2>{});
+    }
+}
+
+}  // namespace
+
+GroupTile plan_group_gemm(int E, long long count, int N, int K, int transposed)
+{
+    (void)N, (void)K, (void)transposed;
+    const long long average = count / E;
+    const int form = average <= 24 ? 0 : average <= 64 ? 1 : 2;
+    return with_form(form, [&](auto f) { return GroupTile{form, f.kRows, f.kCols}; });
+}
+
+hipError_t launch_group_gemm(const GroupGemmArgs &a, hipStream_t stream)
+{
+    const GroupTile t = plan_group_gemm(a.E, a.count, a.N, a.K, a.transposed);
+    return with_form(t.form, [&](auto f) { return f.launch(a, stream); });
+}
+
+}  // namespace w4a16

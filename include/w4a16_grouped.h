@@ -5,7 +5,7 @@
  *
  * All data pointers are DEVICE pointers owned by the caller.  Matrices are FP16 or BF16 (`dtype`), their values contiguous along a
  * row; a leading dimension (ld) is the values from a row to the next.  Rows are 16-byte aligned, so dimensions along rows and ld are multiples
- * of 8 (at most 2^22).  ids, offsets, rows and FP32 arrays need no more than their type's alignment, workspaces 256 bytes.  Calls only enqueue
+ * of 8 (ld at most 2^21).  ids, offsets, rows and FP32 arrays need no more than their type's alignment, workspaces 256 bytes.  Calls only enqueue
  * work on `stream` (a hipStream_t, NULL = the default stream); none allocates, waits or keeps anything, so all may be captured into a HIP graph,
  * and calls on different streams may overlap, each with its own workspace and outputs.  No rows: W4A16_OK; nothing is launched
  * but what w4a16_grouped_gemm_grad and w4a16_lora_grad need to write their zeros, and w4a16_grouped_sort its offsets.

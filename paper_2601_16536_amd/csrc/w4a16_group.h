@@ -27,6 +27,18 @@ struct GroupTile {
 GroupTile plan_group_gemm(int E, long long count, int N, int K, int transposed);
 hipError_t launch_group_gemm(const GroupGemmArgs &a, hipStream_t stream);
 
+// Whole numbers 0 .. 2^31 - 1 divided by d: a multiplication by m = ceil(2^(31 + shift) / d), whose excess, below d, shows in no quotient since d <= 2^shift.
+struct Divisor {
+    uint32_t m, shift;
+    explicit Divisor(int d = 1)
+    {
+        shift = 0;
+        while ((1ll << shift) < d) ++shift;
+        m = (uint32_t)(((1ull << (31 + shift)) + (uint64_t)d - 1) / (uint64_t)d);
+    }
+    __host__ __device__ uint32_t operator()(int n) const { return (uint32_t)(((uint64_t)(uint32_t)n * m) >> (31 + shift)); }
+};
+
 struct GroupGradArgs {
     const void *dY, *X;
     void *dW;
@@ -35,6 +47,7 @@ struct GroupGradArgs {
     int x_rows, count;
     int top_k, E, N, K;
     int type, grad_type, accumulate;
+    Divisor divide{1};  // by top_k (set by launch_group_grad)
 };
 // w4a16_group_grad.hip
 GroupTile plan_group_grad(int E, long long count, int N, int K);

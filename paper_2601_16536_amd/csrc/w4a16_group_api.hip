@@ -10,7 +10,7 @@ bool aligned(const void *p, uintptr_t to) { return (reinterpret_cast<uintptr_t>(
 bool type_16bit(int dtype) { return dtype == W4A16_F16 || dtype == W4A16_BF16; }
 bool bad_width(long long n) { return n < 8 || n % 8 != 0; }
 
-constexpr long long kMaxCount = 1ll << 30, kMaxLd = 1ll << 22;  // 32-bit row numbers; 32-bit offsets inside a tile of 256 rows
+constexpr long long kMaxCount = 1ll << 30, kMaxLd = 1ll << 21;  // 32-bit row numbers; 32-bit offsets inside a tile of 256 rows
 constexpr int kMaxSum = 1 << 17, kMaxWidth = 1 << 20, kMaxLoraRows = 1 << 20;
 
 // A matrix of `rows` rows: SHAPE, ALIGN, UNSUPPORTED or OK.

@@ -56,11 +56,12 @@ struct RowTile {
     int group, row0, end;  // rows row0 .. min(end, row0 + tile) - 1
     int col;               // column tile
 };
+constexpr int kBlockRows = 4;
 template <int THREADS>
 __device__ __forceinline__ bool find_row_tile(const int32_t *offsets, int E, int groups, int count, int tile_rows, int cols, RowTile *found)
 {
     constexpr int kWaves = THREADS / 64;
-    __shared__ int s[kWaves + 3];
+    __shared__ int s[kWaves + 4];
     const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (groups + THREADS - 1) / THREADS;
     int tiles = 0;
     for (int i = 0; i < per; ++i) {
@@ -98,9 +99,14 @@ __device__ __forceinline__ bool find_row_tile(const int32_t *offsets, int E, int
             group_range(offsets, E, count, g, &b, &e);
             const int n = (e - b + tile_rows - 1) / tile_rows;
             if (tile < at + n) {
+                // In a group, kBlockRows row tiles at a time, column by column.
+                const long long in_group = id - (long long)at * cols;
+                const int block = (int)(in_group / ((long long)kBlockRows * cols)), high = min(kBlockRows, n - block * kBlockRows);
+                const int rest = (int)(in_group - (long long)block * kBlockRows * cols);
                 s[kWaves] = g;
-                s[kWaves + 1] = b + (tile - at) * tile_rows;
+                s[kWaves + 1] = b + (block * kBlockRows + rest % high) * tile_rows;
                 s[kWaves + 2] = e;
+                s[kWaves + 3] = rest / high;
                 break;
             }
             at += n;
@@ -109,7 +115,7 @@ __device__ __forceinline__ bool find_row_tile(const int32_t *offsets, int E, int
     found->group = __builtin_amdgcn_readfirstlane(s[kWaves]);
     found->row0 = __builtin_amdgcn_readfirstlane(s[kWaves + 1]);
     found->end = __builtin_amdgcn_readfirstlane(s[kWaves + 2]);
-    found->col = (int)(id - (long long)tile * cols);
+    found->col = __builtin_amdgcn_readfirstlane(s[kWaves + 3]);
     return true;
 }
 // At most so many row tiles.
@@ -124,6 +130,34 @@ __device__ __forceinline__ void load_to_lds(const uint8_t *from, uint8_t *to)
     __builtin_amdgcn_global_load_lds((global_ptr_t)from, (lds_ptr_t)to, 16, 0, 0);
 }
 
+// The same through a buffer that begins at `base`; an offset of kOutOfRange brings zeros.
+__device__ __forceinline__ void load_to_lds(const uint8_t *base, uint32_t offset, int uniform, uint8_t *to)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(base), 0, kOutOfRange - 1, kRawBuffer), (lds_ptr_t)to, 16, offset, uniform, 0, 0);
+}
+
+// The same, unseen by the compiler, for tiles that are read across: ahead of a transposing read of LDS it waits for every load to LDS that it knows of, those of later stages too.
+// No register is written, and whoever reads the bytes waits for them by count (arrive), as with the other form.  `bytes`: of the buffer; zeros past them.
+__device__ __forceinline__ void load_to_lds_unseen(const uint8_t *base, uint32_t bytes, uint32_t offset, int uniform, uint8_t *to)
+{
+    const uint64_t b = reinterpret_cast<uint64_t>(base);
+    const uint4_t r = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) & 0xFFFFu,
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), kRawBuffer};
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_ptr_t)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(offset), "s"(r), "s"(uniform) : "memory", "m0");
+}
+// The same for numbers of four bytes, one a lane.
+__device__ __forceinline__ void numbers_to_lds_unseen(const int32_t *base, uint32_t bytes, uint32_t offset, uint8_t *to)
+{
+    const uint64_t b = reinterpret_cast<uint64_t>(base);
+    const uint4_t r = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) & 0xFFFFu,
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), kRawBuffer};
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_ptr_t)to);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(r) : "memory", "m0");
+}
+// The bytes of `rows` rows of `width` bytes, `row` (at least 16) bytes apart, as far as 32 rows and 256 bytes can reach into them; 0 if there are none.
+__device__ __forceinline__ uint32_t bytes_of(int rows, int row, int width) { return (uint32_t)max((min(rows, 96) - 1) * row + width, 0); }
+
 // ---- tiles ----
 //
 // Each of WAVES waves asks for kLoads KiB of a stage (where there are fewer KiB than waves, some ask for the same one).
@@ -136,6 +170,18 @@ struct AlongTile {
     // The row of the tile that a lane brings in load i, and where in a row of the stage it reads: a piece of eight values.
     static __device__ __forceinline__ int row(int wave, int lane, int i) { return kib(wave, i) * 8 + (lane >> 3); }
     static __device__ __forceinline__ int piece(int lane) { return (lane & 7) ^ (lane >> 3); }
+    // Where a wave's lanes read: FRAGS operands of rows first + 16 i .. + 15, as offsets in LDS.
+    template <int FRAGS>
+    struct Part {
+        uint32_t at[2];
+        __device__ __forceinline__ Part(int lane, int first)
+        {
+            const int c = lane & 15, p = lane >> 4;
+#pragma unroll
+            for (int s = 0; s < 2; ++s) at[s] = (uint32_t)((first + c) * 128 + ((s * 4 + p) ^ (c & 7)) * 16);
+        }
+        __device__ __forceinline__ uint4_t read(const uint8_t *tile, int i, int step) const { return *reinterpret_cast<const uint4_t *>(tile + at[step] + i * 2048); }
+    };
     // Operand of rows first .. first + 15, values 32 step .. + 31 of the stage.
     static __device__ __forceinline__ uint4_t read(const uint8_t *tile, int lane, int first, int step)
     {
@@ -157,6 +203,27 @@ struct AcrossTile {
         const int q = lane % kPieces;
         return ((((q >> 1) ^ turn(row(wave, lane, i))) << 1) | (q & 1)) * 8;
     }
+    // As in an along tile; columns first + 16 i .. + 15.
+    template <int FRAGS>
+    struct Part {
+        uint32_t at[FRAGS];
+        __device__ __forceinline__ Part(int lane, int first)
+        {
+            const int j = lane & 15, k = (lane >> 4) * 8 + (j >> 2);
+#pragma unroll
+            for (int i = 0; i < FRAGS; ++i) at[i] = (uint32_t)(k * (SPAN * 2) + (((first >> 4) + i) ^ turn(k)) * 32 + (j & 3) * 8);
+        }
+        __device__ __forceinline__ uint4_t read(const uint8_t *tile, int i, int step) const
+        {
+            union {
+                short4_t s[2];
+                uint4_t u;
+            } v;
+            v.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(tile + at[i] + step * 32 * SPAN * 2));
+            v.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(tile + at[i] + (step * 32 + 4) * SPAN * 2));
+            return v.u;
+        }
+    };
     // Operand of columns first .. first + 15, rows 32 step .. + 31 of the stage.  A transposing read takes four rows of sixteen columns per sixteen lanes.
     static __device__ __forceinline__ uint4_t read(const uint8_t *tile, int lane, int first, int step)
     {
@@ -227,11 +294,15 @@ __device__ __forceinline__ void group_product(float4_t (&acc)[PI][QI], uint8_t *
     for (; i + DEPTH < whole; ++i) {
         const int next = buf + 1 == DEPTH ? 0 : buf + 1;
         read(kSecond, buf);
+        __builtin_amdgcn_sched_barrier(0);
         multiply(kFirst);
+        __builtin_amdgcn_sched_barrier(0);
         arrive(kLater);
         fetch(i + DEPTH, buf, false);
         read(kFirst, next);
+        __builtin_amdgcn_sched_barrier(0);
         multiply(kSecond);
+        __builtin_amdgcn_sched_barrier(0);
         buf = next;
     }
     for (; i < stages; ++i) {
@@ -246,6 +317,122 @@ __device__ __forceinline__ void group_product(float4_t (&acc)[PI][QI], uint8_t *
         multiply(kSecond);
         buf = next;
     }
+}
+
+// ---- the loop of the largest tiles ----
+//
+// 256 x 256 results, eight waves (two along P by four along Q), each with 64 rows of either half of P and 32 of either half of Q: acc[i][j], i < 4 in P's first
+// half, j < 2 in Q's.  A stage is multiplied in four phases, P0 Q0 | P0 Q1 | P1 Q1 | P1 Q0, ahead of each of which one half tile of 16 KiB goes to registers:
+//     number 4 i: P0 of stage i, 4 i + 1: Q1, 4 i + 2: P1, 4 i + 3: Q0 of stage i + 1 (-1: of stage 0)
+// in place of operands that are done with.  The four waves of P's second part run half a phase behind the others, so that on every SIMD one wave multiplies while the
+// other one reads.  LDS has eight half tiles; that of phase f is free once both have read it, and number f + 8 is asked for in phase f + 1: seven phases ahead of its use,
+// the last six on their way behind every wait.
+// fetch(kind, stage, to, last, steady): the loads of a half tile, kind = number mod 4; with last the stage may reach past the sum's end; steady (a type): in the middle of the loop.
+template <class Act, class Tile0, class Tile1, class Fetch>
+__device__ __forceinline__ void group_product_wide(float4_t (&acc)[8][4], uint8_t *lds, int pw, int qw, int stages, int whole, Fetch fetch)
+{
+    constexpr int kHalf = 16384, kLoads = 2;
+    static_assert(Tile0::kBytes == kHalf && Tile1::kBytes == kHalf && Tile0::kLoads == kLoads && Tile1::kLoads == kLoads, "half tiles");
+    const int lane = (int)threadIdx.x & 63, end = stages * 4 - 1;  // numbers up to end - 1
+    const bool late = pw != 0;
+    uint4_t p[2][4], q[2][2][2];  // [step][..]; [set][step][..]
+    typename Tile0::template Part<4> pp(lane, pw * 64);
+    typename Tile1::template Part<2> qp(lane, qw * 32);
+    auto place = [&](int number) { return lds + (((number & 3) == 3 ? number + 4 : number) & 7) * kHalf; };  // number mod 4 in the half of the stage's parity
+    auto read_p = [&](int number) {
+        const uint8_t *const tile = place(number);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) p[s][i] = pp.read(tile, i, s);
+    };
+    auto read_q = [&](int number, auto set) {
+        const uint8_t *const tile = place(number);
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) q[decltype(set)::value][s][j] = qp.read(tile, j, s);
+    };
+    auto multiply = [&](auto ph, auto qh, auto set) {
+        constexpr int a = decltype(ph)::value, b = decltype(qh)::value, t = decltype(set)::value;
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) acc[a * 4 + i][b * 2 + j] = Act::mfma(Act::x_operand(p[s][i]), Act::x_operand(q[t][s][j]), acc[a * 4 + i][b * 2 + j]);
+    };
+    auto arrive = [&](auto later) {  // all but the last `later` half tiles are there, for every wave, and every wave has read what it reads
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(later)::value * kLoads) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    constexpr std::integral_constant<int, 0> k0{};
+    constexpr std::integral_constant<int, 1> k1{};
+    constexpr std::integral_constant<int, 6> kLater{};
+    auto arrive_at = [&](int later) {
+        switch (later) {
+        case 1: return arrive(k1);
+        case 2: return arrive(std::integral_constant<int, 2>{});
+        case 3: return arrive(std::integral_constant<int, 3>{});
+        case 4: return arrive(std::integral_constant<int, 4>{});
+        case 5: return arrive(std::integral_constant<int, 5>{});
+        case 6: return arrive(kLater);
+        default: return arrive(k0);
+        }
+    };
+    auto stage_of = [](int number) { return (number + 1) >> 2; };  // (Q0 comes with the stage ahead)
+    auto ask = [&](int number) {  // where anything may be past the end
+        if (number < end) fetch(number & 3, stage_of(number), place(number), stage_of(number) >= whole, std::false_type{});
+    };
+
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    if (stages == 0) return;
+    for (int n = -1; n < 7; ++n) ask(n);
+    arrive_at(min(6, end - 1));
+    read_q(-1, k0);
+    arrive_at(min(6, end - 1));
+    if (late) __builtin_amdgcn_s_barrier();
+    // Stage i; set: the registers that have its Q0; parity of the stage as a constant where it is known.
+    auto stage = [&](int i, auto set, auto steady) {
+        constexpr bool kSteady = decltype(steady)::value;
+        constexpr int kSet = decltype(set)::value;
+        constexpr std::integral_constant<int, kSet> first{};
+        constexpr std::integral_constant<int, 1 - kSet> second{};
+        const int f = 4 * i;
+        auto phase = [&](auto read, auto mult, auto n) {  // what is read, what is multiplied
+            constexpr int k = decltype(n)::value;
+            if constexpr (kSteady) fetch((k + 7) & 3, i + ((k + 8) >> 2), place(4 * kSet + k + 7), false, std::true_type{});
+            else ask(f + k + 7);
+            if (kSteady || f + k < end) read();
+            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (kSteady) arrive(kLater);
+            else arrive_at(max(0, min(6, end - 2 - f - k)));
+            __builtin_amdgcn_s_setprio(1);
+            mult();
+            __builtin_amdgcn_s_setprio(0);
+            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+        phase([&] { read_p(4 * kSet); }, [&] { multiply(k0, k0, first); }, k0);
+        phase([&] { read_q(4 * kSet + 1, second); }, [&] { multiply(k0, k1, second); }, k1);
+        phase([&] { read_p(4 * kSet + 2); }, [&] { multiply(k1, k1, second); }, std::integral_constant<int, 2>{});
+        phase([&] { read_q(4 * kSet + 3, second); }, [&] { multiply(k1, k0, first); }, std::integral_constant<int, 3>{});
+    };
+    int i = 0;
+    for (; i + 3 < whole; i += 2) {
+        stage(i, k0, std::true_type{});
+        stage(i + 1, k1, std::true_type{});
+    }
+    for (; i < stages; i += 2) {
+        stage(i, k0, std::false_type{});
+        if (i + 1 < stages) stage(i + 1, k1, std::false_type{});
+    }
+    if (!late) __builtin_amdgcn_s_barrier();
 }
 
 // Four FP32 results to a 16-bit type, 8 bytes.

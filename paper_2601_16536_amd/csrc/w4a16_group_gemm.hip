@@ -87,6 +87,99 @@ __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_gemm_kernel(GroupG
     }
 }
 
+// 256 x 256, eight waves: the loop of half tiles.
+template <int TYPE, bool ACROSS, bool GATHER>
+__global__ __launch_bounds__(512, 1) void group_gemm_wide_kernel(GroupGemmArgs a, int groups, int cols)
+{
+    typedef typename ActOf<TYPE>::type Act;
+    typedef std::conditional_t<ACROSS, AcrossTile<128, 8>, AlongTile<128, 8>> PTile;
+    typedef AlongTile<128, 8> QTile;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    RowTile t;
+    if (!find_row_tile<512>(a.offsets, a.E, groups, a.count, 256, cols, &t)) return;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int pw = wave >> 2, qw = wave & 3, c = lane & 15, p4 = (lane >> 4) * 4;
+    const int n0 = t.col * 256, rows = min(256, t.end - t.row0);
+    const size_t row_x = (size_t)a.ldx * 2, row_w = (size_t)a.ldw * 2;
+    const uint8_t *const x = static_cast<const uint8_t *>(a.X) + (GATHER ? 0 : (size_t)t.row0 * row_x);
+    const bool product = t.group < a.E;
+    const uint8_t *const w = static_cast<const uint8_t *>(a.W) + (product ? (size_t)t.group * (size_t)a.stride_w * 2 : 0) + (ACROSS ? (size_t)n0 * 2 : (size_t)n0 * row_w);
+    uint32_t xo[4], wo[ACROSS ? 1 : 4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int half = (i >> 1) * 128, r = min(half + QTile::row(wave, lane, i & 1), rows - 1), piece = QTile::piece(lane) * 16;
+        xo[i] = (uint32_t)(GATHER ? clamp_to(a.rows[t.row0 + r] / a.top_k, 0, a.x_rows - 1) : r) * (uint32_t)row_x + (uint32_t)piece;
+        if constexpr (!ACROSS) wo[i] = (uint32_t)min(half + PTile::row(wave, lane, i & 1), a.N - 1 - n0) * (uint32_t)row_w + (uint32_t)PTile::piece(lane) * 16u;
+    }
+    // Across, the loads of a lane are whole rows and halves apart, and the buffer's end is where W_e's is: past a row's last column they bring what lies there, for columns that are not kept.
+    if constexpr (ACROSS) wo[0] = (uint32_t)PTile::row(wave, lane, 0) * (uint32_t)row_w + (uint32_t)PTile::column(wave, lane, 0) * 2u;
+    auto fetch = [&](int kind, int stage, uint8_t *to, bool last, auto) {
+        const int k0 = stage * kGroupStage;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const bool past = last && k0 + QTile::piece(lane) * 8 >= a.K;
+            uint8_t *const at = to + QTile::kib(wave, i) * 1024;
+            if (kind == 0 || kind == 2) {
+                if constexpr (ACROSS) {
+                    const int k = k0 + 32 * i, n = kind ? 128 : 0;
+                    load_to_lds_unseen(w + (size_t)k * row_w + 2 * n, bytes_of(a.K - k, (int)row_w, 2 * (a.N - n0 - n)), wo[0], 0, at);
+                } else {
+                    load_to_lds(w, past ? kOutOfRange : kind ? wo[2 + i] : wo[i], k0 * 2, at);
+                }
+            } else {
+                const uint32_t o = past ? kOutOfRange : kind == 1 ? xo[2 + i] : xo[i];
+                if constexpr (ACROSS) load_to_lds_unseen(x, kOutOfRange - 1, o, k0 * 2, at);
+                else load_to_lds(x, o, k0 * 2, at);
+            }
+        }
+    };
+    float4_t acc[8][4];
+    group_product_wide<Act, PTile, QTile>(acc, lds, pw, qw, product ? (a.K + kGroupStage - 1) / kGroupStage : 0, a.K / kGroupStage, fetch);
+
+    uint16_t *const y = static_cast<uint16_t *>(a.Y);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = (j >> 1) * 128 + qw * 32 + 16 * (j & 1) + c;
+        if (r >= rows) continue;
+        bool there = true;
+        if constexpr (GATHER) {
+            const int from = a.rows[t.row0 + r];
+            there = from >= 0 && from / a.top_k < a.x_rows;
+        }
+        uint16_t *const to = y + (size_t)(t.row0 + r) * (size_t)a.ldy;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int n = n0 + (i >> 2) * 128 + pw * 64 + 16 * (i & 3) + p4;
+            if (n < a.N) *reinterpret_cast<uint2_t *>(to + n) = there ? to_16bit4<Act>(acc[i][j]) : (uint2_t){0u, 0u};
+        }
+    }
+}
+
+struct Wide {
+    static constexpr int kRows = 256, kCols = 256, kLds = 131072;
+    template <int TYPE, bool ACROSS, bool GATHER>
+    static hipError_t go(const GroupGemmArgs &a, hipStream_t stream)
+    {
+        const auto kernel = &group_gemm_wide_kernel<TYPE, ACROSS, GATHER>;
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        if (e != hipSuccess) return e;
+        const int groups = a.fill ? a.E + 2 : a.E, cols = (a.N + kCols - 1) / kCols;
+        const long long grid = (most_row_tiles(groups, a.count, kRows) * cols + kPlaceXcds - 1) / kPlaceXcds * kPlaceXcds;
+        if (grid * 512 > 0xFFFFFFFFll) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), kLds, stream, a, groups, cols);
+        return hipGetLastError();
+    }
+    static hipError_t launch(const GroupGemmArgs &a, hipStream_t stream)
+    {
+        auto typed = [&](auto type) {
+            constexpr int T = decltype(type)::value;
+            if (a.transposed) return a.rows ? go<T, true, true>(a, stream) : go<T, true, false>(a, stream);
+            return a.rows ? go<T, false, true>(a, stream) : go<T, false, false>(a, stream);
+        };
+        return a.type == kTypeBF16 ? typed(std::integral_constant<int, kTypeBF16>{}) : typed(std::integral_constant<int, kTypeF16>{});
+    }
+};
+
 template <int TP, int TQ, int PW, int QW, int DEPTH, int PER_CU>
 struct Form {
     static constexpr int kRows = TQ, kCols = TP, kLds = DEPTH * (TP + TQ) * 128;
@@ -122,7 +215,8 @@ auto with_form(int form, Use use)
     switch (form) {
     case 0: return use(Form<128, 16, 4, 1, 4, 2>{});
     case 1: return use(Form<128, 64, 4, 1, 3, 2>{});
-    default: return use(Form<128, 128, 2, 2, 2, 2>{});
+    case 2: return use(Form<128, 128, 2, 2, 2, 2>{});
+    default: return use(Wide{});
     }
 }
 
@@ -130,15 +224,16 @@ auto with_form(int form, Use use)
 
 GroupTile plan_group_gemm(int E, long long count, int N, int K, int transposed)
 {
-    (void)N, (void)K, (void)transposed;
+    (void)K, (void)transposed;
     const long long average = count / E;
-    const int form = average <= 24 ? 0 : average <= 64 ? 1 : 2;
+    const int form = average <= 8 ? 0 : average <= 64 ? 1 : average < 160 || count * N < 128ll * 65536 ? 2 : 3;
     return with_form(form, [&](auto f) { return GroupTile{form, f.kRows, f.kCols}; });
 }
 
 hipError_t launch_group_gemm(const GroupGemmArgs &a, hipStream_t stream)
 {
-    const GroupTile t = plan_group_gemm(a.E, a.count, a.N, a.K, a.transposed);
+    GroupTile t = plan_group_gemm(a.E, a.count, a.N, a.K, a.transposed);
+    if (t.form == 3 && a.rows && (long long)a.x_rows * a.ldx * 2 >= (long long)(kOutOfRange - 1)) t.form = 2;  // (its gathered rows are at 32-bit offsets)
     return with_form(t.form, [&](auto f) { return f.launch(a, stream); });
 }
 

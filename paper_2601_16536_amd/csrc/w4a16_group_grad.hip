@@ -5,6 +5,25 @@
 namespace w4a16 {
 namespace {
 
+template <int TYPE, int GRAD_TYPE>
+__device__ __forceinline__ void store_grad(void *dW, size_t at, float4_t v, int accumulate)
+{
+    typedef typename ActOf<TYPE>::type Act;
+    if constexpr (GRAD_TYPE == kTypeF32) {
+        float4_t *const to = reinterpret_cast<float4_t *>(static_cast<float *>(dW) + at);
+        if (accumulate) v += *to;
+        *to = v;
+    } else {
+        uint2_t *const to = reinterpret_cast<uint2_t *>(static_cast<uint16_t *>(dW) + at);
+        if (accumulate) {
+            const uint2_t old = *to;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += from_16bit<TYPE>((uint16_t)(old[e >> 1] >> (16 * (e & 1))));
+        }
+        *to = to_16bit4<Act>(v);
+    }
+}
+
 // TP columns (of X) by TQ rows (columns of dY) of one dW_e.
 template <int TYPE, int GRAD_TYPE, bool GATHER, int TP, int TQ, int PW, int QW, int DEPTH, int PER_CU>
 __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_grad_kernel(GroupGradArgs a, int cols, int pairs)
@@ -69,23 +88,129 @@ __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_grad_kernel(GroupG
         for (int i = 0; i < PI; ++i) {
             const int k = k0 + pw * PI * 16 + 16 * i + p4;
             if (k >= a.K) continue;
-            float4_t v = acc[i][j];
-            if constexpr (GRAD_TYPE == kTypeF32) {
-                float4_t *const to = reinterpret_cast<float4_t *>(static_cast<float *>(a.dW) + at + k);
-                if (a.accumulate) v += *to;
-                *to = v;
-            } else {
-                uint2_t *const to = reinterpret_cast<uint2_t *>(static_cast<uint16_t *>(a.dW) + at + k);
-                if (a.accumulate) {
-                    const uint2_t old = *to;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] += from_16bit<TYPE>((uint16_t)(old[e >> 1] >> (16 * (e & 1))));
-                }
-                *to = to_16bit4<Act>(v);
-            }
+            store_grad<TYPE, GRAD_TYPE>(a.dW, at + k, acc[i][j], a.accumulate);
         }
     }
 }
+
+// 256 x 256, eight waves: the loop of half tiles.
+template <int TYPE, int GRAD_TYPE, bool GATHER>
+__global__ __launch_bounds__(512, 1) void group_grad_wide_kernel(GroupGradArgs a, int cols, int pairs)
+{
+    typedef typename ActOf<TYPE>::type Act;
+    typedef AcrossTile<128, 8> Tile;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int pw = wave >> 2, qw = wave & 3, c = lane & 15, p4 = (lane >> 4) * 4;
+    // An eighth of every group's tiles to an XCD, neighbours that read the same rows' columns: the groups' lengths differ.
+    const unsigned per = ((unsigned)pairs + kPlaceXcds - 1) / kPlaceXcds, in = blockIdx.x / kPlaceXcds;
+    const int group = (int)(in / per), pair = (int)(blockIdx.x % kPlaceXcds * per + in % per);
+    if (pair >= pairs) return;
+    int tn, tk;
+    {
+        const int high_all = pairs / cols, block = pair / (kBlockRows * cols), high = min(kBlockRows, high_all - block * kBlockRows), rest = pair - block * kBlockRows * cols;
+        tn = block * kBlockRows + rest % high;
+        tk = rest / high;
+    }
+    const int n0 = tn * 256, k0 = tk * 256;
+    int begin, end;
+    group_range(a.offsets, a.E, a.count, group, &begin, &end);
+    begin = __builtin_amdgcn_readfirstlane(begin);
+    const int rows = __builtin_amdgcn_readfirstlane(end) - begin;
+    const uint32_t row_x = (uint32_t)a.ldx * 2, row_y = (uint32_t)a.ldy * 2;
+    const uint8_t *const x = static_cast<const uint8_t *>(a.X) + (size_t)k0 * 2 + (GATHER ? 0 : (size_t)begin * row_x);
+    const uint8_t *const y = static_cast<const uint8_t *>(a.dY) + (size_t)n0 * 2 + (size_t)begin * row_y;
+    // The loads of a lane are whole rows and halves apart; the buffers' ends are the groups': past a row's last column they bring what lies there, for values that are not kept.
+    const int row = Tile::row(wave, lane, 0);
+    const uint32_t xo = (GATHER ? 0u : (uint32_t)row * row_x) + (uint32_t)Tile::column(wave, lane, 0) * 2u, yo = (uint32_t)row * row_y + (uint32_t)Tile::column(wave, lane, 0) * 2u;
+    // Gathered: the rows' numbers come to LDS two stages ahead of the loads that need them, 64 for each stage, of four stages; those of the first two stages as they are.
+    uint32_t xr[2];  // where the rows that X's halves are loaded from begin
+    int *const list = reinterpret_cast<int *>(lds + 131072);
+    auto ask_rows = [&](int stage) {
+        if (stage * kGroupStage < rows)
+            numbers_to_lds_unseen(a.rows + begin + stage * kGroupStage, (uint32_t)(rows - stage * kGroupStage) * 4u, (uint32_t)lane * 4u, reinterpret_cast<uint8_t *>(list + (stage & 3) * 64));
+    };
+    uint32_t start[2][2];  // xr of stages 0 and 1
+    auto place_of = [&](int source, int r) {
+        const uint32_t from = a.divide(source);
+        return (r < rows) & (source >= 0) & (from < (uint32_t)a.x_rows) ? from * row_x : kOutOfRange;
+    };
+    if (GATHER && rows > 0) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = s * kGroupStage + Tile::row(wave, lane, i);
+                start[s][i] = place_of(a.rows[begin + min(r, rows - 1)], r);
+            }
+    }
+    auto take_rows = [&](int stage, auto steady) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int in_stage = Tile::row(wave, lane, i);
+            xr[i] = place_of(list[(stage & 3) * 64 + in_stage], stage * kGroupStage + in_stage);
+            if (!decltype(steady)::value && stage < 2) xr[i] = stage ? start[1][i] : start[0][i];
+        }
+    };
+    const uint32_t x_bytes = (uint32_t)(a.x_rows - 1) * row_x + 2u * (uint32_t)(a.K - k0), x_bytes1 = x_bytes < 256u ? 0u : x_bytes - 256u;  // (gathered: X is below 2 GiB)
+    auto fetch = [&](int kind, int stage, uint8_t *to, bool, auto steady) {
+        const int r0 = stage * kGroupStage;
+        if (GATHER && kind == 0) take_rows(stage, steady);
+        if (GATHER && kind == 0) ask_rows(stage + 2);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int r = r0 + 32 * i;
+            uint8_t *const at = to + Tile::kib(wave, i) * 1024;
+            if (kind == 0 || kind == 2) {
+                const int k = kind ? 128 : 0;
+                if constexpr (GATHER) load_to_lds_unseen(x + 2 * k, kind ? x_bytes1 : x_bytes, xr[i] + xo, 0, at);
+                else load_to_lds_unseen(x + (size_t)r * row_x + 2 * k, bytes_of(rows - r, (int)row_x, 2 * (a.K - k0 - k)), xo, 0, at);
+            } else {
+                const int n = kind == 1 ? 128 : 0;
+                load_to_lds_unseen(y + (size_t)r * row_y + 2 * n, bytes_of(rows - r, (int)row_y, 2 * (a.N - n0 - n)), yo, 0, at);
+            }
+        }
+    };
+    float4_t acc[8][4];
+    group_product_wide<Act, Tile, Tile>(acc, lds, pw, qw, (rows + kGroupStage - 1) / kGroupStage, rows / kGroupStage, fetch);
+
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + (j >> 1) * 128 + qw * 32 + 16 * (j & 1) + c;
+        if (n >= a.N) continue;
+        const size_t at = ((size_t)group * (size_t)a.N + (size_t)n) * (size_t)a.K;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int k = k0 + (i >> 2) * 128 + pw * 64 + 16 * (i & 3) + p4;
+            if (k < a.K) store_grad<TYPE, GRAD_TYPE>(a.dW, at + k, acc[i][j], a.accumulate);
+        }
+    }
+}
+
+struct Wide {
+    static constexpr int kRows = 256, kCols = 256, kLds = 131072 + 1024;
+    template <int TYPE, int GRAD_TYPE, bool GATHER>
+    static hipError_t go(const GroupGradArgs &a, hipStream_t stream)
+    {
+        const auto kernel = &group_grad_wide_kernel<TYPE, GRAD_TYPE, GATHER>;
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
+        if (e != hipSuccess) return e;
+        const int cols = (a.K + kCols - 1) / kCols;
+        const long long pairs = (long long)((a.N + kRows - 1) / kRows) * cols, grid = (pairs + kPlaceXcds - 1) / kPlaceXcds * kPlaceXcds * a.E;
+        if (grid * 512 > 0xFFFFFFFFll) return hipErrorInvalidValue;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), kLds, stream, a, cols, (int)pairs);
+        return hipGetLastError();
+    }
+    static hipError_t launch(const GroupGradArgs &a, hipStream_t stream)
+    {
+        auto typed = [&](auto type) {
+            constexpr int T = decltype(type)::value;
+            if (a.grad_type == kTypeF32) return a.rows ? go<T, kTypeF32, true>(a, stream) : go<T, kTypeF32, false>(a, stream);
+            return a.rows ? go<T, T, true>(a, stream) : go<T, T, false>(a, stream);
+        };
+        return a.type == kTypeBF16 ? typed(std::integral_constant<int, kTypeBF16>{}) : typed(std::integral_constant<int, kTypeF16>{});
+    }
+};
 
 template <int TP, int TQ, int PW, int QW, int DEPTH, int PER_CU>
 struct Form {
@@ -119,7 +244,7 @@ struct Form {
 template <class Use>
 auto with_form(int form, Use use)
 {
-    (void)form;
+    if (form) return use(Wide{});
     return use(Form<128, 128, 2, 2, 2, 2>{});
 }
 
@@ -127,14 +252,16 @@ auto with_form(int form, Use use)
 
 GroupTile plan_group_grad(int E, long long count, int N, int K)
 {
-    (void)E, (void)count, (void)N, (void)K;
-    const int form = 0;
+    const int form = count / E >= 96 && (long long)E * N * K >= 128ll * 65536;
     return with_form(form, [&](auto f) { return GroupTile{form, f.kRows, f.kCols}; });
 }
 
-hipError_t launch_group_grad(const GroupGradArgs &a, hipStream_t stream)
+hipError_t launch_group_grad(const GroupGradArgs &args, hipStream_t stream)
 {
-    const GroupTile t = plan_group_grad(a.E, a.count, a.N, a.K);
+    GroupGradArgs a = args;
+    a.divide = Divisor(a.rows ? a.top_k : 1);
+    GroupTile t = plan_group_grad(a.E, a.count, a.N, a.K);
+    if (t.form && a.rows && (long long)a.x_rows * a.ldx * 2 >= (long long)(kOutOfRange - 1)) t.form = 0;  // (its gathered rows are at 32-bit offsets)
     return with_form(t.form, [&](auto f) { return f.launch(a, stream); });
 }
 

@@ -99,7 +99,7 @@ def test_argument_checks_need_no_gpu(grouped):
         assert g(**bad) == b.ERR_NULL, bad
     for bad in (dict(X=24), dict(W=24), dict(Y=24), dict(offsets=18), dict(rows=18), dict(ldx=68), dict(ldy=36), dict(ldw=68), dict(stride_w=64 * 32 + 4)):
         assert g(**bad) == b.ERR_ALIGN, bad
-    for bad in (dict(count=1 << 30, x_rows=1 << 30), dict(K=(1 << 17) + 8, ldx=1 << 18, ldw=1 << 18), dict(N=(1 << 20) + 8, ldy=1 << 21), dict(ldx=(1 << 22) + 8), dict(ldy=1 << 23),
+    for bad in (dict(count=1 << 30, x_rows=1 << 30), dict(K=(1 << 17) + 8, ldx=1 << 18, ldw=1 << 18), dict(N=(1 << 20) + 8, ldy=1 << 21), dict(ldx=(1 << 21) + 8), dict(ldy=1 << 23),
                 dict(ldw=1 << 23)):
         assert g(**bad) == b.ERR_UNSUPPORTED, bad
     # dY, type, ldy, X, x_rows, ldx, rows, top_k, offsets, E, count, N, K, dW, grad type, accumulate, stream
@@ -258,6 +258,18 @@ def test_gemm_of_every_length(grouped, sizes, N, K, transposed):
 
 
 @gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("K", [8, 64, 120, 128, 192, 256, 328, 448, 520, 1032])
+def test_gemm_in_the_largest_tiles(grouped, K, transposed, gather, kind):
+    """From one stage of 64 values to seventeen, whole and not; rows and columns that end inside a tile."""
+    sizes, N = [300, 0, 257, 1, 700, 256, 2, 540], 4104
+    assert grouped.query_tile(len(sizes), sum(sizes) + 13, N, K, transposed) == (256, 256)
+    run_group_case(grouped, sizes, N, K, kind, transposed, gather, K, 5, 8, "K %d" % K)
+
+
+@gpu
 @pytest.mark.parametrize("transposed", [False, True])
 def test_gemm_of_views(grouped, transposed):
     """X, W and out with strides, and NaN in between."""
@@ -357,6 +369,27 @@ def test_gemm_grad_of_every_width(grouped, sizes, N, K):
     dY = big[:, 8:N + 8]
     ref, terms, n = go.gemm_grad(exact(dY), exact(X), offsets)
     compare(grouped.gemm_grad(dY, X, ints(offsets), dtype=torch.float32), ref, tolerance(torch.float32, ref, terms, n[:, None, None]), "N %d K %d" % (N, K))
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("grads", ["same", "float32"])
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("sizes", [[1, 63, 64, 65, 128, 500, 0, 129], [191, 192, 193, 0, 256, 257, 2, 3], [448, 320, 319, 321, 577, 640, 0, 8]])
+def test_gemm_grad_in_the_largest_tiles(grouped, sizes, gather, grads, kind):
+    import torch
+    N, K = 1032, 1544
+    assert grouped.query_tile(len(sizes), sum(sizes) + 14, N, K, grad=True) == (256, 256)
+    X, W, offsets, rows, top_k = group_case(grouped, sizes, 8, K, kind, False, gather, 41, 5, 9)
+    big = torch.full((offsets[-1] + 9, N + 24), math.nan, device="cuda", dtype=X.dtype)
+    dY = big[:, 16:N + 16]
+    dY[5:offsets[-1]] = values(generator(42), (sum(sizes), N), kind)
+    if rows is not None:
+        rows[[7, 300]] = [-1, 2 ** 31 - 1]
+    kw = {} if rows is None else {"rows": ints(rows), "top_k": top_k}
+    dtype = X.dtype if grads == "same" else torch.float32
+    ref, terms, n = go.gemm_grad(np.nan_to_num(exact(dY)), exact(X), offsets, rows, top_k)
+    compare(grouped.gemm_grad(dY, X, ints(offsets), dtype=dtype, **kw), ref, tolerance(dtype, ref, terms, n[:, None, None]), sizes)
 
 
 @gpu

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(512, 1) void group_grad_wide_kernel(GroupGradArgs a
     uint32_t start[2][2];  // xr of stages 0 and 1
     auto place_of = [&](int source, int r) {
         const uint32_t from = a.divide(source);
-        return (r < rows) & (source >= 0) & (from < (uint32_t)a.x_rows) ? from * row_x : kOutOfRange;
+        return ((r < rows) & (source >= 0) & (from < (uint32_t)a.x_rows)) ? from * row_x : kOutOfRange;
     };
     if (GATHER && rows > 0) {
 #pragma unroll

@@ -104,16 +104,26 @@ __global__ __launch_bounds__(kSortThreads) void sort_place_kernel(const int32_t 
     for (int e = tid; e < keys * kSortWaves; e += kSortThreads) mine[e] = 0;
     __syncthreads();
     if (!counts) {  // ahead of the chunk, and from it on
-        for (int i0 = 0; i0 < chunk0; i0 += kSortThreads) count_key(ahead, key_of(ids, i0 + tid, E), true);
-        for (int i0 = chunk0; i0 < count; i0 += kSortThreads) count_key(begin, i0 + tid < count ? key_of(ids, i0 + tid, E) : E, i0 + tid < count);
+        constexpr int kAtOnce = kChunk / kSortThreads * 2;  // loads on their way
+        for (int i0 = 0; i0 < count; i0 += kSortThreads * kAtOnce) {
+            int k[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int i = i0 + j * kSortThreads + tid;
+                k[j] = i < count ? key_of(ids, i, E) : -1;
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) count_key(i0 + j * kSortThreads < chunk0 ? ahead : begin, k[j], k[j] >= 0);
+        }
     }
     int key[kRun / 64];
 #pragma unroll
     for (int j = 0; j < kRun / 64; ++j) {
         const int i = run0 + j * 64 + lane;
         key[j] = i < count ? key_of(ids, i, E) : -1;
-        count_key(mine + wave * keys, key[j], key[j] >= 0);
     }
+#pragma unroll
+    for (int j = 0; j < kRun / 64; ++j) count_key(mine + wave * keys, key[j], key[j] >= 0);
     __syncthreads();
     if (!counts) {
         for (int e = tid; e < keys; e += kSortThreads) begin[e] += ahead[e];

@@ -1,7 +1,7 @@
 // Low-rank adapters of many requests beside a shared projection, and their gradients:
 //     H = s X A^T  [rows, R] (shrink),   out = Y + H B^T (expand);   backward G = s dY B (shrink), dX += G A (expand), dA = G^T X, dB = dY^T H (grads)
-// for the rows of every adapter.  R is at most 128, so all of it is moving X, Y and the adapters once; H and G are FP32, and what multiplies them does so in FP32
-// (MFMA 16 x 16 x 4), where no rounding and no range of 16 bits has to be thought about.
+// for the rows of every adapter.  R is at most 128, so all of it is moving X, Y and the adapters; the multiplications are few.  H and G are sums in FP32; into the second
+// products, which are 16-bit MFMAs, they go as sums of two or three 16-bit numbers: to 22 bits at least, but for the gradients in 16 bits, where it is 16.
 //
 // Rows of an adapter come in tiles of 16 (few rows) or 64.  Up to kFewRows rows a wave finds the tiles from the ids alone; beyond, the ids are sorted first.
 #include "w4a16_group_device.h"
@@ -84,10 +84,10 @@ __device__ __forceinline__ uint4_t load16(const uint16_t *p, bool have)
     return have ? v : (uint4_t){0u, 0u, 0u, 0u};
 }
 
-// ---- shrink: H[s][i][r] = scaling * sum over slice s of k of X[i, k] W[r, k] ----
+// ---- shrink of few rows: H[s][i][r] = scaling * sum over slice s of k of X[i, k] W[r, k] ----
 //
-// A wave has 16 rows and all of R, steps of 32 k.  TR = 16: four waves share the slice; TR = 64: each has rows of its own.  ACROSS: W is B [K, R] (K the sum's length here), brought
-// to LDS by the wave for itself and read across.  The MFMA's row operand is W, so that a lane has four neighbouring r.
+// A workgroup has 16 rows, a slice of k and all of R; its four waves take steps of 32 k in turn and their sums meet in LDS, in their order.  ACROSS: W is B [K, R] (K the
+// sum's length here), brought to LDS by a wave for itself and read across.  The MFMA's row operand is W, so that a lane has four neighbouring r.
 constexpr int kShrinkUnroll = 4;
 
 struct ShrinkArgs {
@@ -98,29 +98,28 @@ struct ShrinkArgs {
     int K, R, slice;  // slice: a multiple of 128
 };
 
-template <int TYPE, int RT, bool ACROSS, int TR>
-__global__ __launch_bounds__(256) void lora_shrink_kernel(Lists l, ShrinkArgs a)
+template <int TYPE, int RT, bool ACROSS>
+__global__ __launch_bounds__(256) void lora_few_shrink_kernel(Lists l, ShrinkArgs a)
 {
     typedef typename ActOf<TYPE>::type Act;
-    constexpr int kRp = 16 * RT, kWaves = 4;
+    constexpr int kRp = 16 * RT, kWaves = 4, TR = 16;
     __shared__ int rows[TR];
-    __shared__ __attribute__((aligned(16))) float4_t sums[TR == 16 ? (kWaves - 1) * RT * 64 : 1];
+    __shared__ __attribute__((aligned(16))) float4_t sums[(kWaves - 1) * RT * 64];
     __shared__ __attribute__((aligned(16))) uint16_t across[ACROSS ? kWaves * 32 * kRp : 8];
     int adapter, count;
     if (!adapter_tile<TR>(l, (int)blockIdx.x, rows, &adapter, &count) || adapter == l.L) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, p = lane >> 4;
-    const int row = (TR == 16 ? 0 : wave * 16) + c;
+    const int row = c;
     const uint16_t *const x = a.X + (size_t)rows[min(row, count - 1)] * (size_t)a.ldx;
     const uint16_t *const w = a.W + (size_t)adapter * (size_t)a.R * (size_t)a.K;
     const int k0 = (int)blockIdx.y * a.slice, k1 = min(a.K, k0 + a.slice);
-    constexpr int kStep = TR == 16 ? 32 * kWaves : 32;
+    constexpr int kStep = 32 * kWaves;
     uint16_t *const mine = across + (ACROSS ? wave * 32 * kRp : 0);
 
     float4_t acc[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[t] = (float4_t){0.f, 0.f, 0.f, 0.f};
-    if (TR == 16 || wave * 16 < count)
-        for (int k = k0 + (TR == 16 ? wave * 32 : 0); k < k1; k += kStep * kShrinkUnroll) {
+        for (int k = k0 + wave * 32; k < k1; k += kStep * kShrinkUnroll) {
             uint4_t xv[kShrinkUnroll], wv[kShrinkUnroll][RT];
 #pragma unroll
             for (int u = 0; u < kShrinkUnroll; ++u) {
@@ -162,7 +161,7 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lists l, ShrinkArgs a)
                 for (int t = 0; t < RT; ++t) acc[t] = Act::mfma(Act::x_operand(wv[u][t]), Act::x_operand(xv[u]), acc[t]);
             }
         }
-    if constexpr (TR == 16) {  // the waves' sums, in their order
+    {  // the waves' sums, in their order
         if (wave > 0)
 #pragma unroll
             for (int t = 0; t < RT; ++t) sums[((wave - 1) * RT + t) * 64 + lane] = acc[t];
@@ -180,20 +179,158 @@ __global__ __launch_bounds__(256) void lora_shrink_kernel(Lists l, ShrinkArgs a)
     for (int t = 0; t < RT; ++t) *reinterpret_cast<float4_t *>(h + 16 * t) = acc[t] * s;
 }
 
-// H[0] += H[1] + ... + H[slices - 1], in order.
-__global__ __launch_bounds__(256) void lora_sum_kernel(float4_t *__restrict__ h, long long n, int slices)
+// ---- shrink of many rows ----
+//
+// A workgroup has 64 rows, a slice of k and all of R, in stages of 64 k through LDS (w4a16_group_device.h); a wave 16 rows.  A launch of its own adds the slices' sums up, in their
+// order, scales them and, TERMS > 0, writes them as TERMS bfloat16 numbers, one behind the other, too, whose sum they are.  (The last slice's workgroup as the one that adds: 16 us more, M = 2048,
+// K = 8192, rank 64: it waits for memory three times one after the other.)
+struct ShrinkSide {
+    const uint16_t *X, *W;
+    float *partial;    // [slices][M][Rp]; the first one becomes H
+    uint16_t *terms;   // [M][TERMS Rp]
+    long long ldx;
+    int K, slices;
+};
+struct ShrinkArgsMany {
+    ShrinkSide side[2];  // X and A; dY and B, across
+    const float *scaling;
+    int R;
+};
+
+__device__ __forceinline__ float bf16_value(uint16_t v) { return __builtin_bit_cast(float, (uint32_t)v << 16); }
+__device__ __forceinline__ uint16_t bf16_down(float v) { return (uint16_t)(__builtin_bit_cast(uint32_t, v) >> 16); }
+__device__ __forceinline__ bool finite(float v) { return __builtin_fabsf(v) < __builtin_inff(); }
+// The nearest bfloat16; the largest one for finite numbers beyond it.
+__device__ __forceinline__ uint16_t bf16_near(float v)
 {
-    const long long i = (long long)blockIdx.x * 256 + threadIdx.x;
-    if (i >= n) return;
-    float4_t v = h[i];
-    for (int s = 1; s < slices; ++s) v += h[(long long)s * n + i];
-    h[i] = v;
+    const uint16_t n = to_16bit(v, 1);
+    return (n & 0x7FFFu) == 0x7F80u && finite(v) ? (uint16_t)(n - 1) : n;
+}
+// v as a sum of TERMS bfloat16 numbers, each the nearest to what the ones before leave: off by 2^(-8 TERMS) |v| at most.  What is not finite is itself and zeros.
+template <int TERMS>
+__device__ __forceinline__ void bf16_terms(float v, uint16_t (&terms)[TERMS])
+{
+    float rest = v;
+#pragma unroll
+    for (int n = 0; n < TERMS; ++n) {
+        terms[n] = bf16_near(rest);
+        rest = finite(v) ? rest - bf16_value(terms[n]) : 0.f;
+    }
+}
+
+template <int TYPE, int RT, bool ACROSS, bool UNSEEN>
+__device__ __forceinline__ void shrink_side(const Lists &l, const ShrinkSide &a, const ShrinkArgsMany &all, uint8_t *lds, const int *rows, int adapter, int count)
+{
+    typedef typename ActOf<TYPE>::type Act;
+    constexpr int kRp = 16 * RT, kWaves = 4, kDepth = RT == 8 ? 3 : 4;
+    typedef std::conditional_t<ACROSS, AcrossTile<kRp, kWaves>, AlongTile<kRp, kWaves>> PTile;
+    typedef AlongTile<kTileRows, kWaves> QTile;
+    constexpr int kBuffer = PTile::kBytes + QTile::kBytes;
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, p4 = (lane >> 4) * 4;
+    const int R = all.R, slice = (int)blockIdx.x;
+    if (slice >= a.slices) return;
+    // The stages of k are dealt out to the slices one by one: neighbours in memory are read at about the same time.
+    const int k0 = slice * kGroupStage, next_k = a.slices * kGroupStage, stages = ((a.K + kGroupStage - 1) / kGroupStage - slice + a.slices - 1) / a.slices, whole = (a.K / kGroupStage - slice + a.slices - 1) / a.slices;
+    const uint16_t *const w = a.W + (size_t)adapter * (size_t)R * (size_t)a.K;
+    const uint8_t *x[QTile::kLoads], *wp[PTile::kLoads];
+    const int piece = QTile::piece(lane) * 8;
+    // The whole stages in turn, beginning at another one in each tile: rows lie a power of two apart, and were all workgroups at the same k, few of the memory's channels would have all to do.
+    const int turned = whole ? (int)(blockIdx.y * 5u % (unsigned)whole) : 0;
+#pragma unroll
+    for (int i = 0; i < QTile::kLoads; ++i)
+        x[i] = reinterpret_cast<const uint8_t *>(a.X + (size_t)rows[min(QTile::row(wave, lane, i), count - 1)] * (size_t)a.ldx + (size_t)(k0 + turned * next_k + piece));
+    const uint8_t *const zeros = reinterpret_cast<const uint8_t *>(kGroupZeros);
+#pragma unroll
+    for (int i = 0; i < PTile::kLoads; ++i) {
+        if constexpr (ACROSS) wp[i] = PTile::column(wave, lane, i) < R ? reinterpret_cast<const uint8_t *>(w + (size_t)(k0 + turned * next_k + PTile::row(wave, lane, i)) * (size_t)R + (size_t)PTile::column(wave, lane, i)) : zeros;
+        else wp[i] = reinterpret_cast<const uint8_t *>(w + (size_t)min(PTile::row(wave, lane, i), R - 1) * (size_t)a.K + (size_t)(k0 + turned * next_k + piece));
+    }
+    auto bring = [&](const uint8_t *from, uint8_t *to) {
+        if constexpr (UNSEEN) load_to_lds_unseen(from, to);
+        else load_to_lds(from, to);
+    };
+    auto fetch = [&](int stage, int buf, bool last) {
+        uint8_t *const to = lds + buf * kBuffer;
+        const int k = k0 + stage * next_k;  // (of the last stage, if it is not whole; it is behind the others)
+        const int on = stage + 1 == whole ? (turned ? whole - turned + 1 : 1) : stage + 1 == whole - turned ? 1 - whole : 1;  // stages from this one to the next: past the whole ones to the first, and in the end to what is left
+#pragma unroll
+        for (int i = 0; i < PTile::kLoads; ++i) {
+            const bool past = last && k + (ACROSS ? PTile::row(wave, lane, i) : piece) >= a.K;
+            bring(past ? zeros : wp[i], to + PTile::kib(wave, i) * 1024);
+            if constexpr (ACROSS) wp[i] += PTile::column(wave, lane, i) < R ? (ptrdiff_t)on * next_k * R * 2 : 0;
+            else wp[i] += (ptrdiff_t)on * next_k * 2;
+        }
+#pragma unroll
+        for (int i = 0; i < QTile::kLoads; ++i) {
+            bring(last && k + piece >= a.K ? zeros : x[i], to + PTile::kBytes + QTile::kib(wave, i) * 1024);
+            x[i] += (ptrdiff_t)on * next_k * 2;
+        }
+    };
+    float4_t acc[RT][1];
+    group_product<Act, PTile, QTile, RT, 1, kDepth>(acc, lds, 0, wave * 16, stages, whole, fetch);
+
+    const int slot = wave * 16 + c;
+    if (slot >= count) return;
+    float *const to = a.partial + ((size_t)slice * (size_t)l.M + (size_t)rows[slot]) * kRp + p4;
+#pragma unroll
+    for (int t = 0; t < RT; ++t) *reinterpret_cast<float4_t *>(to + 16 * t) = acc[t][0];
+}
+
+// BOTH: side 1 too, by the grid's third dimension.
+template <int TYPE, int RT, bool BOTH>
+__global__ __launch_bounds__(256, 2) void lora_shrink_kernel(Lists l, ShrinkArgsMany a)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    __shared__ int rows[kTileRows];
+    int adapter, count;
+    if (!adapter_tile<kTileRows>(l, (int)blockIdx.y, rows, &adapter, &count) || adapter == l.L) return;
+    if constexpr (BOTH)
+        if (blockIdx.z == 1) return shrink_side<TYPE, RT, true, true>(l, a.side[1], a, lds, rows, adapter, count);
+    shrink_side<TYPE, RT, false, BOTH>(l, a.side[0], a, lds, rows, adapter, count);
+}
+
+// A thread four values of one row; rows without an adapter: what is there, for nobody.
+template <int RT, int TERMS>
+__global__ __launch_bounds__(256) void lora_sum_kernel(Lists l, ShrinkArgsMany a)
+{
+    constexpr int kRp = 16 * RT, kPer = kRp / 4;
+    const ShrinkSide s = a.side[TERMS > 0 ? blockIdx.z : 0];
+    const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / kPer;
+    const int r = (int)(i % kPer) * 4;
+    if (row >= l.M) return;
+    const size_t next = (size_t)l.M * kRp;
+    float *const h = s.partial + (size_t)row * kRp + r;
+    const int adapter = l.ids[row];
+    if (adapter < 0 || adapter >= l.L) return;
+    float4_t v = *reinterpret_cast<const float4_t *>(h);
+    int k = 1;
+    for (; k + 4 <= s.slices; k += 4) {
+        float4_t u[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const float4_t *>(h + (size_t)(k + j) * next);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v += u[j];
+    }
+    for (; k < s.slices; ++k) v += *reinterpret_cast<const float4_t *>(h + (size_t)k * next);
+    v = v * (a.scaling ? a.scaling[adapter] : 1.0f);
+    if (r >= a.R) v = (float4_t){0.f, 0.f, 0.f, 0.f};
+    *reinterpret_cast<float4_t *>(h) = v;
+    if constexpr (TERMS > 0) {
+        uint16_t t[4][TERMS];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) bf16_terms<TERMS>(v[e], t[e]);
+#pragma unroll
+        for (int n = 0; n < TERMS; ++n)
+            *reinterpret_cast<uint2_t *>(s.terms + (size_t)row * (TERMS * kRp) + n * kRp + r) = (uint2_t){(uint32_t)t[0][n] | (uint32_t)t[1][n] << 16, (uint32_t)t[2][n] | (uint32_t)t[3][n] << 16};
+    }
 }
 
 // ---- expand: out[i, n] = base[i, n] + sum over r of H[i][r] W[n, r] ----
 //
-// A wave has 128 columns and the tile's rows by sixteens.  Eight MFMA tiles t: their row m is column 8 m + t, so that a lane ends with 32 neighbouring columns of its
-// row.  ACROSS: W is A [R, N] (N the columns here).  Step e of group g multiplies r = 16 g + 4 (lane / 16) + e.
+// A wave has 128 columns and the tile's rows by sixteens.  Eight MFMA tiles t: their row m is column 8 (4 (m mod 4) + m / 4) + t, so that a lane ends with eight neighbouring
+// columns of its row, four times, and four lanes with 64 bytes of it.  ACROSS: W is A [R, N] (N the columns here): a lane loads eight rows of eight columns and
+// turns them by itself.  H goes in as the sum of three bfloat16 numbers (FP32's 24 bits) or of two FP16 numbers (22): a row of H is first scaled by a power of two, its largest
+// value to 2^13 .. 2^14, so that its smaller ones keep 2^-38 of that; the sums are scaled back.
 struct ExpandArgs {
     const uint16_t *W, *base;
     uint16_t *out;
@@ -202,183 +339,300 @@ struct ExpandArgs {
     int N, R, slices;
 };
 
-template <int TYPE, int RT, bool ACROSS, int TR>
-__global__ __launch_bounds__(256) void lora_expand_kernel(Lists l, ExpandArgs a)
+// Eight values as operands, term by term.
+template <int TYPE>
+struct ExpandTerms;
+template <>
+struct ExpandTerms<kTypeBF16> {
+    static constexpr int kTerms = 3;
+    static __device__ __forceinline__ void split(const float (&h)[8], uint4_t (&to)[3])
+    {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            uint16_t a[3], b[3];
+            bf16_terms<3>(h[e], a);
+            bf16_terms<3>(h[e + 1], b);
+#pragma unroll
+            for (int n = 0; n < 3; ++n) to[n][e / 2] = (uint32_t)a[n] | (uint32_t)b[n] << 16;
+        }
+    }
+};
+template <>
+struct ExpandTerms<kTypeF16> {
+    static constexpr int kTerms = 2;
+    static __device__ __forceinline__ void split(const float (&h)[8], uint4_t (&to)[2])
+    {
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const uint32_t up = ActF16::pack2(h[e], h[e + 1]);
+            to[0][e / 2] = up;
+            to[1][e / 2] = ActF16::pack2(finite(h[e]) ? h[e] - from_16bit<kTypeF16>((uint16_t)up) : 0.f, finite(h[e + 1]) ? h[e + 1] - from_16bit<kTypeF16>((uint16_t)(up >> 16)) : 0.f);
+        }
+    }
+};
+
+template <int TYPE, int G, int RP, bool ACROSS, int TR>
+__global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_kernel(Lists l, ExpandArgs a)
 {
     typedef typename ActOf<TYPE>::type Act;
-    constexpr int kRp = 16 * RT;
     __shared__ int rows[TR];
     int adapter, count;
-    if (!adapter_tile<TR>(l, (int)blockIdx.x, rows, &adapter, &count)) return;
+    if (!adapter_tile<TR>(l, (int)blockIdx.y, rows, &adapter, &count)) return;
     if (adapter == l.L && a.base == a.out) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, p = lane >> 4;
-    const int n0 = ((int)blockIdx.y * ((int)blockDim.x >> 6) + wave) * 128;
+    const int n0 = ((int)blockIdx.x * ((int)blockDim.x >> 6) + wave) * 128;
     if (n0 >= a.N) return;
+    const bool product = adapter < l.L;
 
-    uint16_t w[RT][4][8];  // [g][e][t]
-    if (adapter < l.L) {
+    uint4_t w[G][8];
+    if (product) {
         const uint16_t *const from = a.W + (size_t)adapter * (size_t)a.R * (size_t)a.N;
-        const int n = min(n0 + 8 * c, a.N - 8);
+        const int n = min(n0 + 8 * (4 * (c & 3) + (c >> 2)), a.N - 8);
 #pragma unroll
-        for (int g = 0; g < RT; ++g) {
-            const int r = 16 * g + 4 * p;
+        for (int g = 0; g < G; ++g) {
+            const int r = 32 * g + 8 * p;
             const bool have = r < a.R;
             if constexpr (ACROSS) {
+                uint4_t v[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const uint4_t v = load16(from + (size_t)(have ? r + e : 0) * (size_t)a.N + (size_t)n, have);
+                for (int e = 0; e < 8; ++e) v[e] = load16(from + (size_t)(have ? r + e : 0) * (size_t)a.N + (size_t)n, have);
 #pragma unroll
-                    for (int t = 0; t < 8; ++t) w[g][e][t] = (uint16_t)(v[t >> 1] >> (16 * (t & 1)));
-                }
+                for (int t = 0; t < 8; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[g][t][e] = __builtin_amdgcn_perm(v[2 * e + 1][t >> 1], v[2 * e][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
             } else {
 #pragma unroll
-                for (int t = 0; t < 8; ++t) {
-                    uint2_t v = *reinterpret_cast<const uint2_t *>(from + (size_t)(n + t) * (size_t)a.R + (size_t)(have ? r : 0));
-                    if (!have) v = (uint2_t){0u, 0u};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) w[g][e][t] = (uint16_t)(v[e >> 1] >> (16 * (e & 1)));
-                }
+                for (int t = 0; t < 8; ++t) w[g][t] = load16(from + (size_t)(n + t) * (size_t)a.R + (size_t)(have ? r : 0), have);
             }
         }
     }
+    // The rows' values of base come sixteen rows ahead.
+    auto load = [&](uint4_t (&to)[4], int m) {
+        const int row = rows[min(16 * m + c, count - 1)];
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            to[v] = *reinterpret_cast<const uint4_t *>(a.base ? a.base + (size_t)row * (size_t)a.ldbase + (size_t)min(n0 + 32 * v + 8 * p, a.N - 8) : reinterpret_cast<const uint16_t *>(kGroupZeros));
+    };
+    uint4_t ahead[4];
+    load(ahead, 0);
     for (int m = 0; m * 16 < count; ++m) {
         const bool mine = 16 * m + c < count;
         const int row = rows[min(16 * m + c, count - 1)];
-        float4_t acc[8];
+        uint4_t y[4];
 #pragma unroll
-        for (int t = 0; t < 8; ++t) acc[t] = (float4_t){0.f, 0.f, 0.f, 0.f};
-        if (adapter < l.L) {
+        for (int v = 0; v < 4; ++v) y[v] = ahead[v];
+        typedef ExpandTerms<TYPE> Terms;
+        uint4_t x[G][Terms::kTerms];
+        [[maybe_unused]] int up = 0;
+        if (product) {
+            float h[G][8];
 #pragma unroll
-            for (int g = 0; g < RT; ++g) {
-                const float *h = a.H + (size_t)row * kRp + 16 * g + 4 * p;
-                float4_t x = *reinterpret_cast<const float4_t *>(h);
-                for (int s = 1; s < a.slices; ++s) x += *reinterpret_cast<const float4_t *>(h + (size_t)s * (size_t)l.M * kRp);
-                if (16 * g + 4 * p >= a.R) x = (float4_t){0.f, 0.f, 0.f, 0.f};
+            for (int g = 0; g < G; ++g) {
+                const int r = 32 * g + 8 * p;
+                const float *from = a.H + (size_t)row * RP + (r < a.R ? r : 0);
+                float4_t h0 = *reinterpret_cast<const float4_t *>(from), h1 = *reinterpret_cast<const float4_t *>(from + 4);
+                for (int s = 1; s < a.slices; ++s) {
+                    from += (size_t)l.M * RP;
+                    h0 += *reinterpret_cast<const float4_t *>(from);
+                    h1 += *reinterpret_cast<const float4_t *>(from + 4);
+                }
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
+                for (int e = 0; e < 8; ++e) h[g][e] = r < a.R ? (e < 4 ? h0[e & 3] : h1[e & 3]) : 0.f;
+            }
+            if constexpr (TYPE == kTypeF16) {
+                float most = 0.f;
 #pragma unroll
-                    for (int t = 0; t < 8; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(from_16bit<TYPE>(w[g][e][t]), x[e], acc[t], 0, 0, 0);
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, __builtin_fabsf(h[g][e]));  // (a NaN is passed over: its row is NaN at any scale)
+                most = __builtin_fmaxf(most, __shfl_xor(most, 16, 64));
+                most = __builtin_fmaxf(most, __shfl_xor(most, 32, 64));
+                up = most > 0.f && finite(most) ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) h[g][e] = ldexpf(h[g][e], up);
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g) Terms::split(h[g], x[g]);
+        }
+        if ((m + 1) * 16 < count) load(ahead, m + 1);
+        if (product) {
+#pragma unroll
+            for (int half = 0; half < 8; half += 4) {  // (four tiles' sums at a time, for the registers)
+                float4_t acc[4];
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[t] = (float4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int g = 0; g < G; ++g)
+#pragma unroll
+                    for (int n = 0; n < Terms::kTerms; ++n)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) acc[t] = Act::mfma(Act::x_operand(w[g][half + t]), Act::x_operand(x[g][n]), acc[t]);
+#pragma unroll
+                for (int v = 0; v < 4; ++v)
+#pragma unroll
+                    for (int t = 0; t < 4; t += 2) {
+                        float y0 = acc[t][v], y1 = acc[t + 1][v];
+                        if constexpr (TYPE == kTypeF16) y0 = ldexpf(y0, -up), y1 = ldexpf(y1, -up);
+                        const uint32_t old = y[v][(half + t) >> 1];
+                        y[v][(half + t) >> 1] = Act::pack2(y0 + from_16bit<TYPE>((uint16_t)old), y1 + from_16bit<TYPE>((uint16_t)(old >> 16)));
+                    }
             }
         }
         if (!mine) continue;
-        const uint16_t *const base = a.base ? a.base + (size_t)row * (size_t)a.ldbase : nullptr;
         uint16_t *const out = a.out + (size_t)row * (size_t)a.ldo;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const int n = n0 + 32 * p + 8 * v;
-            if (n >= a.N) break;
-            uint4_t old = {0u, 0u, 0u, 0u};
-            if (base) old = *reinterpret_cast<const uint4_t *>(base + n);
-            if (adapter < l.L) {
-#pragma unroll
-                for (int t = 0; t < 8; t += 2)
-                    old[t >> 1] = Act::pack2(acc[t][v] + from_16bit<TYPE>((uint16_t)old[t >> 1]), acc[t + 1][v] + from_16bit<TYPE>((uint16_t)(old[t >> 1] >> 16)));
-            }
-            *reinterpret_cast<uint4_t *>(out + n) = old;
+            const int n = n0 + 32 * v + 8 * p;
+            if (n < a.N) *reinterpret_cast<uint4_t *>(out + n) = y[v];
         }
     }
 }
 
 // ---- grads: dA[r, k] = sum over the adapter's rows of G[i][r] X[i, k];  dB[n, r] = sum of dY[i, n] H[i][r] ----
 //
-// A workgroup has 128 columns (of X or dY) and 16 RU of r; its waves take four rows at a time in turn and meet in LDS.
-constexpr int kGradWaves = 8;
+// A workgroup has 128 columns of X or dY and all of R; a wave 32 columns.  Stages of 64 rows through LDS, both operands read across: 128 columns, and the terms of G or H one behind
+// the other, each multiplied into the same sums.  FP16 X enters as two bfloat16 numbers, whose sum it is exactly (eight and three bits), because G may be beyond FP16's range.
+// The rows' numbers come to LDS two stages ahead, as in w4a16_group_grad.hip.
+struct GradSide {
+    const uint16_t *X, *terms;
+    void *grad;
+    long long ldx;
+    int width, blocks;
+};
 struct GradArgs {
-    const uint16_t *X, *Y;
-    const float *H, *G;
-    void *dA, *dB;
+    GradSide side[2];  // X and G: dA; dY and H: dB
     const int32_t *offsets, *order;
-    long long ldx, ldy;
-    int R, K, N, M;
-    int blocks_a;  // workgroups of dA, per adapter
+    int R;
 };
 
-template <int TYPE, int GRAD_TYPE, int RU, int RP>
-__global__ __launch_bounds__(64 * kGradWaves) void lora_grads_kernel(GradArgs a)
+template <int TYPE, int GRAD_TYPE, int RT>
+struct GradShape {
+    static constexpr int kTerms = GRAD_TYPE == kTypeF32 ? 3 : 2, kSpan = 16 * RT * kTerms, kBuffer = (128 + kSpan) * 128;
+    static constexpr int kDepth = kBuffer * 3 <= 80 * 1024 - 2048 ? 3 : 2, kLds = kDepth * kBuffer + 4 * 256;
+    static_assert(kLds <= 163840 - 1024, "LDS of a compute unit");
+};
+
+template <int TYPE, int GRAD_TYPE, int RT>
+__global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
 {
     typedef typename ActOf<TYPE>::type Act;
-    extern __shared__ __attribute__((aligned(16))) float4_t red[];
-    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, p = lane >> 4;
-    const int adapter = (int)blockIdx.y, begin = a.offsets[adapter], count = a.offsets[adapter + 1] - begin;
-    const bool of_a = (int)blockIdx.x < a.blocks_a;
-    const int block = of_a ? (int)blockIdx.x : (int)blockIdx.x - a.blocks_a, chunks = (a.R + 16 * RU - 1) / (16 * RU);
-    const int n0 = block / chunks * 128, r0 = block % chunks * 16 * RU, width = of_a ? a.K : a.N;
-    const uint16_t *const x = (of_a ? a.X : a.Y) + min(n0 + 8 * c, width - 8);
-    const float *const h = (of_a ? a.G : a.H) + r0 + c;
-    const long long ld = of_a ? a.ldx : a.ldy;
+    typedef GradShape<TYPE, GRAD_TYPE, RT> Sh;
+    constexpr int kWaves = 4, kRp = 16 * RT, kTerms = Sh::kTerms, kDepth = Sh::kDepth, kParts = TYPE == kTypeF16 ? 2 : 1;
+    typedef AcrossTile<128, kWaves> PTile;
+    typedef AcrossTile<kRp, kWaves> QTile;  // of one term
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, p4 = (lane >> 4) * 4;
+    const bool of_a = (int)blockIdx.x < a.side[0].blocks;
+    const GradSide s = of_a ? a.side[0] : a.side[1];
+    const int adapter = (int)blockIdx.y, n0 = ((int)blockIdx.x - (of_a ? 0 : a.side[0].blocks)) * 128;
+    const int begin = __builtin_amdgcn_readfirstlane(a.offsets[adapter]), count = __builtin_amdgcn_readfirstlane(a.offsets[adapter + 1]) - begin;
+    const int stages = (count + kGroupStage - 1) / kGroupStage;
+    const size_t row_x = (size_t)s.ldx * 2;
+    const uint8_t *const zeros = reinterpret_cast<const uint8_t *>(kGroupZeros);
+    const uint8_t *const x = reinterpret_cast<const uint8_t *>(s.X), *const terms = reinterpret_cast<const uint8_t *>(s.terms);
+    int *const list = reinterpret_cast<int *>(lds + kDepth * Sh::kBuffer);
 
-    float4_t acc[8][RU];
+    float4_t acc[2][RT];  // [16 columns][16 of R]
 #pragma unroll
-    for (int t = 0; t < 8; ++t)
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int u = 0; u < RU; ++u) acc[t][u] = (float4_t){0.f, 0.f, 0.f, 0.f};
-    auto run = [&](auto for_a) {
-        for (int i0 = wave * 4; i0 < count; i0 += 4 * kGradWaves) {
-            const bool have = i0 + p < count;
-            const int row = a.order[begin + min(i0 + p, count - 1)];
-            const uint4_t v = load16(x + (size_t)row * (size_t)ld, have);
-            float g[RU];
+        for (int u = 0; u < RT; ++u) acc[i][u] = (float4_t){0.f, 0.f, 0.f, 0.f};
+    auto ask_rows = [&](int stage) {
+        if (stage < stages)
+            numbers_to_lds_unseen(a.order + begin + stage * kGroupStage, (uint32_t)(count - stage * kGroupStage) * 4u, (uint32_t)lane * 4u, reinterpret_cast<uint8_t *>(list + (stage & 3) * 64));
+    };
+    auto fetch = [&](int stage) {
+        uint8_t *const to = lds + stage % kDepth * Sh::kBuffer;
+        auto row_at = [&](int in_stage) { return stage * kGroupStage + in_stage < count ? list[(stage & 3) * 64 + in_stage] : -1; };
+        ask_rows(stage + 2);
 #pragma unroll
-            for (int u = 0; u < RU; ++u) {
-                g[u] = h[(size_t)row * RP + 16 * u];
-                if (!have) g[u] = 0.f;
-            }
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                const float xt = from_16bit<TYPE>((uint16_t)(v[t >> 1] >> (16 * (t & 1))));
-#pragma unroll
-                for (int u = 0; u < RU; ++u)
-                    acc[t][u] = decltype(for_a)::value ? __builtin_amdgcn_mfma_f32_16x16x4f32(xt, g[u], acc[t][u], 0, 0, 0)
-                                                       : __builtin_amdgcn_mfma_f32_16x16x4f32(g[u], xt, acc[t][u], 0, 0, 0);
-            }
+        for (int i = 0; i < PTile::kLoads; ++i) {
+            const int row = row_at(PTile::row(wave, lane, i));
+            load_to_lds_unseen(row >= 0 ? x + (size_t)row * row_x + (size_t)min(n0 + PTile::column(wave, lane, i), s.width - 8) * 2 : zeros, to + PTile::kib(wave, i) * 1024);
         }
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+            for (int i = 0; i < QTile::kLoads; ++i) {
+                const int row = row_at(QTile::row(wave, lane, i));
+                load_to_lds_unseen(row >= 0 ? terms + (size_t)row * (2 * kTerms * kRp) + (size_t)(t * kRp + QTile::column(wave, lane, i)) * 2 : zeros,
+                                   to + PTile::kBytes + t * QTile::kBytes + QTile::kib(wave, i) * 1024);
+            }
+    };
+    constexpr int kLoads = PTile::kLoads + kTerms * QTile::kLoads;
+    auto arrive = [&](auto later) {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(decltype(later)::value) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    constexpr std::integral_constant<int, 0> kNone{};
+    if (stages > 0) {
+        ask_rows(0);
+        ask_rows(1);
+        arrive(kNone);
+        for (int d = 0; d < kDepth - 1 && d < stages; ++d) {
+            fetch(d);
+            if (d + 2 < kDepth - 1) arrive(kNone);  // (its numbers)
+        }
+    }
+    auto run = [&](auto for_a) {
+    for (int i = 0; i < stages; ++i) {
+        if (kDepth == 3 && i + 1 < stages) arrive(std::integral_constant<int, kLoads>{});
+        else arrive(kNone);
+        if (i + kDepth - 1 < stages) fetch(i + kDepth - 1);
+        const uint8_t *const tile = lds + i % kDepth * Sh::kBuffer;
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+            uint4_t xv[kParts][2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const uint4_t v = PTile::read(tile, lane, wave * 32 + 16 * j, step);
+                if constexpr (TYPE == kTypeBF16) {
+                    xv[0][j] = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float f0 = from_16bit<TYPE>((uint16_t)v[e]), f1 = from_16bit<TYPE>((uint16_t)(v[e] >> 16));
+                        const float r0 = finite(f0) ? f0 - bf16_value(bf16_down(f0)) : 0.f, r1 = finite(f1) ? f1 - bf16_value(bf16_down(f1)) : 0.f;
+                        xv[0][j][e] = (uint32_t)bf16_down(f0) | (uint32_t)bf16_down(f1) << 16;
+                        xv[1][j][e] = (uint32_t)bf16_down(r0) | (uint32_t)bf16_down(r1) << 16;
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+                for (int u = 0; u < RT; ++u) {
+                    const uint4_t g = QTile::read(tile + PTile::kBytes + t * QTile::kBytes, lane, 16 * u, step);
+#pragma unroll
+                    for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j)
+                            acc[j][u] = decltype(for_a)::value ? ActBF16::mfma(ActBF16::x_operand(xv[part][j]), ActBF16::x_operand(g), acc[j][u])
+                                             : ActBF16::mfma(ActBF16::x_operand(g), ActBF16::x_operand(xv[part][j]), acc[j][u]);
+                }
+        }
+    }
     };
     if (of_a) run(std::true_type{});
     else run(std::false_type{});
-#pragma unroll
-    for (int half = kGradWaves / 2; half > 0; half >>= 1) {
-        if (wave >= half && wave < 2 * half)
-#pragma unroll
-            for (int t = 0; t < 8; ++t)
-#pragma unroll
-                for (int u = 0; u < RU; ++u) red[(((wave - half) * 8 + t) * RU + u) * 64 + lane] = acc[t][u];
-        __syncthreads();
-        if (wave < half)
-#pragma unroll
-            for (int t = 0; t < 8; ++t)
-#pragma unroll
-                for (int u = 0; u < RU; ++u) acc[t][u] += red[((wave * 8 + t) * RU + u) * 64 + lane];
-        __syncthreads();
-    }
-    if (wave > 0) return;
-    auto put = [&](void *to, size_t at, float4_t v) {
-        if constexpr (GRAD_TYPE == kTypeF32) *reinterpret_cast<float4_t *>(static_cast<float *>(to) + at) = v;
-        else *reinterpret_cast<uint2_t *>(static_cast<uint16_t *>(to) + at) = to_16bit4<Act>(v);
+    auto put = [&](size_t at, float4_t v) {
+        if constexpr (GRAD_TYPE == kTypeF32) *reinterpret_cast<float4_t *>(static_cast<float *>(s.grad) + at) = v;
+        else *reinterpret_cast<uint2_t *>(static_cast<uint16_t *>(s.grad) + at) = to_16bit4<Act>(v);
     };
-    if (of_a) {  // a lane has r = r0 + 16 u + c, columns n0 + 32 p + 8 v + t
 #pragma unroll
-        for (int u = 0; u < RU; ++u) {
-            const int r = r0 + 16 * u + c;
-            if (r >= a.R) continue;
+    for (int j = 0; j < 2; ++j)
 #pragma unroll
-            for (int v = 0; v < 4; ++v) {
-                const int k = n0 + 32 * p + 8 * v;
-                if (k >= a.K) break;
-                const size_t at = ((size_t)adapter * (size_t)a.R + (size_t)r) * (size_t)a.K + (size_t)k;
-                put(a.dA, at, (float4_t){acc[0][u][v], acc[1][u][v], acc[2][u][v], acc[3][u][v]});
-                put(a.dA, at + 4, (float4_t){acc[4][u][v], acc[5][u][v], acc[6][u][v], acc[7][u][v]});
+        for (int u = 0; u < RT; ++u) {
+            const int n = n0 + wave * 32 + 16 * j, r = 16 * u;
+            if (of_a) {  // dA [R, K]: r + c, columns n + p4 ..
+                if (r + c < a.R && n + p4 < s.width) put(((size_t)adapter * (size_t)a.R + (size_t)(r + c)) * (size_t)s.width + (size_t)(n + p4), acc[j][u]);
+            } else {  // dB [N, R]: column n + c, r + p4 ..
+                if (n + c < s.width && r + p4 < a.R) put(((size_t)adapter * (size_t)s.width + (size_t)(n + c)) * (size_t)a.R + (size_t)(r + p4), acc[j][u]);
             }
         }
-    } else {  // n = n0 + 8 c + t, r = r0 + 16 u + 4 p + v
-        if (n0 + 8 * c >= a.N) return;
-#pragma unroll
-        for (int t = 0; t < 8; ++t)
-#pragma unroll
-            for (int u = 0; u < RU; ++u) {
-                const int r = r0 + 16 * u + 4 * p;
-                if (r < a.R) put(a.dB, ((size_t)adapter * (size_t)a.N + (size_t)(n0 + 8 * c + t)) * (size_t)a.R + (size_t)r, acc[t][u]);
-            }
-    }
 }
 
 // ---- plans ----
@@ -399,79 +653,71 @@ hipError_t with_type(int type, Use use)
 {
     return type == kTypeBF16 ? use(std::integral_constant<int, kTypeBF16>{}) : use(std::integral_constant<int, kTypeF16>{});
 }
-
-// Rows of a tile: 64 where the adapters have that many on average.
-int tile_rows(int M, int L) { return M >= kTileRows && M / L >= 16 ? kTileRows : 16; }
-int slices_of(int M, int L, int K)
+template <class Kernel, class... Args>
+hipError_t enqueue(Kernel kernel, dim3 grid, int threads, int lds, hipStream_t stream, const Args &...args)
 {
-    const long long tiles = most_row_tiles(L + 1, M, tile_rows(M, L));
+    if (lds > 65536 - 1024) {
+        const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (e != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(kernel, grid, dim3((unsigned)threads), (unsigned)lds, stream, args...);
+    return hipGetLastError();
+}
+
+// Slices of K: about two workgroups to a compute unit, of 256 values at least.
+int slices_of(long long tiles, int K)
+{
     long long s = tiles ? 512 / tiles : 1;
     if (s > K / 256) s = K / 256;
     if (s > 32) s = 32;
     return s < 1 ? 1 : (int)s;
 }
+// Of many rows, where the slices of a tile run on different XCDs: eight or sixteen slices have each XCD read its share of the adapters only (M = 2048, K = 8192, rank 64, five adapters).
+int many_slices(long long tiles, int K)
+{
+    const int most = K / 512;
+    if (tiles <= 32 && most >= 16) return 16;
+    if (tiles <= 160 && most >= 8) return 8;
+    const long long s = tiles ? 512 / tiles : 1;
+    return s < 1 || most < 1 ? 1 : (int)(s < most ? s : most);
+}
 int slice_length(int K, int slices) { return ((K + slices - 1) / slices + 127) / 128 * 128; }
+long long few_tiles(int M, int L) { return most_row_tiles(L + 1, M, 16); }
+long long many_tiles(int M, int L) { return most_row_tiles(L + 1, M, kTileRows); }
 
 size_t whole(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
+// What a call has in its workspace, in bytes from its beginning.
 struct Space {
-    size_t offsets, order, sort, h, g, bytes;
+    size_t offsets, order, sort, h[2], terms[2], bytes;
+    int slices[2];
 };
-Space space_of(int M, int L, int R, int K, int N, bool grad)
+Space space_of(int M, int L, int R, int K, int N, bool grad, int grad_type)
 {
     Space s = {};
-    const bool sorted = grad || M > kFewRows;
-    s.order = whole((size_t)(L + 1) * 4);
-    s.sort = s.order + whole((size_t)M * 4);
-    s.h = sorted ? s.sort + whole(group_sort_workspace(M, L)) : 0;
-    const size_t row = (size_t)M * (size_t)padded(R) * 4;
-    s.g = s.h + whole(row * (size_t)slices_of(M, L, K));
-    s.bytes = grad ? s.g + whole(row * (size_t)slices_of(M, L, N)) : s.g;
+    const size_t row = (size_t)M * (size_t)padded(R);
+    if (!grad && M <= kFewRows) {
+        s.slices[0] = slices_of(few_tiles(M, L), K);
+        s.bytes = whole(row * 4 * (size_t)s.slices[0]);
+        return s;
+    }
+    const int sides = grad ? 2 : 1, n_terms = grad ? (grad_type == kTypeF32 ? 3 : 2) : 0;
+    const size_t tiles = (size_t)many_tiles(M, L);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t from = at;
+        at += whole(bytes);
+        return from;
+    };
+    s.offsets = take((size_t)(L + 1) * 4);
+    s.order = take((size_t)M * 4);
+    s.sort = take(group_sort_workspace(M, L));
+    for (int i = 0; i < sides; ++i) {
+        s.slices[i] = many_slices((long long)tiles * sides, i ? N : K);
+        s.h[i] = take(row * 4 * (size_t)s.slices[i]);
+        s.terms[i] = take(row * 2 * (size_t)n_terms);
+    }
+    s.bytes = at;
     return s;
-}
-
-// H for all rows that have an adapter.
-hipError_t shrink(const LoraArgs &a, const Lists &l, const void *X, long long ldx, const void *W, int K, bool across, float *H, bool sum, int *slices, hipStream_t stream)
-{
-    const int length = slice_length(K, slices_of(a.M, a.L, K));
-    *slices = (K + length - 1) / length;
-    const ShrinkArgs s = {static_cast<const uint16_t *>(X), static_cast<const uint16_t *>(W), H, a.scaling, ldx, K, a.R, length};
-    const int tr = tile_rows(a.M, a.L);
-    const dim3 grid((unsigned)most_row_tiles(a.L + 1, a.M, tr), (unsigned)*slices);
-    hipError_t e = with_type(a.type, [&](auto type) {
-        return with_rank(a.R, [&](auto rt) {
-            constexpr int T = decltype(type)::value, RT = decltype(rt)::value;
-            auto go = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, l, s);
-                return hipGetLastError();
-            };
-            if (across) return tr == 16 ? go(&lora_shrink_kernel<T, RT, true, 16>) : go(&lora_shrink_kernel<T, RT, true, kTileRows>);
-            return tr == 16 ? go(&lora_shrink_kernel<T, RT, false, 16>) : go(&lora_shrink_kernel<T, RT, false, kTileRows>);
-        });
-    });
-    if (e != hipSuccess || !sum || *slices == 1) return e;
-    const long long n = (long long)a.M * padded(a.R) / 4;
-    hipLaunchKernelGGL(lora_sum_kernel, dim3((unsigned)((n + 255) / 256)), dim3(256), 0, stream, reinterpret_cast<float4_t *>(H), n, *slices);
-    *slices = 1;
-    return hipGetLastError();
-}
-
-hipError_t expand(const LoraArgs &a, const Lists &l, const ExpandArgs &x, bool across, hipStream_t stream)
-{
-    const int tr = tile_rows(a.M, a.L);
-    const long long tiles = most_row_tiles(a.L + 1, a.M, tr);
-    const int blocks = (x.N + 127) / 128, waves = tiles * blocks >= 2048 ? 4 : 1;
-    const dim3 grid((unsigned)tiles, (unsigned)((blocks + waves - 1) / waves));
-    return with_type(a.type, [&](auto type) {
-        return with_rank(a.R, [&](auto rt) {
-            constexpr int T = decltype(type)::value, RT = decltype(rt)::value;
-            auto go = [&](auto kernel) {
-                hipLaunchKernelGGL(kernel, grid, dim3(64 * (unsigned)waves), 0, stream, l, x);
-                return hipGetLastError();
-            };
-            if (across) return tr == 16 ? go(&lora_expand_kernel<T, RT, true, 16>) : go(&lora_expand_kernel<T, RT, true, kTileRows>);
-            return tr == 16 ? go(&lora_expand_kernel<T, RT, false, 16>) : go(&lora_expand_kernel<T, RT, false, kTileRows>);
-        });
-    });
 }
 
 int key_bits(int L)
@@ -481,63 +727,109 @@ int key_bits(int L)
     return bits;
 }
 
+ShrinkSide side_of(const Space &s, uint8_t *ws, int i, const void *X, long long ldx, const void *W, int K)
+{
+    return {static_cast<const uint16_t *>(X), static_cast<const uint16_t *>(W), reinterpret_cast<float *>(ws + s.h[i]), reinterpret_cast<uint16_t *>(ws + s.terms[i]), ldx, K, s.slices[i]};
+}
+unsigned sum_blocks(int M, int R) { return (unsigned)(((long long)M * (padded(R) / 4) + 255) / 256); }
+
+template <int RT>
+constexpr int shrink_lds() { return (RT == 8 ? 3 : 4) * (16 * RT + kTileRows) * 128; }
+
+hipError_t expand(const LoraArgs &a, const Lists &l, const ExpandArgs &x, bool across, int tr, hipStream_t stream)
+{
+    const long long tiles = tr == 16 ? few_tiles(a.M, a.L) : many_tiles(a.M, a.L);
+    const int blocks = (x.N + 127) / 128, waves = tiles * blocks >= 2048 ? 4 : 1;
+    const dim3 grid((unsigned)((blocks + waves - 1) / waves), (unsigned)tiles);
+    return with_type(a.type, [&](auto type) {
+        return with_rank(a.R, [&](auto rt) {
+            constexpr int T = decltype(type)::value, RT = decltype(rt)::value, G = RT < 2 ? 1 : RT / 2, RP = 16 * RT;
+            if (tr == 16) return enqueue(&lora_expand_kernel<T, G, RP, false, 16>, grid, 64 * waves, 0, stream, l, x);
+            return across ? enqueue(&lora_expand_kernel<T, G, RP, true, kTileRows>, grid, 64 * waves, 0, stream, l, x)
+                          : enqueue(&lora_expand_kernel<T, G, RP, false, kTileRows>, grid, 64 * waves, 0, stream, l, x);
+        });
+    });
+}
+
 }  // namespace
 
-size_t lora_workspace(int M, int L, int R, int K, int N, bool grad) { return space_of(M, L, R, K, N, grad).bytes; }
+size_t lora_workspace(int M, int L, int R, int K, int N, bool grad)
+{
+    return space_of(M, L, R, K, N, grad, kTypeF32).bytes;
+}
 
 hipError_t launch_lora_add(const LoraArgs &a, hipStream_t stream)
 {
-    const Space s = space_of(a.M, a.L, a.R, a.K, a.N, false);
+    const Space s = space_of(a.M, a.L, a.R, a.K, a.N, false, 0);
     uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
     Lists l = {a.ids, nullptr, nullptr, a.M, a.L, key_bits(a.L)};
-    if (a.M > kFewRows) {
-        int32_t *const offsets = reinterpret_cast<int32_t *>(ws), *const order = reinterpret_cast<int32_t *>(ws + s.order);
-        const hipError_t e = launch_group_sort(a.ids, a.M, a.L, offsets, order, nullptr, ws + s.sort, stream);
-        if (e != hipSuccess) return e;
-        l.offsets = offsets;
-        l.order = order;
+    ExpandArgs x = {static_cast<const uint16_t *>(a.B), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), reinterpret_cast<float *>(ws + s.h[0]), a.ldbase, a.ldo,
+                    a.N, a.R, 1};
+    if (a.M <= kFewRows) {
+        const int length = slice_length(a.K, s.slices[0]);
+        x.slices = (a.K + length - 1) / length;
+        const ShrinkArgs f = {static_cast<const uint16_t *>(a.X), static_cast<const uint16_t *>(a.A), reinterpret_cast<float *>(ws), a.scaling, a.ldx, a.K, a.R, length};
+        const dim3 grid((unsigned)few_tiles(a.M, a.L), (unsigned)x.slices);
+        const hipError_t e = with_type(a.type, [&](auto type) {
+            return with_rank(a.R, [&](auto rt) { return enqueue(&lora_few_shrink_kernel<decltype(type)::value, decltype(rt)::value, false>, grid, 256, 0, stream, l, f); });
+        });
+        return e != hipSuccess ? e : expand(a, l, x, false, 16, stream);
     }
-    float *const H = reinterpret_cast<float *>(ws + s.h);
-    int slices;
-    const hipError_t e = shrink(a, l, a.X, a.ldx, a.A, a.K, false, H, a.M > kFewRows, &slices, stream);
+    const size_t tiles = (size_t)many_tiles(a.M, a.L);
+    int32_t *const offsets = reinterpret_cast<int32_t *>(ws + s.offsets), *const order = reinterpret_cast<int32_t *>(ws + s.order);
+    hipError_t e = launch_group_sort(a.ids, a.M, a.L, offsets, order, nullptr, ws + s.sort, stream);
     if (e != hipSuccess) return e;
-    const ExpandArgs x = {static_cast<const uint16_t *>(a.B), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), H, a.ldbase, a.ldo, a.N, a.R, slices};
-    return expand(a, l, x, false, stream);
+    l.offsets = offsets;
+    l.order = order;
+    ShrinkArgsMany m = {};
+    m.side[0] = side_of(s, ws, 0, a.X, a.ldx, a.A, a.K);
+    m.scaling = a.scaling, m.R = a.R;
+    const dim3 grid((unsigned)m.side[0].slices, (unsigned)tiles);
+    e = with_type(a.type, [&](auto type) {
+        return with_rank(a.R, [&](auto rt) {
+            constexpr int RT = decltype(rt)::value;
+            const hipError_t err = enqueue(&lora_shrink_kernel<decltype(type)::value, RT, false>, grid, 256, shrink_lds<RT>(), stream, l, m);
+            return err != hipSuccess ? err : enqueue(&lora_sum_kernel<RT, 0>, dim3(sum_blocks(a.M, a.R)), 256, 0, stream, l, m);
+        });
+    });
+    return e != hipSuccess ? e : expand(a, l, x, false, kTileRows, stream);
 }
 
 hipError_t launch_lora_grad(const LoraArgs &a, hipStream_t stream)
 {
-    const Space s = space_of(a.M, a.L, a.R, a.K, a.N, true);
+    const Space s = space_of(a.M, a.L, a.R, a.K, a.N, true, a.grad_type);
     uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
-    int32_t *const offsets = reinterpret_cast<int32_t *>(ws), *const order = reinterpret_cast<int32_t *>(ws + s.order);
+    const size_t tiles = (size_t)many_tiles(a.M, a.L);
+    int32_t *const offsets = reinterpret_cast<int32_t *>(ws + s.offsets), *const order = reinterpret_cast<int32_t *>(ws + s.order);
     hipError_t e = launch_group_sort(a.ids, a.M, a.L, offsets, order, nullptr, ws + s.sort, stream);
     if (e != hipSuccess) return e;
     const Lists l = {a.ids, offsets, order, a.M, a.L, key_bits(a.L)};
-    float *const H = reinterpret_cast<float *>(ws + s.h), *const G = reinterpret_cast<float *>(ws + s.g);
-    int slices;
-    if (a.M > 0) {
-        e = shrink(a, l, a.X, a.ldx, a.A, a.K, false, H, true, &slices, stream);
-        if (e == hipSuccess) e = shrink(a, l, a.Y, a.ldy, a.B, a.N, true, G, true, &slices, stream);
-        const ExpandArgs x = {static_cast<const uint16_t *>(a.A), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), G, a.ldbase, a.ldo, a.K, a.R, 1};
-        // dX may be written over: dA and dB read X and dY only
-        if (e == hipSuccess) e = expand(a, l, x, true, stream);
-        if (e != hipSuccess) return e;
-    }
+    ShrinkArgsMany m = {};
+    m.side[0] = side_of(s, ws, 0, a.X, a.ldx, a.A, a.K);
+    m.side[1] = side_of(s, ws, 1, a.Y, a.ldy, a.B, a.N);
+    m.scaling = a.scaling, m.R = a.R;
+    const int most = m.side[0].slices > m.side[1].slices ? m.side[0].slices : m.side[1].slices;
     return with_type(a.type, [&](auto type) {
         return with_rank(a.R, [&](auto rt) {
-            constexpr int T = decltype(type)::value, RT = decltype(rt)::value, RU = RT < 4 ? RT : 4;
-            auto go = [&](auto kernel) {
-                const int chunks = (a.R + 16 * RU - 1) / (16 * RU), blocks_a = (a.K + 127) / 128 * chunks, blocks_b = (a.N + 127) / 128 * chunks;
-                const GradArgs g = {static_cast<const uint16_t *>(a.X), static_cast<const uint16_t *>(a.Y), H, G, a.dA, a.dB, offsets, order, a.ldx, a.ldy, a.R, a.K, a.N, a.M, blocks_a};
-                constexpr int kLds = kGradWaves / 2 * 8 * RU * 1024;
-                if (kLds > 65536) {
-                    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
-                    if (err != hipSuccess) return err;
-                }
-                hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks_a + blocks_b), (unsigned)a.L), dim3(64 * kGradWaves), kLds, stream, g);
-                return hipGetLastError();
-            };
-            return a.grad_type == kTypeF32 ? go(&lora_grads_kernel<T, kTypeF32, RU, 16 * RT>) : go(&lora_grads_kernel<T, T, RU, 16 * RT>);
+            constexpr int T = decltype(type)::value, RT = decltype(rt)::value;
+            const bool wide = a.grad_type == kTypeF32;
+            hipError_t err = hipSuccess;
+            if (a.M > 0) {
+                const dim3 grid((unsigned)most, (unsigned)tiles, 2);
+                err = enqueue(&lora_shrink_kernel<T, RT, true>, grid, 256, shrink_lds<RT>(), stream, l, m);
+                const dim3 sums(sum_blocks(a.M, a.R), 1, 2);
+                if (err == hipSuccess) err = wide ? enqueue(&lora_sum_kernel<RT, 3>, sums, 256, 0, stream, l, m) : enqueue(&lora_sum_kernel<RT, 2>, sums, 256, 0, stream, l, m);
+                const ExpandArgs x = {static_cast<const uint16_t *>(a.A), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), m.side[1].partial, a.ldbase, a.ldo, a.K, a.R, 1};
+                if (err == hipSuccess) err = expand(a, l, x, true, kTileRows, stream);  // (dX may be written over: the last launch reads X and dY only)
+                if (err != hipSuccess) return err;
+            }
+            GradArgs g = {};
+            g.side[0] = {static_cast<const uint16_t *>(a.X), m.side[1].terms, a.dA, a.ldx, a.K, (a.K + 127) / 128};
+            g.side[1] = {static_cast<const uint16_t *>(a.Y), m.side[0].terms, a.dB, a.ldy, a.N, (a.N + 127) / 128};
+            g.offsets = offsets, g.order = order, g.R = a.R;
+            const dim3 grid((unsigned)(g.side[0].blocks + g.side[1].blocks), (unsigned)a.L);
+            return wide ? enqueue(&lora_grads_kernel<T, kTypeF32, RT>, grid, 256, GradShape<T, kTypeF32, RT>::kLds, stream, g)
+                        : enqueue(&lora_grads_kernel<T, T, RT>, grid, 256, GradShape<T, T, RT>::kLds, stream, g);
         });
     });
 }

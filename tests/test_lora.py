@@ -3,10 +3,12 @@
 Tolerances, per output, all bounds absolute, |.| of a matrix its values' magnitudes.  H = s X A^T: 16-bit products are exact in FP32; at most K / 32 + 32 roundings in a chain
 of matrix instructions, each of up to 32 products, and 36 where waves and slices of K meet, each below 2^-23 |s| |X| |A|^T; then the multiplication by s:
     dH = ((K / 32 + 68) 2^-23 + 2^-24) |s| |X| |A|^T,   dG the same with dY, B and N.
-H B^T is summed over R in FP32 products and additions, R + 8 roundings at most, each below 2^-23 |H| |B|^T, and what it is added to adds one more:
-    out: dH |B|^T + 2^-23 (R + 9) |H| |B|^T + 2^-23 |out|, then half a unit in the last place.
-dX the same with G and A.  dA = G^T X over n rows: n + 12 roundings (products, additions in four-row steps, eight waves):
-    dA: dG^T |X| + 2^-23 (n + 12) |G|^T |X|, dB with H and dY; then half a unit in the last place of a 16-bit type.
+H B^T is summed over R; a value of H goes in as two or three 16-bit numbers whose sum is off by 2^-22 |H| at most, so there are at most 3 R products and roundings below 2^-23 |H| |B|^T each,
+and what the sum is added to adds one more:
+    out: dH |B|^T + 2^-23 (3 R + 3) |H| |B|^T + 2^-23 |out|, then half a unit in the last place.
+dX the same with G and A.  dA = G^T X over n rows, a value of G as three bfloat16 numbers (two of eight bits each, off by 2^-16, for gradients in 16 bits), one of X as up to two: 6 n products
+and roundings below 2^-23 |G|^T |X|, one after the other at the worst:
+    dA: dG^T |X| + (2^-23 (6 n + 2) + 2^-16, or 2^-24 for FP32) |G|^T |X|, dB with H and dY; then half a unit in the last place of a 16-bit type.
 """
 import math
 import os
@@ -165,25 +167,26 @@ def expected_add(Y, X, A, B, ids, scaling):
         dh = ((K / 32 + 68) * 2.0 ** -23 + 2.0 ** -24) * terms
         b = np.abs(B[a]).T
         out[rows] += h @ B[a].T
-        bound[rows] = dh @ b + 2.0 ** -23 * ((R + 9) * (np.abs(h) @ b) + np.abs(out[rows]))
+        bound[rows] = dh @ b + 2.0 ** -23 * ((3 * R + 3) * (np.abs(h) @ b) + np.abs(out[rows]))
     return out, bound
 
 
-def expected_grad(dY, X, A, B, ids, scaling, dX):
+def expected_grad(dY, X, A, B, ids, scaling, dX, grads="float32"):
     L, R, K = A.shape
     N = B.shape[1]
     dX, ex = np.array(dX), np.zeros(dX.shape)
     dA, ea, dB, eb = np.zeros(A.shape), np.zeros(A.shape), np.zeros(B.shape), np.zeros(B.shape)
+    split = 2.0 ** -24 if grads == "float32" else 2.0 ** -16
     for a, rows, s in of_rows(ids, L, scaling):
         x, y, n = X[rows], dY[rows], len(rows)
         h, g = s * (x @ A[a].T), s * (y @ B[a])
         dh = ((K / 32 + 68) * 2.0 ** -23 + 2.0 ** -24) * abs(s) * (np.abs(x) @ np.abs(A[a]).T)
         dg = ((N / 32 + 68) * 2.0 ** -23 + 2.0 ** -24) * abs(s) * (np.abs(y) @ np.abs(B[a]))
         dX[rows] += g @ A[a]
-        ex[rows] = dg @ np.abs(A[a]) + 2.0 ** -23 * ((R + 9) * (np.abs(g) @ np.abs(A[a])) + np.abs(dX[rows]))
+        ex[rows] = dg @ np.abs(A[a]) + 2.0 ** -23 * ((3 * R + 3) * (np.abs(g) @ np.abs(A[a])) + np.abs(dX[rows]))
         dA[a], dB[a] = g.T @ x, y.T @ h
-        ea[a] = dg.T @ np.abs(x) + 2.0 ** -23 * (n + 12) * (np.abs(g).T @ np.abs(x))
-        eb[a] = np.abs(y).T @ dh + 2.0 ** -23 * (n + 12) * (np.abs(y).T @ np.abs(h))
+        ea[a] = dg.T @ np.abs(x) + (2.0 ** -23 * (6 * n + 2) + split) * (np.abs(g).T @ np.abs(x))
+        eb[a] = np.abs(y).T @ dh + (2.0 ** -23 * (6 * n + 2) + split) * (np.abs(y).T @ np.abs(h))
     return (dX, ex), (dA, ea), (dB, eb)
 
 
@@ -208,7 +211,7 @@ def check_grad(lora, M, L, R, K, N, kind, ids, grads="float32", seed=2, base=Tru
     dX = torch.randn(M, K, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)).to(X.dtype) if base else None
     dtype = torch.float32 if grads == "float32" else X.dtype
     got = lora.grad(dY, X, A, B, who, scaling, dX=dX, dtype=dtype)
-    want = expected_grad(exact(dY), exact(X), exact(A), exact(B), who, exact(scaling), exact(dX) if base else np.zeros((M, K)))
+    want = expected_grad(exact(dY), exact(X), exact(A), exact(B), who, exact(scaling), exact(dX) if base else np.zeros((M, K)), grads)
     assert got[0].dtype is X.dtype and got[1].dtype is dtype and got[2].dtype is dtype
     for g, (ref, bound), name in zip(got, want, ("dX", "dA", "dB")):
         compare(g, ref, bound, where + " " + name)

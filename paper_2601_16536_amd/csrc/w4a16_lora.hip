@@ -182,18 +182,20 @@ __global__ __launch_bounds__(256) void lora_few_shrink_kernel(Lists l, ShrinkArg
 // ---- shrink of many rows ----
 //
 // A workgroup has 64 rows, a slice of k and all of R, in stages of 64 k through LDS (w4a16_group_device.h); a wave 16 rows.  A launch of its own adds the slices' sums up, in their
-// order, scales them and, TERMS > 0, writes them as TERMS bfloat16 numbers, one behind the other, too, whose sum they are.  (The last slice's workgroup as the one that adds: 16 us more, M = 2048,
+// order, scales them and writes them as the 16-bit numbers whose sums they are, one behind the other.  (The last slice's workgroup as the one that adds: 16 us more, M = 2048,
 // K = 8192, rank 64: it waits for memory three times one after the other.)
 struct ShrinkSide {
     const uint16_t *X, *W;
-    float *partial;    // [slices][M][Rp]; the first one becomes H
-    uint16_t *terms;   // [M][TERMS Rp]
+    float *partial;    // [slices][M][Rp]
+    uint16_t *terms;   // of the gradients: [M][terms][Rp]
     long long ldx;
     int K, slices;
 };
 struct ShrinkArgsMany {
     ShrinkSide side[2];  // X and A; dY and B, across
     const float *scaling;
+    uint16_t *operand;   // of the expanding product: [M][terms][Rp]
+    int *up;             // FP16: the power of two that a row of it has been scaled by, [M]
     int R;
 };
 
@@ -276,6 +278,26 @@ __device__ __forceinline__ void shrink_side(const Lists &l, const ShrinkSide &a,
     for (int t = 0; t < RT; ++t) *reinterpret_cast<float4_t *>(to + 16 * t) = acc[t][0];
 }
 
+// What the expanding product takes of a value of H: three bfloat16 numbers, or two FP16 numbers of a value already scaled (below).
+template <int TYPE>
+struct ExpandTerms;
+template <>
+struct ExpandTerms<kTypeBF16> {
+    static constexpr int kTerms = 3;
+    static __device__ __forceinline__ void split(float h, uint16_t (&to)[3]) { bf16_terms<3>(h, to); }
+};
+template <>
+struct ExpandTerms<kTypeF16> {
+    static constexpr int kTerms = 2;
+    static __device__ __forceinline__ void split(float h, uint16_t (&to)[2])
+    {
+        to[0] = to_16bit(h, 0);
+        to[1] = to_16bit(finite(h) ? h - from_16bit<kTypeF16>(to[0]) : 0.f, 0);
+    }
+};
+// A row's power of two for FP16, from its largest value: that one to 2^13 .. 2^14.
+__device__ __forceinline__ int row_scale(float most) { return most > 0.f && finite(most) ? 14 - __builtin_amdgcn_frexp_expf(most) : 0; }
+
 // BOTH: side 1 too, by the grid's third dimension.
 template <int TYPE, int RT, bool BOTH>
 __global__ __launch_bounds__(256, 2) void lora_shrink_kernel(Lists l, ShrinkArgsMany a)
@@ -289,19 +311,21 @@ __global__ __launch_bounds__(256, 2) void lora_shrink_kernel(Lists l, ShrinkArgs
     shrink_side<TYPE, RT, false, BOTH>(l, a.side[0], a, lds, rows, adapter, count);
 }
 
-// A thread four values of one row; rows without an adapter: what is there, for nobody.
-template <int RT, int TERMS>
-__global__ __launch_bounds__(256) void lora_sum_kernel(Lists l, ShrinkArgsMany a)
+// A thread four values of one row; rows without an adapter: nothing.  GRAD: the terms for the gradients, of both sides by the grid's third dimension (0: of H; none of them for add), and
+// what `expanded`, the side that goes through the expanding product next, needs for that.
+template <int TYPE, int RT, int GRAD>
+__global__ __launch_bounds__(256) void lora_sum_kernel(Lists l, ShrinkArgsMany a, int expanded)
 {
+    typedef ExpandTerms<TYPE> Terms;
     constexpr int kRp = 16 * RT, kPer = kRp / 4;
-    const ShrinkSide s = a.side[TERMS > 0 ? blockIdx.z : 0];
+    const int which = GRAD > 0 ? (int)blockIdx.z : 0;
+    const ShrinkSide s = a.side[which];
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / kPer;
     const int r = (int)(i % kPer) * 4;
-    if (row >= l.M) return;
+    const int adapter = row < l.M ? l.ids[row] : -1;
+    if (adapter < 0 || adapter >= l.L) return;  // (a row's threads are in one wave: all of them go)
     const size_t next = (size_t)l.M * kRp;
-    float *const h = s.partial + (size_t)row * kRp + r;
-    const int adapter = l.ids[row];
-    if (adapter < 0 || adapter >= l.L) return;
+    const float *const h = s.partial + (size_t)row * kRp + r;
     float4_t v = *reinterpret_cast<const float4_t *>(h);
     int k = 1;
     for (; k + 4 <= s.slices; k += 4) {
@@ -314,178 +338,218 @@ __global__ __launch_bounds__(256) void lora_sum_kernel(Lists l, ShrinkArgsMany a
     for (; k < s.slices; ++k) v += *reinterpret_cast<const float4_t *>(h + (size_t)k * next);
     v = v * (a.scaling ? a.scaling[adapter] : 1.0f);
     if (r >= a.R) v = (float4_t){0.f, 0.f, 0.f, 0.f};
-    *reinterpret_cast<float4_t *>(h) = v;
-    if constexpr (TERMS > 0) {
-        uint16_t t[4][TERMS];
+    auto put = [&](uint16_t *to, const auto &t, int n) {
+        *reinterpret_cast<uint2_t *>(to + n * kRp + r) = (uint2_t){(uint32_t)t[0][n] | (uint32_t)t[1][n] << 16, (uint32_t)t[2][n] | (uint32_t)t[3][n] << 16};
+    };
+    if constexpr (GRAD > 0) {
+        uint16_t t[4][GRAD];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bf16_terms<TERMS>(v[e], t[e]);
+        for (int e = 0; e < 4; ++e) bf16_terms<GRAD>(v[e], t[e]);
 #pragma unroll
-        for (int n = 0; n < TERMS; ++n)
-            *reinterpret_cast<uint2_t *>(s.terms + (size_t)row * (TERMS * kRp) + n * kRp + r) = (uint2_t){(uint32_t)t[0][n] | (uint32_t)t[1][n] << 16, (uint32_t)t[2][n] | (uint32_t)t[3][n] << 16};
+        for (int n = 0; n < GRAD; ++n) put(s.terms + (size_t)row * (GRAD * kRp), t, n);
     }
+    if (which != expanded) return;
+    if constexpr (TYPE == kTypeF16) {
+        float most = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(v[0]), __builtin_fabsf(v[1])), __builtin_fmaxf(__builtin_fabsf(v[2]), __builtin_fabsf(v[3])));  // (a NaN is passed over: its row is NaN at any scale)
+#pragma unroll
+        for (int d = 1; d < kPer; d <<= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
+        const int up = row_scale(most);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], up);
+        if (r == 0) a.up[row] = up;
+    }
+    uint16_t t[4][Terms::kTerms];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) Terms::split(v[e], t[e]);
+#pragma unroll
+    for (int n = 0; n < Terms::kTerms; ++n) put(a.operand + (size_t)row * (Terms::kTerms * kRp), t, n);
 }
 
 // ---- expand: out[i, n] = base[i, n] + sum over r of H[i][r] W[n, r] ----
 //
-// A wave has 128 columns and the tile's rows by sixteens.  Eight MFMA tiles t: their row m is column 8 (4 (m mod 4) + m / 4) + t, so that a lane ends with eight neighbouring
-// columns of its row, four times, and four lanes with 64 bytes of it.  ACROSS: W is A [R, N] (N the columns here): a lane loads eight rows of eight columns and
+// A wave has 128 columns (64 from rank 72 on, for the registers) and the tile's rows by sixteens.  Eight (four) MFMA tiles t: their column c is column 8 c + t, so that a lane ends with eight
+// neighbouring columns of four rows, and sixteen lanes with 256 bytes of a row.  (With the columns as the MFMA's rows it is 64 bytes of sixteen rows: to read and write 2048 x 8192 so alone took 20 us.)  ACROSS: W is A [R, N] (N the columns here): a lane loads eight rows of eight columns and
 // turns them by itself.  H goes in as the sum of three bfloat16 numbers (FP32's 24 bits) or of two FP16 numbers (22): a row of H is first scaled by a power of two, its largest
 // value to 2^13 .. 2^14, so that its smaller ones keep 2^-38 of that; the sums are scaled back.
 struct ExpandArgs {
     const uint16_t *W, *base;
     uint16_t *out;
-    const float *H;
+    const float *H;           // few rows: [slices][M][Rp], else null
+    const uint16_t *operand;  // else: [M][terms][Rp]
+    const int *up;
     long long ldbase, ldo;
     int N, R, slices;
-};
-
-// Eight values as operands, term by term.
-template <int TYPE>
-struct ExpandTerms;
-template <>
-struct ExpandTerms<kTypeBF16> {
-    static constexpr int kTerms = 3;
-    static __device__ __forceinline__ void split(const float (&h)[8], uint4_t (&to)[3])
-    {
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            uint16_t a[3], b[3];
-            bf16_terms<3>(h[e], a);
-            bf16_terms<3>(h[e + 1], b);
-#pragma unroll
-            for (int n = 0; n < 3; ++n) to[n][e / 2] = (uint32_t)a[n] | (uint32_t)b[n] << 16;
-        }
-    }
-};
-template <>
-struct ExpandTerms<kTypeF16> {
-    static constexpr int kTerms = 2;
-    static __device__ __forceinline__ void split(const float (&h)[8], uint4_t (&to)[2])
-    {
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-            const uint32_t up = ActF16::pack2(h[e], h[e + 1]);
-            to[0][e / 2] = up;
-            to[1][e / 2] = ActF16::pack2(finite(h[e]) ? h[e] - from_16bit<kTypeF16>((uint16_t)up) : 0.f, finite(h[e + 1]) ? h[e + 1] - from_16bit<kTypeF16>((uint16_t)(up >> 16)) : 0.f);
-        }
-    }
 };
 
 template <int TYPE, int G, int RP, bool ACROSS, int TR>
 __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_kernel(Lists l, ExpandArgs a)
 {
     typedef typename ActOf<TYPE>::type Act;
+    constexpr int kTiles = G <= 2 ? 8 : 4;  // MFMA tiles of sixteen columns; a lane's neighbouring columns
+    typedef std::conditional_t<kTiles == 8, uint4_t, uint2_t> Piece;
     __shared__ int rows[TR];
     int adapter, count;
     if (!adapter_tile<TR>(l, (int)blockIdx.y, rows, &adapter, &count)) return;
     if (adapter == l.L && a.base == a.out) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, p = lane >> 4;
-    const int n0 = ((int)blockIdx.x * ((int)blockDim.x >> 6) + wave) * 128;
-    if (n0 >= a.N) return;
+    const int n0 = ((int)blockIdx.x * ((int)blockDim.x >> 6) + wave) * 16 * kTiles;
     const bool product = adapter < l.L;
+    typedef ExpandTerms<TYPE> Terms;
 
-    uint4_t w[G][8];
+    // Of many rows, the operands that H gives come to LDS, for all of the workgroup's waves: read by each of them from memory they are three times base's bytes.
+    constexpr int kPieces = Terms::kTerms * RP / 8, kRow = Terms::kTerms * RP * 2 + 16;  // of a row; its bytes in LDS, so that sixteen rows lie on all banks
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    if (TR != 16 && product) {
+        for (int i = (int)threadIdx.x; i < TR * kPieces; i += (int)blockDim.x) {
+            const int row = i / kPieces, piece = i % kPieces;
+            if (row < count) *reinterpret_cast<uint4_t *>(lds + row * kRow + piece * 16) = *reinterpret_cast<const uint4_t *>(a.operand + (size_t)rows[row] * (kPieces * 8) + piece * 8);
+        }
+        __syncthreads();
+    }
+    if (n0 >= a.N) return;
+
+    uint4_t w[G][kTiles];
     if (product) {
         const uint16_t *const from = a.W + (size_t)adapter * (size_t)a.R * (size_t)a.N;
-        const int n = min(n0 + 8 * (4 * (c & 3) + (c >> 2)), a.N - 8);
+        const int n = min(n0 + kTiles * c, a.N - kTiles);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
             const int r = 32 * g + 8 * p;
             const bool have = r < a.R;
             if constexpr (ACROSS) {
-                uint4_t v[8];
+                Piece v[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = load16(from + (size_t)(have ? r + e : 0) * (size_t)a.N + (size_t)n, have);
+                for (int e = 0; e < 8; ++e) {
+                    v[e] = *reinterpret_cast<const Piece *>(from + (size_t)(have ? r + e : 0) * (size_t)a.N + (size_t)n);
+                    if (!have) v[e] = (Piece)0u;
+                }
 #pragma unroll
-                for (int t = 0; t < 8; ++t)
+                for (int t = 0; t < kTiles; ++t)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[g][t][e] = __builtin_amdgcn_perm(v[2 * e + 1][t >> 1], v[2 * e][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
             } else {
 #pragma unroll
-                for (int t = 0; t < 8; ++t) w[g][t] = load16(from + (size_t)(n + t) * (size_t)a.R + (size_t)(have ? r : 0), have);
+                for (int t = 0; t < kTiles; ++t) w[g][t] = load16(from + (size_t)(n + t) * (size_t)a.R + (size_t)(have ? r : 0), have);
             }
         }
     }
     // The rows' values of base come sixteen rows ahead.
-    auto load = [&](uint4_t (&to)[4], int m) {
-        const int row = rows[min(16 * m + c, count - 1)];
-#pragma unroll
-        for (int v = 0; v < 4; ++v)
-            to[v] = *reinterpret_cast<const uint4_t *>(a.base ? a.base + (size_t)row * (size_t)a.ldbase + (size_t)min(n0 + 32 * v + 8 * p, a.N - 8) : reinterpret_cast<const uint16_t *>(kGroupZeros));
+    const int n = n0 + kTiles * c;
+    struct Rows {
+        Piece y[4];
+        int up;
     };
-    uint4_t ahead[4];
-    load(ahead, 0);
-    for (int m = 0; m * 16 < count; ++m) {
-        const bool mine = 16 * m + c < count;
-        const int row = rows[min(16 * m + c, count - 1)];
-        uint4_t y[4];
+    uint4_t x[G][Terms::kTerms];
+    auto load = [&](Rows &to, int m) {
 #pragma unroll
-        for (int v = 0; v < 4; ++v) y[v] = ahead[v];
-        typedef ExpandTerms<TYPE> Terms;
-        uint4_t x[G][Terms::kTerms];
-        [[maybe_unused]] int up = 0;
-        if (product) {
+        for (int v = 0; v < 4; ++v) {
+            const int row = rows[min(16 * m + 4 * p + v, count - 1)];
+            to.y[v] = *reinterpret_cast<const Piece *>(a.base ? a.base + (size_t)row * (size_t)a.ldbase + (size_t)min(n, a.N - kTiles) : reinterpret_cast<const uint16_t *>(kGroupZeros));
+        }
+        if (!product) return;
+        const int row = rows[min(16 * m + c, count - 1)];
+        if constexpr (TR != 16) {
+            if constexpr (TYPE == kTypeF16) to.up = a.up[row];
+        } else {  // few rows: the slices' sums meet here
             float h[G][8];
+            const size_t next = (size_t)l.M * RP;
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 const int r = 32 * g + 8 * p;
                 const float *from = a.H + (size_t)row * RP + (r < a.R ? r : 0);
                 float4_t h0 = *reinterpret_cast<const float4_t *>(from), h1 = *reinterpret_cast<const float4_t *>(from + 4);
-                for (int s = 1; s < a.slices; ++s) {
-                    from += (size_t)l.M * RP;
-                    h0 += *reinterpret_cast<const float4_t *>(from);
-                    h1 += *reinterpret_cast<const float4_t *>(from + 4);
+                for (int s = 1; s < a.slices; s += 4) {
+                    float4_t u[4][2];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float *const of = from + (size_t)min(s + j, a.slices - 1) * next;
+                        u[j][0] = *reinterpret_cast<const float4_t *>(of);
+                        u[j][1] = *reinterpret_cast<const float4_t *>(of + 4);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (s + j < a.slices) {
+                            h0 += u[j][0];
+                            h1 += u[j][1];
+                        }
                 }
 #pragma unroll
                 for (int e = 0; e < 8; ++e) h[g][e] = r < a.R ? (e < 4 ? h0[e & 3] : h1[e & 3]) : 0.f;
             }
+            to.up = 0;
             if constexpr (TYPE == kTypeF16) {
                 float most = 0.f;
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, __builtin_fabsf(h[g][e]));  // (a NaN is passed over: its row is NaN at any scale)
+                    for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, __builtin_fabsf(h[g][e]));
                 most = __builtin_fmaxf(most, __shfl_xor(most, 16, 64));
                 most = __builtin_fmaxf(most, __shfl_xor(most, 32, 64));
-                up = most > 0.f && finite(most) ? 14 - __builtin_amdgcn_frexp_expf(most) : 0;
+                to.up = row_scale(most);
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) h[g][e] = ldexpf(h[g][e], up);
+                    for (int e = 0; e < 8; ++e) h[g][e] = ldexpf(h[g][e], to.up);
             }
 #pragma unroll
-            for (int g = 0; g < G; ++g) Terms::split(h[g], x[g]);
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int e = 0; e < 8; e += 2) {
+                    uint16_t t0[Terms::kTerms], t1[Terms::kTerms];
+                    Terms::split(h[g][e], t0);
+                    Terms::split(h[g][e + 1], t1);
+#pragma unroll
+                    for (int i = 0; i < Terms::kTerms; ++i) x[g][i][e / 2] = (uint32_t)t0[i] | (uint32_t)t1[i] << 16;
+                }
         }
-        if ((m + 1) * 16 < count) load(ahead, m + 1);
+    };
+    Rows ahead;
+    load(ahead, 0);
+    for (int m = 0; m * 16 < count; ++m) {
+        Rows now = ahead;
+        Piece(&y)[4] = now.y;
+        if (TR != 16 && (m + 1) * 16 < count) load(ahead, m + 1);
+        if (TR != 16 && product) {
+            const uint8_t *const from = lds + min(16 * m + c, count - 1) * kRow;
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int i = 0; i < Terms::kTerms; ++i) {
+                    const bool have = 32 * g + 8 * p < RP;
+                    const uint4_t v = *reinterpret_cast<const uint4_t *>(from + i * RP * 2 + (have ? 64 * g + 16 * p : 0));
+                    x[g][i] = have ? v : (uint4_t){0u, 0u, 0u, 0u};
+                }
+        }
         if (product) {
 #pragma unroll
-            for (int half = 0; half < 8; half += 4) {  // (four tiles' sums at a time, for the registers)
+            for (int half = 0; half < kTiles; half += 4) {  // (four tiles' sums at a time, for the registers)
                 float4_t acc[4];
 #pragma unroll
                 for (int t = 0; t < 4; ++t) acc[t] = (float4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int n = 0; n < Terms::kTerms; ++n)
+                    for (int i = 0; i < Terms::kTerms; ++i)
 #pragma unroll
-                        for (int t = 0; t < 4; ++t) acc[t] = Act::mfma(Act::x_operand(w[g][half + t]), Act::x_operand(x[g][n]), acc[t]);
+                        for (int t = 0; t < 4; ++t) acc[t] = Act::mfma(Act::x_operand(x[g][i]), Act::x_operand(w[g][half + t]), acc[t]);
 #pragma unroll
-                for (int v = 0; v < 4; ++v)
+                for (int v = 0; v < 4; ++v) {
+                    [[maybe_unused]] int down = 0;
+                    if constexpr (TYPE == kTypeF16) down = -__shfl(now.up, 4 * p + v, 64);  // of the row that the lane has here
 #pragma unroll
                     for (int t = 0; t < 4; t += 2) {
                         float y0 = acc[t][v], y1 = acc[t + 1][v];
-                        if constexpr (TYPE == kTypeF16) y0 = ldexpf(y0, -up), y1 = ldexpf(y1, -up);
+                        if constexpr (TYPE == kTypeF16) y0 = ldexpf(y0, down), y1 = ldexpf(y1, down);
                         const uint32_t old = y[v][(half + t) >> 1];
                         y[v][(half + t) >> 1] = Act::pack2(y0 + from_16bit<TYPE>((uint16_t)old), y1 + from_16bit<TYPE>((uint16_t)(old >> 16)));
                     }
+                }
             }
         }
-        if (!mine) continue;
-        uint16_t *const out = a.out + (size_t)row * (size_t)a.ldo;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const int n = n0 + 32 * v + 8 * p;
-            if (n < a.N) *reinterpret_cast<uint4_t *>(out + n) = y[v];
+            const int i = 16 * m + 4 * p + v;
+            if (i < count && n < a.N) *reinterpret_cast<Piece *>(a.out + (size_t)rows[i] * (size_t)a.ldo + (size_t)n) = y[v];
         }
     }
 }
@@ -688,7 +752,7 @@ long long many_tiles(int M, int L) { return most_row_tiles(L + 1, M, kTileRows);
 size_t whole(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 // What a call has in its workspace, in bytes from its beginning.
 struct Space {
-    size_t offsets, order, sort, h[2], terms[2], bytes;
+    size_t offsets, order, sort, h[2], terms[2], operand, up, bytes;
     int slices[2];
 };
 Space space_of(int M, int L, int R, int K, int N, bool grad, int grad_type)
@@ -716,6 +780,8 @@ Space space_of(int M, int L, int R, int K, int N, bool grad, int grad_type)
         s.h[i] = take(row * 4 * (size_t)s.slices[i]);
         s.terms[i] = take(row * 2 * (size_t)n_terms);
     }
+    s.operand = take(row * 2 * 3);
+    s.up = take((size_t)M * 4);
     s.bytes = at;
     return s;
 }
@@ -739,14 +805,15 @@ constexpr int shrink_lds() { return (RT == 8 ? 3 : 4) * (16 * RT + kTileRows) * 
 hipError_t expand(const LoraArgs &a, const Lists &l, const ExpandArgs &x, bool across, int tr, hipStream_t stream)
 {
     const long long tiles = tr == 16 ? few_tiles(a.M, a.L) : many_tiles(a.M, a.L);
-    const int blocks = (x.N + 127) / 128, waves = tiles * blocks >= 2048 ? 4 : 1;
+    const int width = a.R <= 64 ? 128 : 64, blocks = (x.N + width - 1) / width, waves = tiles * blocks >= 2048 ? 4 : 1;
     const dim3 grid((unsigned)((blocks + waves - 1) / waves), (unsigned)tiles);
     return with_type(a.type, [&](auto type) {
         return with_rank(a.R, [&](auto rt) {
             constexpr int T = decltype(type)::value, RT = decltype(rt)::value, G = RT < 2 ? 1 : RT / 2, RP = 16 * RT;
+            constexpr int kLds = kTileRows * (ExpandTerms<T>::kTerms * RP * 2 + 16);
             if (tr == 16) return enqueue(&lora_expand_kernel<T, G, RP, false, 16>, grid, 64 * waves, 0, stream, l, x);
-            return across ? enqueue(&lora_expand_kernel<T, G, RP, true, kTileRows>, grid, 64 * waves, 0, stream, l, x)
-                          : enqueue(&lora_expand_kernel<T, G, RP, false, kTileRows>, grid, 64 * waves, 0, stream, l, x);
+            return across ? enqueue(&lora_expand_kernel<T, G, RP, true, kTileRows>, grid, 64 * waves, kLds, stream, l, x)
+                          : enqueue(&lora_expand_kernel<T, G, RP, false, kTileRows>, grid, 64 * waves, kLds, stream, l, x);
         });
     });
 }
@@ -763,11 +830,11 @@ hipError_t launch_lora_add(const LoraArgs &a, hipStream_t stream)
     const Space s = space_of(a.M, a.L, a.R, a.K, a.N, false, 0);
     uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
     Lists l = {a.ids, nullptr, nullptr, a.M, a.L, key_bits(a.L)};
-    ExpandArgs x = {static_cast<const uint16_t *>(a.B), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), reinterpret_cast<float *>(ws + s.h[0]), a.ldbase, a.ldo,
-                    a.N, a.R, 1};
+    ExpandArgs x = {static_cast<const uint16_t *>(a.B), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), nullptr, nullptr, nullptr, a.ldbase, a.ldo, a.N, a.R, 1};
     if (a.M <= kFewRows) {
         const int length = slice_length(a.K, s.slices[0]);
         x.slices = (a.K + length - 1) / length;
+        x.H = reinterpret_cast<const float *>(ws);
         const ShrinkArgs f = {static_cast<const uint16_t *>(a.X), static_cast<const uint16_t *>(a.A), reinterpret_cast<float *>(ws), a.scaling, a.ldx, a.K, a.R, length};
         const dim3 grid((unsigned)few_tiles(a.M, a.L), (unsigned)x.slices);
         const hipError_t e = with_type(a.type, [&](auto type) {
@@ -784,12 +851,14 @@ hipError_t launch_lora_add(const LoraArgs &a, hipStream_t stream)
     ShrinkArgsMany m = {};
     m.side[0] = side_of(s, ws, 0, a.X, a.ldx, a.A, a.K);
     m.scaling = a.scaling, m.R = a.R;
+    x.operand = m.operand = reinterpret_cast<uint16_t *>(ws + s.operand);
+    x.up = m.up = reinterpret_cast<int *>(ws + s.up);
     const dim3 grid((unsigned)m.side[0].slices, (unsigned)tiles);
     e = with_type(a.type, [&](auto type) {
         return with_rank(a.R, [&](auto rt) {
             constexpr int RT = decltype(rt)::value;
             const hipError_t err = enqueue(&lora_shrink_kernel<decltype(type)::value, RT, false>, grid, 256, shrink_lds<RT>(), stream, l, m);
-            return err != hipSuccess ? err : enqueue(&lora_sum_kernel<RT, 0>, dim3(sum_blocks(a.M, a.R)), 256, 0, stream, l, m);
+            return err != hipSuccess ? err : enqueue(&lora_sum_kernel<decltype(type)::value, RT, 0>, dim3(sum_blocks(a.M, a.R)), 256, 0, stream, l, m, 0);
         });
     });
     return e != hipSuccess ? e : expand(a, l, x, false, kTileRows, stream);
@@ -808,6 +877,7 @@ hipError_t launch_lora_grad(const LoraArgs &a, hipStream_t stream)
     m.side[0] = side_of(s, ws, 0, a.X, a.ldx, a.A, a.K);
     m.side[1] = side_of(s, ws, 1, a.Y, a.ldy, a.B, a.N);
     m.scaling = a.scaling, m.R = a.R;
+    m.operand = reinterpret_cast<uint16_t *>(ws + s.operand), m.up = reinterpret_cast<int *>(ws + s.up);
     const int most = m.side[0].slices > m.side[1].slices ? m.side[0].slices : m.side[1].slices;
     return with_type(a.type, [&](auto type) {
         return with_rank(a.R, [&](auto rt) {
@@ -818,8 +888,8 @@ hipError_t launch_lora_grad(const LoraArgs &a, hipStream_t stream)
                 const dim3 grid((unsigned)most, (unsigned)tiles, 2);
                 err = enqueue(&lora_shrink_kernel<T, RT, true>, grid, 256, shrink_lds<RT>(), stream, l, m);
                 const dim3 sums(sum_blocks(a.M, a.R), 1, 2);
-                if (err == hipSuccess) err = wide ? enqueue(&lora_sum_kernel<RT, 3>, sums, 256, 0, stream, l, m) : enqueue(&lora_sum_kernel<RT, 2>, sums, 256, 0, stream, l, m);
-                const ExpandArgs x = {static_cast<const uint16_t *>(a.A), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), m.side[1].partial, a.ldbase, a.ldo, a.K, a.R, 1};
+                if (err == hipSuccess) err = wide ? enqueue(&lora_sum_kernel<T, RT, 3>, sums, 256, 0, stream, l, m, 1) : enqueue(&lora_sum_kernel<T, RT, 2>, sums, 256, 0, stream, l, m, 1);
+                const ExpandArgs x = {static_cast<const uint16_t *>(a.A), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), nullptr, m.operand, m.up, a.ldbase, a.ldo, a.K, a.R, 1};
                 if (err == hipSuccess) err = expand(a, l, x, true, kTileRows, stream);  // (dX may be written over: the last launch reads X and dY only)
                 if (err != hipSuccess) return err;
             }

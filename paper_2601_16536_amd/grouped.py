@@ -77,7 +77,7 @@ def query_tile(E: int, count: int, N: int, K: int, transposed: bool = False, gra
 
 
 def sort_workspace_bytes(count: int, E: int) -> int:
-    """Bytes of workspace that `sort` needs for so many ids; 0 up to 65536."""
+    """Bytes of workspace that `sort` needs for so many ids; 0 up to 4096."""
     return int(lib().w4a16_grouped_sort_workspace_bytes(count, E))
 
 

@@ -124,7 +124,7 @@ def test_every_size_has_a_tile(grouped):
                 for kw in ({}, {"transposed": True}, {"grad": True}):
                     rows, cols = grouped.query_tile(E, count, N, K, **kw)
                     assert rows % 16 == 0 and cols % 16 == 0 and 16 <= rows <= 256 and 16 <= cols <= 256
-    assert grouped.sort_workspace_bytes(65536, 1024) == 0 and grouped.sort_workspace_bytes(65537, 3) > 0
+    assert grouped.sort_workspace_bytes(4096, 1024) == 0 and grouped.sort_workspace_bytes(4097, 3) > 0
 
 
 def test_binding_refuses_host_tensors_and_other_types(grouped):

@@ -24,6 +24,32 @@ __device__ __forceinline__ void store_grad(void *dW, size_t at, float4_t v, int 
     }
 }
 
+// 16 rows from n on by 128 bytes from column k on, as whole lines through `mine`, the wave's own kStaging bytes of LDS: 32 bytes of each row at a time took 8 us per 256 x 256 tile.  `of(i)`: the
+// 16 x 16 values at column k + 16 i, four columns of row lane % 16 in a lane.
+constexpr int kStageRow = 144, kStaging = 16 * kStageRow;
+template <int TYPE, int GRAD_TYPE, class Of>
+__device__ __forceinline__ void store_lines(const GroupGradArgs &a, int group, int n, int k, uint8_t *mine, Of of)
+{
+    typedef typename ActOf<TYPE>::type Act;
+    constexpr int kSize = GRAD_TYPE == kTypeF32 ? 4 : 2, kValues = 16 / kSize;
+    const int lane = (int)threadIdx.x & 63;
+    uint8_t *const dw = static_cast<uint8_t *>(a.dW) + (size_t)group * (size_t)a.N * (size_t)a.K * kSize;
+#pragma unroll
+    for (int i = 0; i < 8 / kSize; ++i) {
+        uint8_t *const to = mine + (lane & 15) * kStageRow + (16 * i + (lane >> 4) * 4) * kSize;
+        if constexpr (GRAD_TYPE == kTypeF32) *reinterpret_cast<float4_t *>(to) = of(i);
+        else *reinterpret_cast<uint2_t *>(to) = to_16bit4<Act>(of(i));
+    }
+    asm volatile("" ::: "memory");  // (of one wave, whose LDS accesses are in order)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int row = h * 8 + (lane >> 3), at_n = n + row, at_k = k + (lane & 7) * kValues;
+        const uint4_t v = *reinterpret_cast<const uint4_t *>(mine + row * kStageRow + (lane & 7) * 16);
+        if (at_n < a.N && at_k < a.K) *reinterpret_cast<uint4_t *>(dw + ((size_t)at_n * (size_t)a.K + (size_t)at_k) * kSize) = v;
+    }
+    asm volatile("" ::: "memory");
+}
+
 // TP columns (of X) by TQ rows (columns of dY) of one dW_e.
 template <int TYPE, int GRAD_TYPE, bool GATHER, int TP, int TQ, int PW, int QW, int DEPTH, int PER_CU>
 __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_grad_kernel(GroupGradArgs a, int cols, int pairs)
@@ -79,6 +105,17 @@ __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_grad_kernel(GroupG
     float4_t acc[PI][QI];
     group_product<Act, PTile, QTile, PI, QI, DEPTH>(acc, lds, pw * PI * 16, qw * QI * 16, (rows + kGroupStage - 1) / kGroupStage, rows / kGroupStage, fetch);
 
+    if (!a.accumulate) {
+        constexpr int kFrags = GRAD_TYPE == kTypeF32 ? 2 : 4;
+        static_assert(PI % kFrags == 0 && kWaves * kStaging <= DEPTH * kBuffer, "whole lines, staged where the tiles were");
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < QI; ++j)
+#pragma unroll
+            for (int i0 = 0; i0 < PI; i0 += kFrags)
+                store_lines<TYPE, GRAD_TYPE>(a, group, n0 + qw * QI * 16 + 16 * j, k0 + pw * PI * 16 + 16 * i0, lds + wave * kStaging, [&](int i) { return acc[i0 + i][j]; });
+        return;
+    }
 #pragma unroll
     for (int j = 0; j < QI; ++j) {
         const int n = n0 + qw * QI * 16 + 16 * j + c;
@@ -97,9 +134,8 @@ __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_grad_kernel(GroupG
 //
 // A tile has as many stages as its group has 64 rows, often eight or fewer, so the loop of half tiles (group_product_wide in w4a16_group_device.h) runs on from one tile to the next: its numbers count
 // on, the loads of the next tile's first stages are asked for while this one's last are multiplied, and a tile's results are stored in between.  (One launch of a workgroup per tile, 4096 tokens,
-// top 8 of 64 experts, K = N = 4096, BF16: 1763 us.)  The stores go through LDS, a wave's own 16 rows of 128 bytes, so that they are whole lines: 32 bytes of each row at a time took
-// 8 us per tile.
-constexpr int kGradWorkgroups = 256, kStageRow = 144, kStaging = 16 * kStageRow;
+// top 8 of 64 experts, K = N = 4096, BF16: 1763 us.)
+constexpr int kGradWorkgroups = 256;
 
 // The tiles of a workgroup, in order, and the stages of those that have some.  XCD x takes the x-th eighth of every group's tiles, neighbours that read the same rows' columns (the groups' lengths
 // differ); its workgroups take them in turn.
@@ -343,28 +379,12 @@ __global__ __launch_bounds__(512, 1) void group_grad_wide_kernel(GroupGradArgs a
                 }
             return false;
         }
-        constexpr int kSize = GRAD_TYPE == kTypeF32 ? 4 : 2, kFrags = 128 / (16 * kSize), kValues = 16 / kSize;  // that 128 bytes of a row hold; values of 16 bytes
-        uint8_t *const dw = static_cast<uint8_t *>(a.dW) + (size_t)t.group * (size_t)a.N * (size_t)a.K * kSize;
+        constexpr int kFrags = GRAD_TYPE == kTypeF32 ? 2 : 4;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int i0 = 0; i0 < 8; i0 += kFrags) {
-#pragma unroll
-                for (int i = 0; i < kFrags; ++i) {
-                    uint8_t *const to = mine + c * kStageRow + (16 * i + p4) * kSize;
-                    if constexpr (GRAD_TYPE == kTypeF32) *reinterpret_cast<float4_t *>(to) = acc[i0 + i][j];
-                    else *reinterpret_cast<uint2_t *>(to) = to_16bit4<Act>(acc[i0 + i][j]);
-                }
-                asm volatile("" ::: "memory");  // (of one wave, whose LDS accesses are in order)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const int row = h * 8 + (lane >> 3), n = n0 + (j >> 1) * 128 + qw * 32 + 16 * (j & 1) + row;
-                    const int k = k0 + (i0 >> 2) * 128 + pw * 64 + 16 * (i0 & 3) + (lane & 7) * kValues;
-                    const uint4_t v = *reinterpret_cast<const uint4_t *>(mine + row * kStageRow + (lane & 7) * 16);
-                    if (n < a.N && k < a.K) *reinterpret_cast<uint4_t *>(dw + ((size_t)n * (size_t)a.K + (size_t)k) * kSize) = v;
-                }
-                asm volatile("" ::: "memory");
-            }
+            for (int i0 = 0; i0 < 8; i0 += kFrags)
+                store_lines<TYPE, GRAD_TYPE>(a, t.group, n0 + (j >> 1) * 128 + qw * 32 + 16 * (j & 1), k0 + (i0 >> 2) * 128 + pw * 64 + 16 * (i0 & 3), mine, [&](int i) { return acc[i0 + i][j]; });
         return n0 + 256 <= a.N && k0 + 256 <= a.K;
     };
 
@@ -477,7 +497,12 @@ auto with_form(int form, Use use)
 
 GroupTile plan_group_grad(int E, long long count, int N, int K)
 {
-    const int form = count / E >= 96 && (long long)E * N * K >= 128ll * 65536;
+    // The largest tiles where every workgroup has eight, or groups are so large that all have as many of each: as the tiles of a group have as many stages as the group has rows, few are uneven.
+    // Groups of 0.3 to 4 times the mean, us of 128 x 128 | 256 x 256 tiles: 4096 x 4096, 64 groups of 512 rows 1844 | 1462, 8 of 37 66 | 62; 2048 x 4096, 128 of 3 482 | 420; 1024 x 1024, 128 of 75
+    // 103 | 91; with fewer tiles, 2048 x 2048, 16 of 512 116 | 158, 16 of 100 68 | 66; 1024 x 1024, 64 of 512 119 | 171; one group, 8192 x 8192 x 8192 1193 | 1064.
+    (void)count;
+    const long long pairs = (long long)((N + 255) / 256) * ((K + 255) / 256);
+    const int form = pairs * E >= 8 * kGradWorkgroups || pairs >= 4 * kGradWorkgroups;
     return with_form(form, [&](auto f) { return GroupTile{form, f.kRows, f.kCols}; });
 }
 

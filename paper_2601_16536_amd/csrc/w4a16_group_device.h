@@ -333,13 +333,14 @@ __device__ __forceinline__ void group_product(float4_t (&acc)[PI][QI], uint8_t *
 // other one reads.  LDS has eight half tiles; that of phase f is free once both have read it, and number f + 8 is asked for in phase f + 1: seven phases ahead of its use,
 // the last six on their way behind every wait.
 // fetch(kind, stage, to, last, steady): the loads of a half tile, kind = number mod 4; with last the stage may reach past the sum's end; steady (a type): in the middle of the loop.
-template <class Act, class Tile0, class Tile1, class Fetch>
-__device__ __forceinline__ void group_product_wide(float4_t (&acc)[8][4], uint8_t *lds, int pw, int qw, int stages, int whole, Fetch fetch)
+template <class Act, class Tile0, class Tile1, bool ALL, class Fetch>
+__device__ __forceinline__ void group_product_wide(float4_t (&acc)[8][4], uint8_t *lds, int pw, int qw, int q_there, int stages, int whole, Fetch fetch)
 {
     constexpr int kHalf = 16384, kLoads = 2;
     static_assert(Tile0::kBytes == kHalf && Tile1::kBytes == kHalf && Tile0::kLoads == kLoads && Tile1::kLoads == kLoads, "half tiles");
     const int lane = (int)threadIdx.x & 63, end = stages * 4 - 1;  // numbers up to end - 1
     const bool late = pw != 0;
+    const bool q0 = ALL || qw * 32 < q_there, q1 = ALL || qw * 32 + 128 < q_there;  // (the wave's part of the half)
     uint4_t p[2][4], q[2][2][2];  // [step][..]; [set][step][..]
     typename Tile0::template Part<4> pp(lane, pw * 64);
     typename Tile1::template Part<2> qp(lane, qw * 32);
@@ -423,10 +424,10 @@ __device__ __forceinline__ void group_product_wide(float4_t (&acc)[8][4], uint8_
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
-        phase([&] { read_p(4 * kSet); }, [&] { multiply(k0, k0, first); }, k0);
-        phase([&] { read_q(4 * kSet + 1, second); }, [&] { multiply(k0, k1, second); }, k1);
-        phase([&] { read_p(4 * kSet + 2); }, [&] { multiply(k1, k1, second); }, std::integral_constant<int, 2>{});
-        phase([&] { read_q(4 * kSet + 3, second); }, [&] { multiply(k1, k0, first); }, std::integral_constant<int, 3>{});
+        phase([&] { read_p(4 * kSet); }, [&] { if (q0) multiply(k0, k0, first); }, k0);
+        phase([&] { read_q(4 * kSet + 1, second); }, [&] { if (q1) multiply(k0, k1, second); }, k1);
+        phase([&] { read_p(4 * kSet + 2); }, [&] { if (q1) multiply(k1, k1, second); }, std::integral_constant<int, 2>{});
+        phase([&] { read_q(4 * kSet + 3, second); }, [&] { if (q0) multiply(k1, k0, first); }, std::integral_constant<int, 3>{});
     };
     int i = 0;
     for (; i + 3 < whole; i += 2) {
@@ -443,5 +444,21 @@ __device__ __forceinline__ void group_product_wide(float4_t (&acc)[8][4], uint8_
 // Four FP32 results to a 16-bit type, 8 bytes.
 template <class Act>
 __device__ __forceinline__ uint2_t to_16bit4(float4_t v) { return (uint2_t){Act::pack2(v[0], v[1]), Act::pack2(v[2], v[3])}; }
+
+// 16 rows of 128 bytes of results as whole lines, through `mine`, the wave's own kStaging bytes of LDS: v[i] is what a lane has of row lane % 16, its 4 values lane / 16 of the i-th 16.
+// to(row, bytes from the row's first on, 16 bytes).  (32 bytes of each row at a time took 8 us per 256 x 256 tile.)
+constexpr int kStageRow = 144, kStaging = 16 * kStageRow;
+template <class V, int COUNT, class To>
+__device__ __forceinline__ void store_lines(uint8_t *mine, const V (&v)[COUNT], To to)
+{
+    static_assert(COUNT * 4 * sizeof(V) == 128, "a line");
+    const int lane = (int)threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) *reinterpret_cast<V *>(mine + (lane & 15) * kStageRow + (4 * i + (lane >> 4)) * (int)sizeof(V)) = v[i];
+    asm volatile("" ::: "memory");  // (of one wave, whose LDS accesses are in order)
+#pragma unroll
+    for (int h = 0; h < 2; ++h) to(h * 8 + (lane >> 3), (lane & 7) * 16, *reinterpret_cast<const uint4_t *>(mine + (h * 8 + (lane >> 3)) * kStageRow + (lane & 7) * 16));
+    asm volatile("" ::: "memory");
+}
 
 }  // namespace w4a16

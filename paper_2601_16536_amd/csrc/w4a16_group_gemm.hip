@@ -109,6 +109,7 @@ __global__ __launch_bounds__(512, 1) void group_gemm_wide_kernel(GroupGemmArgs a
     for (int i = 0; i < 4; ++i) {
         const int half = (i >> 1) * 128, r = min(half + QTile::row(wave, lane, i & 1), rows - 1), piece = QTile::piece(lane) * 16;
         xo[i] = (uint32_t)(GATHER ? clamp_to(a.rows[t.row0 + r] / a.top_k, 0, a.x_rows - 1) : r) * (uint32_t)row_x + (uint32_t)piece;
+        if (half >= rows) xo[i] = kOutOfRange;
         if constexpr (!ACROSS) wo[i] = (uint32_t)min(half + PTile::row(wave, lane, i & 1), a.N - 1 - n0) * (uint32_t)row_w + (uint32_t)PTile::piece(lane) * 16u;
     }
     // Across, the loads of a lane are whole rows and halves apart, and the buffer's end is where W_e's is: past a row's last column they bring what lies there, for columns that are not kept.
@@ -134,23 +135,31 @@ __global__ __launch_bounds__(512, 1) void group_gemm_wide_kernel(GroupGemmArgs a
         }
     };
     float4_t acc[8][4];
-    group_product_wide<Act, PTile, QTile>(acc, lds, pw, qw, product ? (a.K + kGroupStage - 1) / kGroupStage : 0, a.K / kGroupStage, fetch);
+    const int stages = product ? (a.K + kGroupStage - 1) / kGroupStage : 0;
+    if (rows > 224) group_product_wide<Act, PTile, QTile, true>(acc, lds, pw, qw, rows, stages, a.K / kGroupStage, fetch);
+    else group_product_wide<Act, PTile, QTile, false>(acc, lds, pw, qw, rows, stages, a.K / kGroupStage, fetch);
 
-    uint16_t *const y = static_cast<uint16_t *>(a.Y);
+    uint16_t *const y = static_cast<uint16_t *>(a.Y) + (size_t)t.row0 * (size_t)a.ldy;
+    uint8_t *const mine = lds + wave * kStaging;
+    __syncthreads();  // (the tiles' place in LDS)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int r = (j >> 1) * 128 + qw * 32 + 16 * (j & 1) + c;
-        if (r >= rows) continue;
+        const int r0 = (j >> 1) * 128 + qw * 32 + 16 * (j & 1);
+        if (r0 >= rows) continue;
         bool there = true;
         if constexpr (GATHER) {
-            const int from = a.rows[t.row0 + r];
+            const int from = a.rows[t.row0 + min(r0 + c, rows - 1)];
             there = from >= 0 && from / a.top_k < a.x_rows;
         }
-        uint16_t *const to = y + (size_t)(t.row0 + r) * (size_t)a.ldy;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int n = n0 + (i >> 2) * 128 + pw * 64 + 16 * (i & 3) + p4;
-            if (n < a.N) *reinterpret_cast<uint2_t *>(to + n) = there ? to_16bit4<Act>(acc[i][j]) : (uint2_t){0u, 0u};
+        for (int h = 0; h < 2; ++h) {
+            uint2_t v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = there ? to_16bit4<Act>(acc[h * 4 + i][j]) : (uint2_t){0u, 0u};
+            store_lines(mine, v, [&](int row, int bytes, uint4_t piece) {
+                const int n = n0 + h * 128 + pw * 64 + bytes / 2;
+                if (r0 + row < rows && n < a.N) *reinterpret_cast<uint4_t *>(y + (size_t)(r0 + row) * (size_t)a.ldy + n) = piece;
+            });
         }
     }
 }
@@ -226,7 +235,7 @@ GroupTile plan_group_gemm(int E, long long count, int N, int K, int transposed)
 {
     (void)K, (void)transposed;
     const long long average = count / E;
-    const int form = average <= 8 ? 0 : average <= 64 ? 1 : average < 160 || count * N < 128ll * 65536 ? 2 : 3;
+    const int form = average <= 8 ? 0 : average <= 64 ? 1 : average < 96 || count * N < 128ll * 65536 ? 2 : 3;
     return with_form(form, [&](auto f) { return GroupTile{form, f.kRows, f.kCols}; });
 }
 

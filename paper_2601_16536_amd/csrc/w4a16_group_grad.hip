@@ -24,30 +24,29 @@ __device__ __forceinline__ void store_grad(void *dW, size_t at, float4_t v, int 
     }
 }
 
-// 16 rows from n on by 128 bytes from column k on, as whole lines through `mine`, the wave's own kStaging bytes of LDS: 32 bytes of each row at a time took 8 us per 256 x 256 tile.  `of(i)`: the
-// 16 x 16 values at column k + 16 i, four columns of row lane % 16 in a lane.
-constexpr int kStageRow = 144, kStaging = 16 * kStageRow;
+// 16 rows from n on by 128 bytes from column k on.  Where they are whole lines, past the caches, whose room the operands need (777 tokens, top 6 of 64, 2048 x 4096 305 -> 260 us; where rows of dW end
+// inside a line, 35 us in place of 20 for 600 rows of 8 groups, 2056 x 1000).  of(i): the 16 x 16 values at column k + 16 i, four columns of row lane % 16 in a lane.
 template <int TYPE, int GRAD_TYPE, class Of>
-__device__ __forceinline__ void store_lines(const GroupGradArgs &a, int group, int n, int k, uint8_t *mine, Of of)
+__device__ __forceinline__ void store_grads(const GroupGradArgs &a, int group, int n, int k, uint8_t *mine, Of of)
 {
     typedef typename ActOf<TYPE>::type Act;
-    constexpr int kSize = GRAD_TYPE == kTypeF32 ? 4 : 2, kValues = 16 / kSize;
-    const int lane = (int)threadIdx.x & 63;
-    uint8_t *const dw = static_cast<uint8_t *>(a.dW) + (size_t)group * (size_t)a.N * (size_t)a.K * kSize;
-#pragma unroll
-    for (int i = 0; i < 8 / kSize; ++i) {
-        uint8_t *const to = mine + (lane & 15) * kStageRow + (16 * i + (lane >> 4) * 4) * kSize;
-        if constexpr (GRAD_TYPE == kTypeF32) *reinterpret_cast<float4_t *>(to) = of(i);
-        else *reinterpret_cast<uint2_t *>(to) = to_16bit4<Act>(of(i));
+    constexpr int kSize = GRAD_TYPE == kTypeF32 ? 4 : 2;
+    const uint32_t row_size = (uint32_t)a.K * kSize;
+    const bool lines = row_size % 128 == 0;
+    const __amdgpu_buffer_rsrc_t dw = __builtin_amdgcn_make_buffer_rsrc(
+        static_cast<uint8_t *>(a.dW) + ((size_t)group * (size_t)a.N + (size_t)n) * row_size + (size_t)k * kSize, 0, kOutOfRange - 1, kRawBuffer);
+    auto to = [&](int row, int bytes, uint4_t piece) {
+        const uint32_t at = n + row < a.N && k + bytes / kSize < a.K ? (uint32_t)row * row_size + (uint32_t)bytes : kOutOfRange;
+        if (lines) __builtin_amdgcn_raw_buffer_store_b128(piece, dw, at, 0, 2);  // non-temporal
+        else __builtin_amdgcn_raw_buffer_store_b128(piece, dw, at, 0, 0);
+    };
+    if constexpr (GRAD_TYPE == kTypeF32) {
+        const float4_t v[2] = {of(0), of(1)};
+        store_lines(mine, v, to);
+    } else {
+        const uint2_t v[4] = {to_16bit4<Act>(of(0)), to_16bit4<Act>(of(1)), to_16bit4<Act>(of(2)), to_16bit4<Act>(of(3))};
+        store_lines(mine, v, to);
     }
-    asm volatile("" ::: "memory");  // (of one wave, whose LDS accesses are in order)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int row = h * 8 + (lane >> 3), at_n = n + row, at_k = k + (lane & 7) * kValues;
-        const uint4_t v = *reinterpret_cast<const uint4_t *>(mine + row * kStageRow + (lane & 7) * 16);
-        if (at_n < a.N && at_k < a.K) *reinterpret_cast<uint4_t *>(dw + ((size_t)at_n * (size_t)a.K + (size_t)at_k) * kSize) = v;
-    }
-    asm volatile("" ::: "memory");
 }
 
 // TP columns (of X) by TQ rows (columns of dY) of one dW_e.
@@ -113,7 +112,7 @@ __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_grad_kernel(GroupG
         for (int j = 0; j < QI; ++j)
 #pragma unroll
             for (int i0 = 0; i0 < PI; i0 += kFrags)
-                store_lines<TYPE, GRAD_TYPE>(a, group, n0 + qw * QI * 16 + 16 * j, k0 + pw * PI * 16 + 16 * i0, lds + wave * kStaging, [&](int i) { return acc[i0 + i][j]; });
+                store_grads<TYPE, GRAD_TYPE>(a, group, n0 + qw * QI * 16 + 16 * j, k0 + pw * PI * 16 + 16 * i0, lds + wave * kStaging, [&](int i) { return acc[i0 + i][j]; });
         return;
     }
 #pragma unroll
@@ -130,309 +129,115 @@ __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_grad_kernel(GroupG
     }
 }
 
-// 256 x 256 tiles, one workgroup of eight waves to a compute unit that takes tile after tile.
-//
-// A tile has as many stages as its group has 64 rows, often eight or fewer, so the loop of half tiles (group_product_wide in w4a16_group_device.h) runs on from one tile to the next: its numbers count
-// on, the loads of the next tile's first stages are asked for while this one's last are multiplied, and a tile's results are stored in between.  (One launch of a workgroup per tile, 4096 tokens,
-// top 8 of 64 experts, K = N = 4096, BF16: 1763 us.)
-constexpr int kGradWorkgroups = 256;
-
-// The tiles of a workgroup, in order, and the stages of those that have some.  XCD x takes the x-th eighth of every group's tiles, neighbours that read the same rows' columns (the groups' lengths
-// differ); its workgroups take them in turn.
-struct GradTiles {
-    typedef const __attribute__((address_space(4))) int32_t *scalar_ints_t;
-    scalar_ints_t offsets;
-    int E, count, pairs, per, at;       // at: among the XCD's tiles
-    int group, pair, begin, rows;       // of this tile
-    int stage, stages;
-    __device__ __forceinline__ GradTiles(const GroupGradArgs &a, int all)
-        : offsets((scalar_ints_t)(uintptr_t)a.offsets), E(a.E), count(a.count), pairs(all), per((all + (int)kPlaceXcds - 1) / (int)kPlaceXcds),
-          at((int)(blockIdx.x / kPlaceXcds) - (int)(gridDim.x / kPlaceXcds)), stage(0), stages(0)
-    {
-    }
-    __device__ __forceinline__ bool next_tile()
-    {
-        for (;;) {
-            at += (int)(gridDim.x / kPlaceXcds);
-            group = at / per;
-            if (group >= E) return false;
-            pair = (int)(blockIdx.x % kPlaceXcds) * per + at - group * per;
-            if (pair < pairs) break;
-        }
-        begin = clamp_to(offsets[group], 0, count);
-        rows = clamp_to(offsets[group + 1], begin, count) - begin;
-        stages = (rows + kGroupStage - 1) / kGroupStage;
-        stage = 0;
-        return true;
-    }
-    __device__ __forceinline__ bool next_stage()
-    {
-        if (++stage < stages) return true;
-        do
-            if (!next_tile()) return false;
-        while (stages == 0);
-        return true;
-    }
-};
-
+// 256 x 256, eight waves, a workgroup to a compute unit: the loop of half tiles (group_product_wide in w4a16_group_device.h).
+// 4096 tokens, top 8 of 64 experts, K = N = 4096, BF16: 1490 us, rows as they are 1380; one group of 8192, 8192 x 8192 784.  A workgroup that runs on from tile to tile, the next one's first stages on their way while this one's
+// results are stored, took 1563, 1449 and 1047:
+// what a stage needs to know about where it is costs more than the 9 us between two tiles.
 template <int TYPE, int GRAD_TYPE, bool GATHER>
 __global__ __launch_bounds__(512, 1) void group_grad_wide_kernel(GroupGradArgs a, int cols, int pairs)
 {
     typedef typename ActOf<TYPE>::type Act;
     typedef AcrossTile<128, 8> Tile;
-    constexpr int kHalf = 16384, kLoads = 2;
-    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];  // eight half tiles, the rows' numbers, the waves' staging
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int pw = wave >> 2, qw = wave & 3;
-    const bool late = pw != 0;
-    const uint32_t row_x = (uint32_t)a.ldx * 2, row_y = (uint32_t)a.ldy * 2;
-    // A tile's place in dW_e: blocks of four tiles' rows, column by column.
-    auto place_of_tile = [&](int pair, int *n0, int *k0) {
+    const int pw = wave >> 2, qw = wave & 3, c = lane & 15, p4 = (lane >> 4) * 4;
+    // An eighth of every group's tiles to an XCD, neighbours that read the same rows' columns: the groups' lengths differ.
+    const unsigned per = ((unsigned)pairs + kPlaceXcds - 1) / kPlaceXcds, in = blockIdx.x / kPlaceXcds;
+    const int group = (int)(in / per), pair = (int)(blockIdx.x % kPlaceXcds * per + in % per);
+    if (pair >= pairs) return;
+    int tn, tk;
+    {
         const int high_all = pairs / cols, block = pair / (kBlockRows * cols), high = min(kBlockRows, high_all - block * kBlockRows), rest = pair - block * kBlockRows * cols;
-        *n0 = (block * kBlockRows + rest % high) * 256;
-        *k0 = rest / high * 256;
-    };
-
-    // ---- loads ----
+        tn = block * kBlockRows + rest % high;
+        tk = rest / high;
+    }
+    const int n0 = tn * 256, k0 = tk * 256;
+    int begin, end;
+    group_range(a.offsets, a.E, a.count, group, &begin, &end);
+    begin = __builtin_amdgcn_readfirstlane(begin);
+    const int rows = __builtin_amdgcn_readfirstlane(end) - begin;
+    const uint32_t row_x = (uint32_t)a.ldx * 2, row_y = (uint32_t)a.ldy * 2;
+    const uint8_t *const x = static_cast<const uint8_t *>(a.X) + (size_t)k0 * 2 + (GATHER ? 0 : (size_t)begin * row_x);
+    const uint8_t *const y = static_cast<const uint8_t *>(a.dY) + (size_t)n0 * 2 + (size_t)begin * row_y;
     // The loads of a lane are whole rows and halves apart; the buffers' ends are the groups': past a row's last column they bring what lies there, for values that are not kept.
-    const int lane_row = Tile::row(wave, lane, 0);
-    const uint32_t xo = (GATHER ? 0u : (uint32_t)lane_row * row_x) + (uint32_t)Tile::column(wave, lane, 0) * 2u, yo = (uint32_t)lane_row * row_y + (uint32_t)Tile::column(wave, lane, 0) * 2u;
-    GradTiles from(a, pairs), numbers(a, pairs);  // what is loaded; gathered: whose rows' numbers are, two stages ahead, 64 numbers for each of four stages
-    int from_n0 = 0, from_k0 = 0, unit = -1;      // (unit: stages loaded)
-    const uint8_t *x = nullptr, *y = nullptr;     // at the tile's columns and, x if it is not gathered, the group's first row
-    uint32_t x_bytes = 0, x_bytes1 = 0;           // gathered, X is below 2 GiB
-    uint32_t xr[2];                               // gathered: where the rows that X's halves are loaded from begin
-    int *const list = reinterpret_cast<int *>(lds + 8 * kHalf);
-    bool more_numbers = GATHER;
-    auto ask_numbers = [&](int of) {
-        if (!more_numbers) return;
-        more_numbers = numbers.next_stage();
-        if (more_numbers)
-            numbers_to_lds_unseen(a.rows + numbers.begin + numbers.stage * kGroupStage, (uint32_t)(numbers.rows - numbers.stage * kGroupStage) * 4u, (uint32_t)lane * 4u,
-                                  reinterpret_cast<uint8_t *>(list + (of & 3) * 64));
+    const int row = Tile::row(wave, lane, 0);
+    const uint32_t xo = (GATHER ? 0u : (uint32_t)row * row_x) + (uint32_t)Tile::column(wave, lane, 0) * 2u, yo = (uint32_t)row * row_y + (uint32_t)Tile::column(wave, lane, 0) * 2u;
+    // Gathered: the rows' numbers come to LDS two stages ahead of the loads that need them, 64 for each stage, of four stages; those of the first two stages as they are.
+    uint32_t xr[2];  // where the rows that X's halves are loaded from begin
+    int *const list = reinterpret_cast<int *>(lds + 131072);
+    auto ask_rows = [&](int stage) {
+        if (stage * kGroupStage < rows)
+            numbers_to_lds_unseen(a.rows + begin + stage * kGroupStage, (uint32_t)(rows - stage * kGroupStage) * 4u, (uint32_t)lane * 4u, reinterpret_cast<uint8_t *>(list + (stage & 3) * 64));
     };
-    auto next_unit = [&]() {
-        if (!from.next_stage()) return false;
-        ++unit;
-        if (from.stage == 0) {
-            place_of_tile(from.pair, &from_n0, &from_k0);
-            x = static_cast<const uint8_t *>(a.X) + (size_t)from_k0 * 2 + (GATHER ? 0 : (size_t)from.begin * row_x);
-            y = static_cast<const uint8_t *>(a.dY) + (size_t)from_n0 * 2 + (size_t)from.begin * row_y;
-            if constexpr (GATHER) {
-                x_bytes = (uint32_t)(a.x_rows - 1) * row_x + 2u * (uint32_t)(a.K - from_k0);
-                x_bytes1 = x_bytes < 256u ? 0u : x_bytes - 256u;
+    uint32_t start[2][2];  // xr of stages 0 and 1
+    auto place_of = [&](int source, int r) {
+        const uint32_t from = a.divide(source);
+        return ((r < rows) & (source >= 0) & (from < (uint32_t)a.x_rows)) ? from * row_x : kOutOfRange;
+    };
+    if (GATHER && rows > 0) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = s * kGroupStage + Tile::row(wave, lane, i);
+                start[s][i] = place_of(a.rows[begin + min(r, rows - 1)], r);
             }
+    }
+    auto take_rows = [&](int stage, auto steady) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int in_stage = Tile::row(wave, lane, i);
+            xr[i] = place_of(list[(stage & 3) * 64 + in_stage], stage * kGroupStage + in_stage);
+            if (!decltype(steady)::value && stage < 2) xr[i] = stage ? start[1][i] : start[0][i];
         }
-        return true;
     };
-    // The two loads of a half tile of the unit (0 P0, 1 Q1, 2 P1, 3 Q0): their addresses are made while the half tile before is multiplied.
-    struct Loads {
-        const uint8_t *base[2];
-        uint32_t bytes[2], offset[2];
-    };
-    Loads next;
-    auto prepare = [&](int kind) {
-        if (GATHER && kind == 0) {
+    const uint32_t x_bytes = (uint32_t)(a.x_rows - 1) * row_x + 2u * (uint32_t)(a.K - k0), x_bytes1 = x_bytes < 256u ? 0u : x_bytes - 256u;  // (gathered: X is below 2 GiB)
+    auto fetch = [&](int kind, int stage, uint8_t *to, bool, auto steady) {
+        const int r0 = stage * kGroupStage;
+        if (GATHER && kind == 0) take_rows(stage, steady);
+        if (GATHER && kind == 0) ask_rows(stage + 2);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int in_stage = Tile::row(wave, lane, i), source = list[(unit & 3) * 64 + in_stage];
-                const uint32_t r = a.divide(source);
-                xr[i] = ((from.stage * kGroupStage + in_stage < from.rows) & (source >= 0) & (r < (uint32_t)a.x_rows)) ? r * row_x + xo : kOutOfRange;
-            }
-        }
-        const int r = from.stage * kGroupStage, left = from.rows - r;
-        if (kind == 0 || kind == 2) {
-            const int k = kind ? 128 : 0;
-            const uint8_t *const at = x + 2 * k + (GATHER ? 0 : (size_t)r * row_x);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                next.base[i] = at + (GATHER ? 0 : (size_t)(32 * i) * row_x);
-                next.bytes[i] = GATHER ? (kind ? x_bytes1 : x_bytes) : bytes_of(left - 32 * i, (int)row_x, 2 * (a.K - from_k0 - k));
-                next.offset[i] = GATHER ? xr[i] : xo;
-            }
-        } else {
-            const int n = kind == 1 ? 128 : 0;
-            const uint8_t *const at = y + (size_t)r * row_y + 2 * n;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                next.base[i] = at + (size_t)(32 * i) * row_y;
-                next.bytes[i] = bytes_of(left - 32 * i, (int)row_y, 2 * (a.N - from_n0 - n));
-                next.offset[i] = yo;
+        for (int i = 0; i < 2; ++i) {
+            const int r = r0 + 32 * i;
+            uint8_t *const at = to + Tile::kib(wave, i) * 1024;
+            if (kind == 0 || kind == 2) {
+                const int k = kind ? 128 : 0;
+                if constexpr (GATHER) load_to_lds_unseen(x + 2 * k, kind ? x_bytes1 : x_bytes, xr[i] + xo, 0, at);
+                else load_to_lds_unseen(x + (size_t)r * row_x + 2 * k, bytes_of(rows - r, (int)row_x, 2 * (a.K - k0 - k)), xo, 0, at);
+            } else {
+                const int n = kind == 1 ? 128 : 0;
+                load_to_lds_unseen(y + (size_t)r * row_y + 2 * n, bytes_of(rows - r, (int)row_y, 2 * (a.N - n0 - n)), yo, 0, at);
             }
         }
     };
-    auto issue = [&](int kind, uint8_t *to) {
-        if (GATHER && kind == 0) ask_numbers(unit + 2);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) load_to_lds_unseen(next.base[i], next.bytes[i], next.offset[i], 0, to + Tile::kib(wave, i) * 1024);
-    };
-
-    // ---- products ----
     float4_t acc[8][4];
-    uint4_t p[2][4], q[2][2][2];  // [step][..]; [half][step][..]
-    const typename Tile::template Part<4> pp(lane, pw * 64);
-    const typename Tile::template Part<2> qp(lane, qw * 32);
-    auto place = [&](int number) { return lds + (((number & 3) == 3 ? number + 4 : number) & 7) * kHalf; };
-    auto read_p = [&](int number) {
-        const uint8_t *const tile = place(number);
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) p[s][i] = pp.read(tile, i, s);
-    };
-    auto read_q = [&](int number, auto half) {
-        const uint8_t *const tile = place(number);
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) q[decltype(half)::value][s][j] = qp.read(tile, j, s);
-    };
-    auto multiply = [&](auto ph, auto qh, auto meanwhile) {
-        constexpr int h = decltype(ph)::value, b = decltype(qh)::value;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) acc[h * 4 + i][b * 2 + j] = Act::mfma(Act::x_operand(p[s][i]), Act::x_operand(q[b][s][j]), acc[h * 4 + i][b * 2 + j]);
-            if (s == 0) meanwhile();
-        }
-    };
-    // What the stores of a tile add to the count: the stage behind them need not wait for them, as they are younger than what it needs.
-    constexpr int kStores = GRAD_TYPE == kTypeF32 ? 32 : 16;
-    // All but the last `halves` half tiles of this wave are there (7: six, and a tile has been stored just ahead of this stage), and it has read what it reads.
-    auto wait = [&](int halves) {
-        switch (halves) {
-        case 0: asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory"); break;
-        case 1: asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(1 * kLoads) : "memory"); break;
-        case 2: asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(2 * kLoads) : "memory"); break;
-        case 3: asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(3 * kLoads) : "memory"); break;
-        case 4: asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(4 * kLoads) : "memory"); break;
-        case 5: asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(5 * kLoads) : "memory"); break;
-        case 6: asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(6 * kLoads) : "memory"); break;
-        default: asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(6 * kLoads + kStores) : "memory"); break;
-        }
-    };
-    auto arrive = [&](int halves) {
-        wait(halves);
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-    };
-    constexpr std::integral_constant<int, 0> k0{};
-    constexpr std::integral_constant<int, 1> k1{};
-    int done = 0, end = 0x7FFFFFFF;  // stages multiplied; half tiles that there are, as far as is known
-    bool more = false;               // whether the stage two behind this one is loaded; then `next` has its first half tile
-    auto look = [&](int of) {        // `of`: the stage that is multiplied next
-        more = next_unit();
-        if (more) prepare(3);
-        else end = 4 * of + 7;  // (its half tiles and the next stage's are there or on their way)
-    };
-    auto stage = [&](bool after) {  // after: a tile has been stored just ahead
-        const bool loads = more, usual = more && !after;
-        auto phase = [&](auto read, auto ph, auto qh, auto n) {
-            constexpr int k = decltype(n)::value;
-            const int f = 4 * done + k;
-            if (loads) issue((k + 7) & 3, place(f + 7));
-            read(f);  // (behind the last stage's P1 there is no Q0: what lies there, for nobody)
-            __builtin_amdgcn_sched_barrier(0);
-            if (usual) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(6 * kLoads) : "memory");
-            else wait(loads ? 7 : max(0, min(6, end - 2 - f)));
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            __builtin_amdgcn_s_setprio(1);
-            multiply(ph, qh, [&] {
-                if constexpr (k < 3) {
-                    if (loads) prepare(k);
-                } else {
-                    if (loads) look(done + 1);
-                }
-            });
-            __builtin_amdgcn_s_setprio(0);
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-        };
-        phase([&](int f) { read_p(f); }, k0, k0, k0);
-        phase([&](int f) { read_q(f, k1); }, k0, k1, k1);
-        phase([&](int f) { read_p(f); }, k1, k1, std::integral_constant<int, 2>{});
-        phase([&](int f) { read_q(f, k1); }, k1, k0, std::integral_constant<int, 3>{});
-#pragma unroll
-        for (int s = 0; s < 2; ++s)
-#pragma unroll
-            for (int j = 0; j < 2; ++j) q[0][s][j] = q[1][s][j];  // (the next stage's Q0)
-        ++done;
-    };
+    group_product_wide<Act, Tile, Tile, true>(acc, lds, pw, qw, 256, (rows + kGroupStage - 1) / kGroupStage, rows / kGroupStage, fetch);
 
-    // ---- results ----
-    uint8_t *const mine = lds + 8 * kHalf + 1024 + wave * kStaging;
-    auto store = [&](const GradTiles &t) {  // whether it took kStores stores of every wave
-        int n0, k0;
-        place_of_tile(t.pair, &n0, &k0);
-        const int c = lane & 15, p4 = (lane >> 4) * 4;
-        if (a.accumulate) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const int n = n0 + (j >> 1) * 128 + qw * 32 + 16 * (j & 1) + c, k = k0 + (i >> 2) * 128 + pw * 64 + 16 * (i & 3) + p4;
-                    if (n < a.N && k < a.K) store_grad<TYPE, GRAD_TYPE>(a.dW, ((size_t)t.group * (size_t)a.N + (size_t)n) * (size_t)a.K + (size_t)k, acc[i][j], 1);
-                }
-            return false;
-        }
+    if (!a.accumulate) {
         constexpr int kFrags = GRAD_TYPE == kTypeF32 ? 2 : 4;
+        __syncthreads();
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int i0 = 0; i0 < 8; i0 += kFrags)
-                store_lines<TYPE, GRAD_TYPE>(a, t.group, n0 + (j >> 1) * 128 + qw * 32 + 16 * (j & 1), k0 + (i0 >> 2) * 128 + pw * 64 + 16 * (i0 & 3), mine, [&](int i) { return acc[i0 + i][j]; });
-        return n0 + 256 <= a.N && k0 + 256 <= a.K;
-    };
-
-    // ---- the tiles ----
-    if constexpr (GATHER) {
-        ask_numbers(0);
-        ask_numbers(1);
-        arrive(0);
+                store_grads<TYPE, GRAD_TYPE>(a, group, n0 + (j >> 1) * 128 + qw * 32 + 16 * (j & 1), k0 + (i0 >> 2) * 128 + pw * 64 + 16 * (i0 & 3), lds + wave * kStaging, [&](int i) { return acc[i0 + i][j]; });
+        return;
     }
-    const bool any = next_unit();
-    if (any) {
-        auto whole = [&](int number) {  // a stage's half tiles, from Q0 on
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int kind = (i + 3) & 3;
-                prepare(kind);
-                issue(kind, place(number + i));
-            }
-        };
-        whole(-1);
-        const bool two = next_unit();
-        if (two) whole(3);
-        arrive(two ? 6 : 2);
-        read_q(-1, k0);
-        arrive(two ? 6 : 2);
-        if (two) look(0);
-        else end = 3;
-        if (late) __builtin_amdgcn_s_barrier();
-    }
-    GradTiles of(a, pairs);
-    bool after = false;
-    while (of.next_tile()) {
+    for (int j = 0; j < 4; ++j) {
+        const int n = n0 + (j >> 1) * 128 + qw * 32 + 16 * (j & 1) + c;
+        if (n >= a.N) continue;
+        const size_t at = ((size_t)group * (size_t)a.N + (size_t)n) * (size_t)a.K;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[i][j] = (float4_t){0.f, 0.f, 0.f, 0.f};
-        for (int i = 0; i < of.stages; ++i) {
-            stage(after);
-            after = false;
+        for (int i = 0; i < 8; ++i) {
+            const int k = k0 + (i >> 2) * 128 + pw * 64 + 16 * (i & 3) + p4;
+            if (k < a.K) store_grad<TYPE, GRAD_TYPE>(a.dW, at + k, acc[i][j], a.accumulate);
         }
-        after = store(of) && of.stages > 0;
     }
-    if (any && !late) __builtin_amdgcn_s_barrier();
 }
 
 struct Wide {
-    static constexpr int kRows = 256, kCols = 256, kLds = 131072 + 1024 + 8 * kStaging;
-    static_assert(kLds <= 163840, "LDS of a compute unit");
+    static constexpr int kRows = 256, kCols = 256, kLds = 131072 + 1024;
     template <int TYPE, int GRAD_TYPE, bool GATHER>
     static hipError_t go(const GroupGradArgs &a, hipStream_t stream)
     {
@@ -440,9 +245,8 @@ struct Wide {
         const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kLds);
         if (e != hipSuccess) return e;
         const int cols = (a.K + kCols - 1) / kCols;
-        const long long pairs = (long long)((a.N + kRows - 1) / kRows) * cols, tiles = (pairs + kPlaceXcds - 1) / kPlaceXcds * kPlaceXcds * a.E;
-        if (tiles > 0x7FFFFFFF) return hipErrorInvalidValue;
-        const long long grid = tiles < kGradWorkgroups ? tiles : kGradWorkgroups;
+        const long long pairs = (long long)((a.N + kRows - 1) / kRows) * cols, grid = (pairs + kPlaceXcds - 1) / kPlaceXcds * kPlaceXcds * a.E;
+        if (grid * 512 > 0xFFFFFFFFll) return hipErrorInvalidValue;
         hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(512), kLds, stream, a, cols, (int)pairs);
         return hipGetLastError();
     }
@@ -497,12 +301,10 @@ auto with_form(int form, Use use)
 
 GroupTile plan_group_grad(int E, long long count, int N, int K)
 {
-    // The largest tiles where every workgroup has eight, or groups are so large that all have as many of each: as the tiles of a group have as many stages as the group has rows, few are uneven.
-    // Groups of 0.3 to 4 times the mean, us of 128 x 128 | 256 x 256 tiles: 4096 x 4096, 64 groups of 512 rows 1844 | 1462, 8 of 37 66 | 62; 2048 x 4096, 128 of 3 482 | 420; 1024 x 1024, 128 of 75
-    // 103 | 91; with fewer tiles, 2048 x 2048, 16 of 512 116 | 158, 16 of 100 68 | 66; 1024 x 1024, 64 of 512 119 | 171; one group, 8192 x 8192 x 8192 1193 | 1064.
-    (void)count;
-    const long long pairs = (long long)((N + 255) / 256) * ((K + 255) / 256);
-    const int form = pairs * E >= 8 * kGradWorkgroups || pairs >= 4 * kGradWorkgroups;
+    // The largest tiles where there are two for each compute unit and stages enough to run into the loop; us of 128 x 128 | 256 x 256 tiles, BF16, groups of 0.3 to 4 times the mean:
+    // 4096 x 4096, 64 groups of 512 rows 1744 | 1402, 8 of 37 58 | 71; 2048 x 2048, 16 of 128 46 | 43, 8 of 75 19 | 20; 1024 x 1024, 128 of 128 131 | 92, 128 of 75 77 | 79;
+    // with 256 tiles 1024 x 2048, 8 of 1024 50 | 50, 1024 x 1024, 16 of 200 22 | 24, with 128 2048 x 2048, 2 of 4096 81 | 98.
+    const int form = count / E >= 96 && (long long)E * ((N + 255) / 256) * ((K + 255) / 256) >= 512;
     return with_form(form, [&](auto f) { return GroupTile{form, f.kRows, f.kCols}; });
 }
 

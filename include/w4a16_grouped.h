@@ -7,8 +7,9 @@
  * row; a leading dimension (ld) is the values from a row to the next.  Rows are 16-byte aligned, so dimensions along rows and ld are multiples
  * of 8 (ld at most 2^21).  ids, offsets, rows and FP32 arrays need no more than their type's alignment, workspaces 256 bytes.  Calls only enqueue
  * work on `stream` (a hipStream_t, NULL = the default stream); none allocates, waits or keeps anything, so all may be captured into a HIP graph,
- * and calls on different streams may overlap, each with its own workspace and outputs.  No rows: W4A16_OK; nothing is launched
- * but what w4a16_grouped_gemm_grad and w4a16_lora_grad need to write their zeros, and w4a16_grouped_sort its offsets.
+ * and calls on different streams may overlap, each with its own workspace and outputs.  Outputs may not overlap inputs or each other, but where
+ * it is said.  No rows: W4A16_OK; nothing is launched but what w4a16_grouped_gemm_grad and w4a16_lora_grad need to write their zeros, and
+ * w4a16_grouped_sort its offsets.
  *
  * Errors: a w4a16_status; on any error nothing is launched.  Sums are FP32, with one rounding to the output's type; results are
  * bitwise reproducible for fixed arguments.
@@ -41,7 +42,7 @@ int w4a16_grouped_sort(const int32_t *ids, long long count, int E, int32_t *offs
  *   also the gradient of the first form's rows, with the gradients of its outputs as X.
  * Rows of Y that no group has are left as they are, or set to 0 with `fill` nonzero.  A row number outside of X stands for a row of zeros; offsets that
  * descend or leave the range make some rows' values undefined and touch no memory outside of the arguments.
- * E <= 1024, K <= 131072, N <= 2^20, count and x_rows < 2^30; without `rows` x_rows >= count.  Y may not overlap X or W.
+ * E <= 1024, K <= 131072, N <= 2^20, count and x_rows < 2^30; without `rows` x_rows >= count.
  */
 int w4a16_grouped_gemm(const void *X, int dtype, long long x_rows, long long ldx, const int32_t *rows, int top_k, const void *W, long long stride_w,
                        long long ldw, int transposed, const int32_t *offsets, int E, long long count, int N, int K, void *Y, long long ldy, int fill,
@@ -61,7 +62,7 @@ int w4a16_grouped_query_tile(int E, long long count, int N, int K, int transpose
 /*
  * Low-rank adapters beside a shared projection:  out[i] = Y[i] + s_a (X[i] A_a^T) B_a^T,  a = ids[i], in FP32 until the one rounding; rows whose id is
  * outside of 0 .. L - 1 have none: out[i] = Y[i].
- *   X [M, K], ldx;  Y and out [M, N], ldy and ldo (out may be Y, with the same ld, and may otherwise not overlap any input);  ids int32 [M]
+ *   X [M, K], ldx;  Y and out [M, N], ldy and ldo (out may be Y, with the same ld);  ids int32 [M]
  *   A [L, R, K], B [L, N, R], contiguous, R a multiple of 8, at most 128 (shorter adapters: rows of A and columns of B of zeros)
  *   scaling FP32 [L], or NULL: 1
  * L <= 1024, M <= 2^20, K and N <= 131072.  `workspace`: w4a16_lora_workspace_bytes, this call's own until its work is done.

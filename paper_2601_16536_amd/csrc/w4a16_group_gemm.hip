@@ -98,7 +98,7 @@ __global__ __launch_bounds__(512, 1) void group_gemm_wide_kernel(GroupGemmArgs a
     RowTile t;
     if (!find_row_tile<512>(a.offsets, a.E, groups, a.count, 256, cols, &t)) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int pw = wave >> 2, qw = wave & 3, c = lane & 15, p4 = (lane >> 4) * 4;
+    const int pw = wave >> 2, qw = wave & 3, c = lane & 15;
     const int n0 = t.col * 256, rows = min(256, t.end - t.row0);
     const size_t row_x = (size_t)a.ldx * 2, row_w = (size_t)a.ldw * 2;
     const uint8_t *const x = static_cast<const uint8_t *>(a.X) + (GATHER ? 0 : (size_t)t.row0 * row_x);

@@ -556,7 +556,8 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
 
 // ---- grads: dA[r, k] = sum over the adapter's rows of G[i][r] X[i, k];  dB[n, r] = sum of dY[i, n] H[i][r] ----
 //
-// A workgroup has 128 columns of X or dY and all of R; a wave 32 columns.  Stages of 64 rows through LDS, both operands read across: 128 columns, and the terms of G or H one behind
+// A workgroup has 128 columns of X or dY and all of R, a wave 32 columns; half of them up to rank 32 where there are few workgroups, as adapters' rows differ (4096 rows of four adapters,
+// K = N = 8192, rank 32: 51 -> 40 us; 250 rows of three, 4096 and 11008, rank 8, FP32 6.5 -> 5.3).  Bound by how X and dY come from memory, 134 MB in the first of these.  Stages of 64 rows through LDS, both operands read across: 128 columns, and the terms of G or H one behind
 // the other, each multiplied into the same sums.  FP16 X enters as two bfloat16 numbers, whose sum it is exactly (eight and three bits), because G may be beyond FP16's range.
 // The rows' numbers come to LDS two stages ahead, as in w4a16_group_grad.hip.
 struct GradSide {
@@ -571,26 +572,26 @@ struct GradArgs {
     int R;
 };
 
-template <int TYPE, int GRAD_TYPE, int RT>
+template <int TYPE, int GRAD_TYPE, int RT, int COLS>
 struct GradShape {
-    static constexpr int kTerms = GRAD_TYPE == kTypeF32 ? 3 : 2, kSpan = 16 * RT * kTerms, kBuffer = (128 + kSpan) * 128;
+    static constexpr int kTerms = GRAD_TYPE == kTypeF32 ? 3 : 2, kSpan = 16 * RT * kTerms, kBuffer = (COLS + kSpan) * 128;
     static constexpr int kDepth = kBuffer * 3 <= 80 * 1024 - 2048 ? 3 : 2, kLds = kDepth * kBuffer + 4 * 256;
     static_assert(kLds <= 163840 - 1024, "LDS of a compute unit");
 };
 
-template <int TYPE, int GRAD_TYPE, int RT>
+template <int TYPE, int GRAD_TYPE, int RT, int COLS>
 __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
 {
     typedef typename ActOf<TYPE>::type Act;
-    typedef GradShape<TYPE, GRAD_TYPE, RT> Sh;
-    constexpr int kWaves = 4, kRp = 16 * RT, kTerms = Sh::kTerms, kDepth = Sh::kDepth, kParts = TYPE == kTypeF16 ? 2 : 1;
-    typedef AcrossTile<128, kWaves> PTile;
+    typedef GradShape<TYPE, GRAD_TYPE, RT, COLS> Sh;
+    constexpr int kWaves = 4, J = COLS / 64, kRp = 16 * RT, kTerms = Sh::kTerms, kDepth = Sh::kDepth, kParts = TYPE == kTypeF16 ? 2 : 1;
+    typedef AcrossTile<COLS, kWaves> PTile;
     typedef AcrossTile<kRp, kWaves> QTile;  // of one term
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, p4 = (lane >> 4) * 4;
     const bool of_a = (int)blockIdx.x < a.side[0].blocks;
     const GradSide s = of_a ? a.side[0] : a.side[1];
-    const int adapter = (int)blockIdx.y, n0 = ((int)blockIdx.x - (of_a ? 0 : a.side[0].blocks)) * 128;
+    const int adapter = (int)blockIdx.y, n0 = ((int)blockIdx.x - (of_a ? 0 : a.side[0].blocks)) * COLS;
     const int begin = __builtin_amdgcn_readfirstlane(a.offsets[adapter]), count = __builtin_amdgcn_readfirstlane(a.offsets[adapter + 1]) - begin;
     const int stages = (count + kGroupStage - 1) / kGroupStage;
     const size_t row_x = (size_t)s.ldx * 2;
@@ -598,9 +599,9 @@ __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
     const uint8_t *const x = reinterpret_cast<const uint8_t *>(s.X), *const terms = reinterpret_cast<const uint8_t *>(s.terms);
     int *const list = reinterpret_cast<int *>(lds + kDepth * Sh::kBuffer);
 
-    float4_t acc[2][RT];  // [16 columns][16 of R]
+    float4_t acc[J][RT];  // [16 columns][16 of R]
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < J; ++i)
 #pragma unroll
         for (int u = 0; u < RT; ++u) acc[i][u] = (float4_t){0.f, 0.f, 0.f, 0.f};
     auto ask_rows = [&](int stage) {
@@ -649,10 +650,10 @@ __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
         const uint8_t *const tile = lds + i % kDepth * Sh::kBuffer;
 #pragma unroll
         for (int step = 0; step < 2; ++step) {
-            uint4_t xv[kParts][2];
+            uint4_t xv[kParts][J];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint4_t v = PTile::read(tile, lane, wave * 32 + 16 * j, step);
+            for (int j = 0; j < J; ++j) {
+                const uint4_t v = PTile::read(tile, lane, wave * 16 * J + 16 * j, step);
                 if constexpr (TYPE == kTypeBF16) {
                     xv[0][j] = v;
                 } else {
@@ -673,7 +674,7 @@ __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
 #pragma unroll
                     for (int part = 0; part < kParts; ++part)
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
+                        for (int j = 0; j < J; ++j)
                             acc[j][u] = decltype(for_a)::value ? ActBF16::mfma(ActBF16::x_operand(xv[part][j]), ActBF16::x_operand(g), acc[j][u])
                                              : ActBF16::mfma(ActBF16::x_operand(g), ActBF16::x_operand(xv[part][j]), acc[j][u]);
                 }
@@ -687,10 +688,10 @@ __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
         else *reinterpret_cast<uint2_t *>(static_cast<uint16_t *>(s.grad) + at) = to_16bit4<Act>(v);
     };
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < J; ++j)
 #pragma unroll
         for (int u = 0; u < RT; ++u) {
-            const int n = n0 + wave * 32 + 16 * j, r = 16 * u;
+            const int n = n0 + wave * 16 * J + 16 * j, r = 16 * u;
             if (of_a) {  // dA [R, K]: r + c, columns n + p4 ..
                 if (r + c < a.R && n + p4 < s.width) put(((size_t)adapter * (size_t)a.R + (size_t)(r + c)) * (size_t)s.width + (size_t)(n + p4), acc[j][u]);
             } else {  // dB [N, R]: column n + c, r + p4 ..
@@ -894,12 +895,21 @@ hipError_t launch_lora_grad(const LoraArgs &a, hipStream_t stream)
                 if (err != hipSuccess) return err;
             }
             GradArgs g = {};
-            g.side[0] = {static_cast<const uint16_t *>(a.X), m.side[1].terms, a.dA, a.ldx, a.K, (a.K + 127) / 128};
-            g.side[1] = {static_cast<const uint16_t *>(a.Y), m.side[0].terms, a.dB, a.ldy, a.N, (a.N + 127) / 128};
+            g.side[0] = {static_cast<const uint16_t *>(a.X), m.side[1].terms, a.dA, a.ldx, a.K, 0};
+            g.side[1] = {static_cast<const uint16_t *>(a.Y), m.side[0].terms, a.dB, a.ldy, a.N, 0};
             g.offsets = offsets, g.order = order, g.R = a.R;
-            const dim3 grid((unsigned)(g.side[0].blocks + g.side[1].blocks), (unsigned)a.L);
-            return wide ? enqueue(&lora_grads_kernel<T, kTypeF32, RT>, grid, 256, GradShape<T, kTypeF32, RT>::kLds, stream, g)
-                        : enqueue(&lora_grads_kernel<T, T, RT>, grid, 256, GradShape<T, T, RT>::kLds, stream, g);
+            auto grads = [&](auto grad_type, auto columns) {
+                constexpr int kGrad = decltype(grad_type)::value, kCols = decltype(columns)::value;
+                for (GradSide &side : g.side) side.blocks = (side.width + kCols - 1) / kCols;
+                return enqueue(&lora_grads_kernel<T, kGrad, RT, kCols>, dim3((unsigned)(g.side[0].blocks + g.side[1].blocks), (unsigned)a.L), 256,
+                               GradShape<T, kGrad, RT, kCols>::kLds, stream, g);
+            };
+            constexpr std::integral_constant<int, 128> k128{};
+            constexpr std::integral_constant<int, 64> k64{};
+            if constexpr (RT <= 2) {  // (beyond, the terms would be most of what a stage brings)
+                if ((long long)(a.K + a.N) / 128 * a.L <= 1024) return wide ? grads(std::integral_constant<int, kTypeF32>{}, k64) : grads(type, k64);
+            }
+            return wide ? grads(std::integral_constant<int, kTypeF32>{}, k128) : grads(type, k128);
         });
     });
 }

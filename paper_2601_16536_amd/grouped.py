@@ -84,7 +84,7 @@ def sort_workspace_bytes(count: int, E: int) -> int:
 def sort(ids, E: int, out=None, workspace=None, stream=None):
     """ids int32 (any shape; 0 .. E - 1, anything else: no group) -> (offsets [E + 1], order [count], place [count]), all int32: group e has the places
     offsets[e] .. offsets[e + 1] - 1, order lists the ids' flat numbers by group, in their order inside one and those without a group last, and place
-    is its inverse.  `out`: the three to fill.  `workspace`: as in moe.experts, where sort_workspace_bytes is not 0."""
+    is its inverse.  `out`: the three to fill, none of them ids.  `workspace`: as in moe.experts, where sort_workspace_bytes is not 0."""
     import torch
     check_ints(ids, "ids")
     count = ids.numel()
@@ -164,7 +164,8 @@ def gemm(X, W, offsets, rows=None, top_k: int = 1, transposed: bool = False, out
 
 def gemm_grad(dY, X, offsets, rows=None, top_k: int = 1, dtype=None, out=None, accumulate: bool = False, stream=None):
     """dW [E, N, K], dW_e = the sum over the group's rows i of dY[i]^T x_i, x_i as in gemm; zeros for a group without rows.  dY [count, N] and X of the same
-    type; dW of `dtype` (X's by default, or float32, or out's type).  `accumulate`: added to what `out` holds (contiguous)."""
+    type; dW of `dtype` (X's by default, or float32, or out's type).  `accumulate`: added to what `out` holds
+    (contiguous, and apart from dY and X)."""
     import torch
     code = mx.type_code(X.dtype, False)
     x_rows, K, ldx = matrix(X, "X")

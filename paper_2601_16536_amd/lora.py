@@ -65,7 +65,7 @@ def _check(X, A, B, ids, scaling, other, name: str):
 
 def add(Y, X, A, B, ids, scaling=None, out=None, workspace=None, stream=None):
     """Y + scaling[a] (x A_a^T) B_a^T, a = ids[row], [M, N]; rows without an adapter as they are.  Y, X [M, K], A and B float16 or all bfloat16, Y and X with a row
-    stride if need be; scaling float32 [L] (by default 1).  The result is a new tensor, or `out`, which may be Y itself.  `workspace`: as in moe.experts,
+    stride if need be; scaling float32 [L] (by default 1).  The result is a new tensor, or `out`, which may be Y itself and may not overlap X.  `workspace`: as in moe.experts,
     of workspace_bytes(M, L, R, K, N)."""
     code, M, L, R, K, N, ldx, ldy = _check(X, A, B, ids, scaling, Y, "Y")
     out, ldo = mx._out_matrix(out, M, N, X, X.dtype)
@@ -81,7 +81,7 @@ def add(Y, X, A, B, ids, scaling=None, out=None, workspace=None, stream=None):
 def grad(dY, X, A, B, ids, scaling=None, dX=None, dtype=None, out=None, workspace=None, stream=None):
     """(dX + scaling[a] (dy B_a) A_a, dA [L, R, K], dB [L, N, R]) for add's arguments and the gradient dY [M, N] of its result.  dX [M, K]: what the shared
     projection passed back (by default 0).  dA and dB of `dtype`: X's by default, or float32; zeros for an adapter without rows.  `out`: the three to fill, the first
-    of which may be dX itself.  `workspace`: of workspace_bytes(M, L, R, K, N, grad=True)."""
+    of which may be dX itself; none may overlap dY, X, A or B.  `workspace`: of workspace_bytes(M, L, R, K, N, grad=True)."""
     import torch
     code, M, L, R, K, N, ldx, ldy = _check(X, A, B, ids, scaling, dY, "dY")
     lddx = 0

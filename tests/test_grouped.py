@@ -478,10 +478,12 @@ def test_rows_beyond_two_and_four_gib(grouped):
 
 
 @gpu
-def test_replayed_graphs_and_other_streams(grouped):
+@pytest.mark.parametrize("T,N,K,tile", [(50, 136, 264, 16), (3000, 2056, 2064, 256)])
+def test_replayed_graphs_and_other_streams(grouped, T, N, K, tile):
     import torch
     gen = generator(8)
-    T, E, top_k, N, K = 50, 8, 2, 136, 264
+    E, top_k = 8, 2
+    assert grouped.query_tile(E, T * top_k, N, K)[0] in (tile, 64) and grouped.query_tile(E, T * top_k, N, K, grad=True)[0] == max(tile, 128)
     ids = torch.randint(-1, E, (T, top_k), generator=gen, device="cuda", dtype=torch.int32)
     X, W = values(gen, (T, K), "bfloat16"), values(gen, (E, N, K), "bfloat16")
 

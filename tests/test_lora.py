@@ -260,6 +260,14 @@ def test_grad_of_every_rank(lora, R, K, N, grads):
 
 
 @gpu
+@pytest.mark.parametrize("grads", ["same", "float32"])
+@pytest.mark.parametrize("R,kind", [(8, "float16"), (32, "bfloat16")])
+def test_grad_of_many_adapters(lora, R, kind, grads):
+    """So many columns of gradients that a workgroup has 128 of them at every rank."""
+    check_grad(lora, 700, 130, R, 584, 600, kind, "mixed", grads)
+
+
+@gpu
 def test_strides(lora):
     import torch
     M, L, R, K, N = 75, 3, 24, 136, 200

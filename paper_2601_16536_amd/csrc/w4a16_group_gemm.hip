@@ -5,7 +5,10 @@
 namespace w4a16 {
 namespace {
 
-// TP columns of Y (rows of W, or its columns where it is transposed) by TQ rows, of PW x QW waves.
+// TP columns of Y (rows of W, or its columns where it is transposed) by TQ rows, of PW x QW waves; DEPTH stages of 64 values of K in LDS.
+//
+// Few rows to a group: the weights are the bytes, each read once, and what counts is how many are on their way (four stages of 128 x 64 values, two workgroups to a compute unit).  One token, top 8 of 64
+// experts, K = N = 4096, BF16: 268 MB, 52 us, 5.2 TB/s; 48 tokens of 128 experts, K = 2048, N = 4096, FP16: 1.6 GB, 280 us, 5.8 TB/s.  (K shared out among workgroups: not needed, as 8 groups are 256 workgroups.)
 template <int TYPE, bool ACROSS, bool GATHER, int TP, int TQ, int PW, int QW, int DEPTH, int PER_CU>
 __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_gemm_kernel(GroupGemmArgs a, int groups, int cols)
 {
@@ -87,7 +90,9 @@ __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_gemm_kernel(GroupG
     }
 }
 
-// 256 x 256, eight waves: the loop of half tiles.
+// 256 x 256, eight waves: the loop of half tiles.  Bound by the matrix instructions: one group of 8192 rows, 8192 x 8192 BF16 717 us, 1.53 PFLOP/s.  With 64 groups of 512 rows (0.3 to 4 times that),
+// 4096 x 4096, 965 us, 1.14 PFLOP/s: a fifth of the tiles' rows are behind a group's end, and between two tiles are some 8 us without products.  Waves whose rows are behind the end leave their products
+// out (16384 rows of 128 groups, 2048 x 4096 555 -> 494 us); in a loop of its own, as the test costs the whole tiles 4 %.
 template <int TYPE, bool ACROSS, bool GATHER>
 __global__ __launch_bounds__(512, 1) void group_gemm_wide_kernel(GroupGemmArgs a, int groups, int cols)
 {
@@ -235,7 +240,10 @@ GroupTile plan_group_gemm(int E, long long count, int N, int K, int transposed)
 {
     (void)K, (void)transposed;
     const long long average = count / E;
-    const int form = average <= 8 ? 0 : average <= 64 ? 1 : average < 96 || count * N < 128ll * 65536 ? 2 : 3;
+    // A tile's rows are the group's, so far as there are any: the weights are to be read once, and rows behind a group's end cost nothing while the weights are what takes the time.  us of 128 x 128 |
+    // 128 columns x 64 rows | 256 x 256: 64 groups of 73 rows, 2048 x 4096 251 | 233 | 244, transposed 306 | 292 | 268; of 70, 2048 x 2048 transposed 149 | 159 | 115; 128 of 128, 4096 x 2048
+    // 608 | 621 | 477; 8 of 90, 14336 x 4096 203 | 242 | 197; where there are few tiles, 64 of 130, 1024 x 1024 50 | 52 | 55, 8 of 75, 1000 x 2056 27 | - | 43, but 8 of 1024, 1024 x 2048 59 | 61 | 50.
+    const int form = average <= 8 ? 0 : average <= 64 ? 1 : count * N < 128ll * 65536 ? 2 : 3;
     return with_form(form, [&](auto f) { return GroupTile{form, f.kRows, f.kCols}; });
 }
 

@@ -399,10 +399,23 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
     // Of many rows, the operands that H gives come to LDS, for all of the workgroup's waves: read by each of them from memory they are three times base's bytes.
     constexpr int kPieces = Terms::kTerms * RP / 8, kRow = Terms::kTerms * RP * 2 + 16;  // of a row; its bytes in LDS, so that sixteen rows lie on all banks
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int m_each = TR / 16 / (int)gridDim.z, m_begin = (int)blockIdx.z * m_each, m_end = min(m_begin + m_each, (count + 15) / 16);  // the workgroup's part of the tile, by sixteen rows
+    if (m_begin >= m_end) return;
     if (TR != 16 && product) {
-        for (int i = (int)threadIdx.x; i < TR * kPieces; i += (int)blockDim.x) {
-            const int row = i / kPieces, piece = i % kPieces;
-            if (row < count) *reinterpret_cast<uint4_t *>(lds + row * kRow + piece * 16) = *reinterpret_cast<const uint4_t *>(a.operand + (size_t)rows[row] * (kPieces * 8) + piece * 8);
+        constexpr int kAtOnce = 4;  // loads on their way
+        const int from = m_begin * 16 * kPieces, to = min(m_end * 16, count) * kPieces;
+        for (int i0 = from + (int)threadIdx.x; i0 < to; i0 += (int)blockDim.x * kAtOnce) {
+            uint4_t v[kAtOnce];
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {  // (past the last: the last again)
+                const int i = min(i0 + j * (int)blockDim.x, to - 1);
+                v[j] = *reinterpret_cast<const uint4_t *>(a.operand + (size_t)rows[i / kPieces] * (kPieces * 8) + i % kPieces * 8);
+            }
+#pragma unroll
+            for (int j = 0; j < kAtOnce; ++j) {
+                const int i = min(i0 + j * (int)blockDim.x, to - 1);
+                *reinterpret_cast<uint4_t *>(lds + i / kPieces * kRow + i % kPieces * 16) = v[j];
+            }
         }
         __syncthreads();
     }
@@ -458,16 +471,16 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
                 const int r = 32 * g + 8 * p;
                 const float *from = a.H + (size_t)row * RP + (r < a.R ? r : 0);
                 float4_t h0 = *reinterpret_cast<const float4_t *>(from), h1 = *reinterpret_cast<const float4_t *>(from + 4);
-                for (int s = 1; s < a.slices; s += 4) {
-                    float4_t u[4][2];
+                for (int s = 1; s < a.slices; s += 8) {
+                    float4_t u[8][2];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
+                    for (int j = 0; j < 8; ++j) {
                         const float *const of = from + (size_t)min(s + j, a.slices - 1) * next;
                         u[j][0] = *reinterpret_cast<const float4_t *>(of);
                         u[j][1] = *reinterpret_cast<const float4_t *>(of + 4);
                     }
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < 8; ++j)
                         if (s + j < a.slices) {
                             h0 += u[j][0];
                             h1 += u[j][1];
@@ -504,11 +517,11 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
         }
     };
     Rows ahead;
-    load(ahead, 0);
-    for (int m = 0; m * 16 < count; ++m) {
+    load(ahead, m_begin);
+    for (int m = m_begin; m < m_end; ++m) {
         Rows now = ahead;
         Piece(&y)[4] = now.y;
-        if (TR != 16 && (m + 1) * 16 < count) load(ahead, m + 1);
+        if (TR != 16 && m + 1 < m_end) load(ahead, m + 1);
         if (TR != 16 && product) {
             const uint8_t *const from = lds + min(16 * m + c, count - 1) * kRow;
 #pragma unroll
@@ -738,13 +751,24 @@ int slices_of(long long tiles, int K)
     return s < 1 ? 1 : (int)s;
 }
 // Of many rows, where the slices of a tile run on different XCDs: eight or sixteen slices have each XCD read its share of the adapters only (M = 2048, K = 8192, rank 64, five adapters).
+// Short ones, of 128 values, where there would be fewer workgroups than compute units.
 int many_slices(long long tiles, int K)
 {
     const int most = K / 512;
-    if (tiles <= 32 && most >= 16) return 16;
-    if (tiles <= 160 && most >= 8) return 8;
-    const long long s = tiles ? 512 / tiles : 1;
-    return s < 1 || most < 1 ? 1 : (int)(s < most ? s : most);
+    long long s;
+    if (tiles <= 32 && most >= 16) s = 16;
+    else if (tiles <= 160 && most >= 8) s = 8;
+    else {
+        s = tiles ? 512 / tiles : 1;
+        if (s > most) s = most;
+    }
+    if (s * tiles < 256) {
+        long long more = K / 128;
+        if (tiles && more > 256 / tiles) more = 256 / tiles;
+        if (more > 16) more = 16;
+        if (s < more) s = more;
+    }
+    return s < 1 ? 1 : (int)s;
 }
 int slice_length(int K, int slices) { return ((K + slices - 1) / slices + 127) / 128 * 128; }
 long long few_tiles(int M, int L) { return most_row_tiles(L + 1, M, 16); }
@@ -807,7 +831,8 @@ hipError_t expand(const LoraArgs &a, const Lists &l, const ExpandArgs &x, bool a
 {
     const long long tiles = tr == 16 ? few_tiles(a.M, a.L) : many_tiles(a.M, a.L);
     const int width = a.R <= 64 ? 128 : 64, blocks = (x.N + width - 1) / width, waves = tiles * blocks >= 2048 ? 4 : 1;
-    const dim3 grid((unsigned)((blocks + waves - 1) / waves), (unsigned)tiles);
+    // A tile of 64 rows in four parts where there are few: one wave after the other takes as long as its loads do (363 rows of one adapter, rank 104, K = 1920, N = 1600: 22.7 -> 6.3 us).
+    const dim3 grid((unsigned)((blocks + waves - 1) / waves), (unsigned)tiles, tr != 16 && waves == 1 ? 4 : 1);
     return with_type(a.type, [&](auto type) {
         return with_rank(a.R, [&](auto rt) {
             constexpr int T = decltype(type)::value, RT = decltype(rt)::value, G = RT < 2 ? 1 : RT / 2, RP = 16 * RT;

@@ -8,7 +8,7 @@ namespace {
 // TP columns of Y (rows of W, or its columns where it is transposed) by TQ rows, of PW x QW waves; DEPTH stages of 64 values of K in LDS.
 //
 // Few rows to a group: the weights are the bytes, each read once, and what counts is how many are on their way (four stages of 128 x 64 values, two workgroups to a compute unit).  One token, top 8 of 64
-// experts, K = N = 4096, BF16: 268 MB, 52 us, 5.2 TB/s; 48 tokens of 128 experts, K = 2048, N = 4096, FP16: 1.6 GB, 280 us, 5.8 TB/s.  (K shared out among workgroups: not needed, as 8 groups are 256 workgroups.)
+// experts, K = N = 4096, BF16: 268 MB, 52 us, 5.2 TB/s; 48 tokens of 128 experts, K = 2048, N = 4096, FP16: 1.6 GB, 280 us, 5.8 TB/s.
 template <int TYPE, bool ACROSS, bool GATHER, int TP, int TQ, int PW, int QW, int DEPTH, int PER_CU>
 __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_gemm_kernel(GroupGemmArgs a, int groups, int cols)
 {
@@ -230,6 +230,8 @@ auto with_form(int form, Use use)
     case 0: return use(Form<128, 16, 4, 1, 4, 2>{});
     case 1: return use(Form<128, 64, 4, 1, 3, 2>{});
     case 2: return use(Form<128, 128, 2, 2, 2, 2>{});
+    case 4: return use(Form<32, 16, 2, 1, 8, 2>{});
+    case 5: return use(Form<32, 64, 1, 4, 6, 2>{});
     default: return use(Wide{});
     }
 }
@@ -239,10 +241,16 @@ auto with_form(int form, Use use)
 GroupTile plan_group_gemm(int E, long long count, int N, int K, int transposed)
 {
     (void)K, (void)transposed;
-    const long long average = count / E;
+    const long long groups = count < E ? (count ? count : 1) : E, average = count / E, blocks = (N + 127) / 128;
+    auto tiles = [&](int rows) { return groups * ((count / groups + rows - 1) / rows) * blocks; };  // of 128 columns
     // A tile's rows are the group's, so far as there are any: the weights are to be read once, and rows behind a group's end cost nothing while the weights are what takes the time.  us of 128 x 128 |
     // 128 columns x 64 rows | 256 x 256: 64 groups of 73 rows, 2048 x 4096 251 | 233 | 244, transposed 306 | 292 | 268; of 70, 2048 x 2048 transposed 149 | 159 | 115; 128 of 128, 4096 x 2048
     // 608 | 621 | 477; 8 of 90, 14336 x 4096 203 | 242 | 197; where there are few tiles, 64 of 130, 1024 x 1024 50 | 52 | 55, 8 of 75, 1000 x 2056 27 | - | 43, but 8 of 1024, 1024 x 2048 59 | 61 | 50.
+    // Few tiles: columns by 32 and more stages on their way, as a workgroup alone is bound by the way of a stage.  us of 128 columns x 16 rows | 128 x 64 | 128 x 128 | 32 x 16 | 32 x 64: 2 groups of 28 rows,
+    // 576 x 5776 32 | 34 | 63 | 15 | 18; 4 of 4, 2048 x 4096 21 | 27 | 49 | 14 | 15; 4 of 30, 4096 x 4096 50 | 42 | 62 | 45 | 35; 8 of 75, 1000 x 2056
+    // 25 | 19 | 27 | 24 | 17, transposed 24 | 31 | 38 | 36 | 23; but 8 of one, 4096 x 4096, weights from memory 51 | - | - | 55, 6 of 50, 4096 x 4096 70 | 49 | 67 | 77 | 59.
+    if (average <= 16 && tiles(16) < 256) return with_form(4, [&](auto f) { return GroupTile{4, f.kRows, f.kCols}; });
+    if (tiles(64) <= 128) return with_form(5, [&](auto f) { return GroupTile{5, f.kRows, f.kCols}; });
     const int form = average <= 8 ? 0 : average <= 64 ? 1 : count * N < 128ll * 65536 ? 2 : 3;
     return with_form(form, [&](auto f) { return GroupTile{form, f.kRows, f.kCols}; });
 }

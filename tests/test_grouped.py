@@ -261,6 +261,18 @@ def test_gemm_of_every_length(grouped, sizes, N, K, transposed):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("gather", [False, True])
 @pytest.mark.parametrize("transposed", [False, True])
+@pytest.mark.parametrize("K", [8, 328, 1032])
+@pytest.mark.parametrize("sizes,N,tile", [([1, 0, 2] * 40, 400, (16, 128)), ([20, 0, 64, 65, 1, 33] * 6, 520, (64, 128)), ([100, 0, 129, 65, 128, 127, 300, 1, 200, 90] * 2, 520, (128, 128)),
+                                          ([3, 0, 17, 1], 72, (16, 32)), ([37, 0, 64, 65, 130], 264, (64, 32))], ids=lambda v: "" if isinstance(v, list) else None)
+def test_gemm_in_every_tile(grouped, sizes, N, tile, K, transposed, gather, kind):
+    assert grouped.query_tile(len(sizes), sum(sizes) + 7, N, K, transposed) == tile
+    run_group_case(grouped, sizes, N, K, kind, transposed, gather, 14, 3, 4, "K %d" % K)
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("transposed", [False, True])
 @pytest.mark.parametrize("K", [8, 64, 120, 128, 192, 256, 328, 448, 520, 1032])
 def test_gemm_in_the_largest_tiles(grouped, K, transposed, gather, kind):
     """From one stage of 64 values to seventeen, whole and not; rows and columns that end inside a tile."""

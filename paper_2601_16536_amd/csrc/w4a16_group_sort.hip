@@ -4,7 +4,7 @@
 // earlier chunks have of a pair's group, what earlier waves have, what earlier lanes have.  Up to 4096 pairs one workgroup places all: one launch.  Up to 65536, chunks of 1024: one launch
 // counts them, and each workgroup of a second one sums over their counts by itself.  Beyond, chunks of 4096, with a launch in between that sums.
 // Bound by latency, not by bytes (32768 pairs: 0.4 MB): what costs is the chain of a load, a count, a sum and a store, and the launches: up to 1024 pairs
-// 3.2 us, 4096 pairs 5.1 us, 32768 pairs of 64 groups 2.6 + 7.8 us (in one launch, whose workgroups counted all pairs ahead of theirs by themselves, 16.7 us).
+// 3.2 us, 4096 pairs 5.1 us, 32768 pairs of 256 groups 2.6 + 7.8 us (in one launch, whose workgroups counted all pairs ahead of theirs by themselves, 16.7 us).
 // All sums are of whole numbers: the order of the additions does not show.
 #include "w4a16_group_device.h"
 

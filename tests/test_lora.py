@@ -260,6 +260,21 @@ def test_grad_of_every_rank(lora, R, K, N, grads):
 
 
 @gpu
+@pytest.mark.parametrize("M", [4096, 4097, 70000])
+def test_many_rows(lora, M):
+    """The rows' sort has another form from 4097 and from 65537 rows on."""
+    check_add(lora, M, 5, 8, 16, 24, "bfloat16", "mixed")
+    check_grad(lora, M, 5, 8, 16, 24, "float16", "mixed")
+
+
+@gpu
+@pytest.mark.parametrize("M,L,R,K,N", [(363, 1, 104, 1920, 1600), (363, 40, 104, 1920, 264), (2000, 3, 64, 264, 8200), (2000, 3, 128, 264, 4104), (2000, 3, 16, 264, 16392)])
+def test_add_in_parts_and_whole(lora, M, L, R, K, N):
+    """Tiles of 64 rows that the expanding product takes in four parts (up to 2047 waves), and whole."""
+    check_add(lora, M, L, R, K, N, "bfloat16", "mixed")
+
+
+@gpu
 @pytest.mark.parametrize("grads", ["same", "float32"])
 @pytest.mark.parametrize("R,kind", [(8, "float16"), (32, "bfloat16")])
 def test_grad_of_many_adapters(lora, R, kind, grads):

@@ -293,7 +293,8 @@ struct Form {
 template <class Use>
 auto with_form(int form, Use use)
 {
-    if (form) return use(Wide{});
+    if (form == 1) return use(Wide{});
+    if (form == 2) return use(Form<64, 64, 1, 4, 4, 2>{});
     return use(Form<128, 128, 2, 2, 2, 2>{});
 }
 
@@ -304,6 +305,9 @@ GroupTile plan_group_grad(int E, long long count, int N, int K)
     // The largest tiles where there are two for each compute unit and stages enough to run into the loop; us of 128 x 128 | 256 x 256 tiles, BF16, groups of 0.3 to 4 times the mean:
     // 4096 x 4096, 64 groups of 512 rows 1744 | 1402, 8 of 37 58 | 71; 2048 x 2048, 16 of 128 46 | 43, 8 of 75 19 | 20; 1024 x 1024, 128 of 128 131 | 92, 128 of 75 77 | 79;
     // with 256 tiles 1024 x 2048, 8 of 1024 50 | 50, 1024 x 1024, 16 of 200 22 | 24, with 128 2048 x 2048, 2 of 4096 81 | 98.
+    // Few tiles: 64 x 64 with more stages on their way, as a workgroup alone is bound by the way of a stage; 128 x 128 | 64 x 64: one group of 8192 rows, 512 x 512 123 | 81, 2 of 4096, 1024 x 1024
+    // 68 | 47, 8 of 300, 512 x 512 9.1 | 7.1, but 4 of 300, 1024 x 1024 8.8 | 10.6.
+    if ((long long)E * ((N + 127) / 128) * ((K + 127) / 128) <= 128) return with_form(2, [&](auto f) { return GroupTile{2, f.kRows, f.kCols}; });
     const int form = count / E >= 96 && (long long)E * ((N + 255) / 256) * ((K + 255) / 256) >= 512;
     return with_form(form, [&](auto f) { return GroupTile{form, f.kRows, f.kCols}; });
 }
@@ -313,7 +317,7 @@ hipError_t launch_group_grad(const GroupGradArgs &args, hipStream_t stream)
     GroupGradArgs a = args;
     a.divide = Divisor(a.rows ? a.top_k : 1);
     GroupTile t = plan_group_grad(a.E, a.count, a.N, a.K);
-    if (t.form && a.rows && (long long)a.x_rows * a.ldx * 2 >= (long long)(kOutOfRange - 1)) t.form = 0;  // (its gathered rows are at 32-bit offsets)
+    if (t.form == 1 && a.rows && (long long)a.x_rows * a.ldx * 2 >= (long long)(kOutOfRange - 1)) t.form = 0;  // (its gathered rows are at 32-bit offsets)
     return with_form(t.form, [&](auto f) { return f.launch(a, stream); });
 }
 

@@ -387,6 +387,23 @@ def test_gemm_grad_of_every_width(grouped, sizes, N, K):
 @pytest.mark.parametrize("kind", KINDS)
 @pytest.mark.parametrize("grads", ["same", "float32"])
 @pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("N,K,tile", [(136, 328, 64), (1000, 520, 128)])
+def test_gemm_grad_in_the_smaller_tiles(grouped, N, K, tile, gather, grads, kind):
+    import torch
+    sizes = [100, 0, 129, 65, 128, 127, 700, 1]
+    assert grouped.query_tile(len(sizes), sum(sizes) + 7, N, K, grad=True) == (tile, tile)
+    X, _, offsets, rows, top_k = group_case(grouped, sizes, 8, K, kind, False, gather, 51, 3, 4)
+    dY = values(generator(52), (len(X) if rows is None else len(rows), N), kind)
+    kw = {} if rows is None else {"rows": ints(rows), "top_k": top_k}
+    dtype = X.dtype if grads == "same" else torch.float32
+    ref, terms, n = go.gemm_grad(exact(dY), exact(X), offsets, rows, top_k)
+    compare(grouped.gemm_grad(dY, X, ints(offsets), dtype=dtype, **kw), ref, tolerance(dtype, ref, terms, n[:, None, None]), "N %d K %d" % (N, K))
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("grads", ["same", "float32"])
+@pytest.mark.parametrize("gather", [False, True])
 @pytest.mark.parametrize("sizes", [[1, 63, 64, 65, 128, 500, 0, 129], [191, 192, 193, 0, 256, 257, 2, 3], [448, 320, 319, 321, 577, 640, 0, 8], [0, 0, 0, 5, 0, 0, 0, 0],
                                    [1, 0, 64, 65, 3, 0, 0, 16]])
 def test_gemm_grad_in_the_largest_tiles(grouped, sizes, gather, grads, kind):
@@ -495,7 +512,7 @@ def test_replayed_graphs_and_other_streams(grouped, T, N, K, tile):
     import torch
     gen = generator(8)
     E, top_k = 8, 2
-    assert grouped.query_tile(E, T * top_k, N, K)[0] in (tile, 64) and grouped.query_tile(E, T * top_k, N, K, grad=True)[0] == max(tile, 128)
+    assert grouped.query_tile(E, T * top_k, N, K)[0] in (tile, 64) and grouped.query_tile(E, T * top_k, N, K, grad=True)[0] == max(tile, 64)
     ids = torch.randint(-1, E, (T, top_k), generator=gen, device="cuda", dtype=torch.int32)
     X, W = values(gen, (T, K), "bfloat16"), values(gen, (E, N, K), "bfloat16")
 

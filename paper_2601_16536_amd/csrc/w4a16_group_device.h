@@ -333,6 +333,7 @@ __device__ __forceinline__ void group_product(float4_t (&acc)[PI][QI], uint8_t *
 // other one reads.  LDS has eight half tiles; that of phase f is free once both have read it, and number f + 8 is asked for in phase f + 1: seven phases ahead of its use,
 // the last six on their way behind every wait.
 // fetch(kind, stage, to, last, steady): the loads of a half tile, kind = number mod 4; with last the stage may reach past the sum's end; steady (a type): in the middle of the loop.
+// q_there: rows of Q that there are; without ALL a wave leaves out the products of a half of Q where its part of it is behind them.
 template <class Act, class Tile0, class Tile1, bool ALL, class Fetch>
 __device__ __forceinline__ void group_product_wide(float4_t (&acc)[8][4], uint8_t *lds, int pw, int qw, int q_there, int stages, int whole, Fetch fetch)
 {

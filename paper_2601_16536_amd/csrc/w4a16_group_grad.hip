@@ -130,9 +130,9 @@ __global__ __launch_bounds__(64 * PW * QW, PER_CU) void group_grad_kernel(GroupG
 }
 
 // 256 x 256, eight waves, a workgroup to a compute unit: the loop of half tiles (group_product_wide in w4a16_group_device.h).
-// 4096 tokens, top 8 of 64 experts, K = N = 4096, BF16: 1490 us, rows as they are 1380; one group of 8192, 8192 x 8192 784.  A workgroup that runs on from tile to tile, the next one's first stages on their way while this one's
-// results are stored, took 1563, 1449 and 1047:
-// what a stage needs to know about where it is costs more than the 9 us between two tiles.
+// 4096 tokens, top 8 of 64 experts, K = N = 4096, BF16: 1490 us, rows as they are 1380; one group of 8192, 8192 x 8192 784.
+// A workgroup that runs on from tile to tile, the next one's first stages on their way while this one's results are stored, took 1563, 1449 and 1047: what a stage needs to know about where it is
+// costs more than the 9 us between two tiles.
 template <int TYPE, int GRAD_TYPE, bool GATHER>
 __global__ __launch_bounds__(512, 1) void group_grad_wide_kernel(GroupGradArgs a, int cols, int pairs)
 {

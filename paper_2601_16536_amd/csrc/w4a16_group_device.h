@@ -137,19 +137,21 @@ __device__ __forceinline__ void load_to_lds(const uint8_t *base, uint32_t offset
 }
 
 // The same, unseen by the compiler, for tiles that are read across: ahead of a transposing read of LDS it waits for every load to LDS that it knows of, those of later stages too.
-// No vector register is written, and whoever reads the bytes waits for them by count (arrive), as with the other form; m0 is the kernel's alone (none has both forms).  `bytes`: of the buffer; zeros past them.
+// No vector register is written, and whoever reads the bytes waits for them by count (arrive), as with the other form.  `bytes`: of the buffer; zeros past them.
+// The descriptor's words may come from vector instructions (v_readfirstlane) just ahead, and a memory instruction has to be five wait states behind such a write of a scalar register it reads.  The compiler
+// counts that for its own instructions and not for these, so they bring the five themselves (of which m0, that the compiler writes, needs one).
 __device__ __forceinline__ void load_to_lds_unseen(const uint8_t *base, uint32_t bytes, uint32_t offset, int uniform, uint8_t *to)
 {
     const uint64_t b = reinterpret_cast<uint64_t>(base);
     const uint4_t r = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) & 0xFFFFu,
                        (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), kRawBuffer};
     const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_ptr_t)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(at), "v"(offset), "s"(r), "s"(uniform) : "memory");
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %0, %1, %2 offen lds" ::"v"(offset), "s"(r), "s"(uniform), "{m0}"(at) : "memory");
 }
 __device__ __forceinline__ void load_to_lds_unseen(const uint8_t *from, uint8_t *to)
 {
     const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_ptr_t)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from), "{m0}"(at) : "memory");  // (its address is in vector registers)
 }
 // The same for numbers of four bytes, one a lane.
 __device__ __forceinline__ void numbers_to_lds_unseen(const int32_t *base, uint32_t bytes, uint32_t offset, uint8_t *to)
@@ -158,7 +160,7 @@ __device__ __forceinline__ void numbers_to_lds_unseen(const int32_t *base, uint3
     const uint4_t r = {(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32)) & 0xFFFFu,
                        (uint32_t)__builtin_amdgcn_readfirstlane((int)bytes), kRawBuffer};
     const uint32_t at = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(uintptr_t)(lds_ptr_t)to);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds" ::"s"(at), "v"(offset), "s"(r) : "memory");
+    asm volatile("s_nop 4\n\tbuffer_load_dword %0, %1, 0 offen lds" ::"v"(offset), "s"(r), "{m0}"(at) : "memory");
 }
 // The bytes of `rows` rows of `width` bytes, `row` (at least 16) bytes apart, as far as 32 rows and 256 bytes can reach into them; 0 if there are none.
 __device__ __forceinline__ uint32_t bytes_of(int rows, int row, int width) { return (uint32_t)max((min(rows, 96) - 1) * row + width, 0); }

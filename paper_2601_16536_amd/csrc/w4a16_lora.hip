@@ -617,13 +617,14 @@ __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
     for (int i = 0; i < J; ++i)
 #pragma unroll
         for (int u = 0; u < RT; ++u) acc[i][u] = (float4_t){0.f, 0.f, 0.f, 0.f};
-    auto ask_rows = [&](int stage) {
+    auto ask_rows = [&](int stage) __attribute__((always_inline)) {
         if (stage < stages)
             numbers_to_lds_unseen(a.order + begin + stage * kGroupStage, (uint32_t)(count - stage * kGroupStage) * 4u, (uint32_t)lane * 4u, reinterpret_cast<uint8_t *>(list + (stage & 3) * 64));
     };
-    auto fetch = [&](int stage) {
+    // (Called from three places: left to the compiler, a function of its own at rank 128, with what it captures in scratch and a wait for every load on the way.)
+    auto fetch = [&](int stage) __attribute__((always_inline)) {
         uint8_t *const to = lds + stage % kDepth * Sh::kBuffer;
-        auto row_at = [&](int in_stage) { return stage * kGroupStage + in_stage < count ? list[(stage & 3) * 64 + in_stage] : -1; };
+        auto row_at = [&](int in_stage) __attribute__((always_inline)) { return stage * kGroupStage + in_stage < count ? list[(stage & 3) * 64 + in_stage] : -1; };
         ask_rows(stage + 2);
 #pragma unroll
         for (int i = 0; i < PTile::kLoads; ++i) {

@@ -125,14 +125,24 @@ def test_the_check_sees_what_it_is_for():
     assert {r for _, _, r in too_soon([m0[0], (88, "s_nop", "0", None), load, first, (108, "s_cbranch_scc1", "x", 84), (112, "s_endpgm", "", None)], 84)} == {"s6"}
 
 
-def test_scalar_operands_are_there_in_time(code_objects):
-    seen = bad = 0
-    first = []
+@pytest.fixture(scope="module")
+def checked(code_objects):
+    """Of all functions: how many memory instructions, the reads that come too soon, calls."""
+    seen, soon, calls = 0, [], []
     for path in code_objects:
         for name, start, body in functions(path):
             seen += sum(1 for i in body if i[1].startswith(MEMORY))
-            found = too_soon(body, start)
-            bad += len(found)
-            first += [(name, "%x" % a, i, r) for a, i, r in sorted(found)[:2]]
+            soon += [(name, "%x" % a, i, r) for a, i, r in sorted(too_soon(body, start))]
+            calls += [name for i in body if i[1] in ("s_swappc_b64", "s_call_b64")]
+    return seen, soon, calls
+
+
+def test_scalar_operands_are_there_in_time(checked):
+    seen, soon, _ = checked
     assert seen > 10000
-    assert bad == 0, "%d reads too soon, the first %r" % (bad, first[:12])
+    assert not soon, "%d reads too soon, the first %r" % (len(soon), soon[:12])
+
+
+def test_loops_call_no_function(checked):
+    """A function of its own gets what it needs through scratch memory, and waits there for the loads that a loop has on their way."""
+    assert not checked[2], sorted(set(checked[2]))

@@ -1,7 +1,7 @@
 // Low-rank adapters of many requests beside a shared projection, and their gradients:
 //     H = s X A^T  [rows, R] (shrink),   out = Y + H B^T (expand);   backward G = s dY B (shrink), dX += G A (expand), dA = G^T X, dB = dY^T H (grads)
 // for the rows of every adapter.  R is at most 128, so all of it is moving X, Y and the adapters; the multiplications are few.  H and G are sums in FP32; into the second
-// products, which are 16-bit MFMAs, they go as sums of two or three 16-bit numbers: to 22 bits at least, but for the gradients in 16 bits, where it is 16.
+// products, which are 16-bit MFMAs, they go as sums of two or three 16-bit numbers: to 22 bits in out and dX, to all 24 in dA and dB, whose sums over many rows may cancel.
 //
 // Rows of an adapter come in tiles of 16 (few rows) or 64.  Up to kFewRows rows a wave finds the tiles from the ids alone; beyond, the ids are sorted first.
 #include "w4a16_group_device.h"
@@ -311,14 +311,15 @@ __global__ __launch_bounds__(256, 2) void lora_shrink_kernel(Lists l, ShrinkArgs
     shrink_side<TYPE, RT, false, BOTH>(l, a.side[0], a, lds, rows, adapter, count);
 }
 
-// A thread four values of one row; rows without an adapter: nothing.  GRAD: the terms for the gradients, of both sides by the grid's third dimension (0: of H; none of them for add), and
+// A thread four values of one row; rows without an adapter: nothing.  GRAD: the terms for the gradients, of both sides by the grid's third dimension (0: of H), and
 // what `expanded`, the side that goes through the expanding product next, needs for that.
-template <int TYPE, int RT, int GRAD>
+constexpr int kGradTerms = 3;  // FP32's 24 bits, for gradients of either type (two, 16 bits, for those in 16 bits lost what differs little between rows whose products cancel)
+template <int TYPE, int RT, bool GRAD>
 __global__ __launch_bounds__(256) void lora_sum_kernel(Lists l, ShrinkArgsMany a, int expanded)
 {
     typedef ExpandTerms<TYPE> Terms;
     constexpr int kRp = 16 * RT, kPer = kRp / 4;
-    const int which = GRAD > 0 ? (int)blockIdx.z : 0;
+    const int which = GRAD ? (int)blockIdx.z : 0;
     const ShrinkSide s = a.side[which];
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / kPer;
     const int r = (int)(i % kPer) * 4;
@@ -341,12 +342,12 @@ __global__ __launch_bounds__(256) void lora_sum_kernel(Lists l, ShrinkArgsMany a
     auto put = [&](uint16_t *to, const auto &t, int n) {
         *reinterpret_cast<uint2_t *>(to + n * kRp + r) = (uint2_t){(uint32_t)t[0][n] | (uint32_t)t[1][n] << 16, (uint32_t)t[2][n] | (uint32_t)t[3][n] << 16};
     };
-    if constexpr (GRAD > 0) {
-        uint16_t t[4][GRAD];
+    if constexpr (GRAD) {
+        uint16_t t[4][kGradTerms];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bf16_terms<GRAD>(v[e], t[e]);
+        for (int e = 0; e < 4; ++e) bf16_terms<kGradTerms>(v[e], t[e]);
 #pragma unroll
-        for (int n = 0; n < GRAD; ++n) put(s.terms + (size_t)row * (GRAD * kRp), t, n);
+        for (int n = 0; n < kGradTerms; ++n) put(s.terms + (size_t)row * (kGradTerms * kRp), t, n);
     }
     if (which != expanded) return;
     if constexpr (TYPE == kTypeF16) {
@@ -585,9 +586,9 @@ struct GradArgs {
     int R;
 };
 
-template <int TYPE, int GRAD_TYPE, int RT, int COLS>
+template <int RT, int COLS>
 struct GradShape {
-    static constexpr int kTerms = GRAD_TYPE == kTypeF32 ? 3 : 2, kSpan = 16 * RT * kTerms, kBuffer = (COLS + kSpan) * 128;
+    static constexpr int kSpan = 16 * RT * kGradTerms, kBuffer = (COLS + kSpan) * 128;
     static constexpr int kDepth = kBuffer * 3 <= 80 * 1024 - 2048 ? 3 : 2, kLds = kDepth * kBuffer + 4 * 256;
     static_assert(kLds <= 163840 - 1024, "LDS of a compute unit");
 };
@@ -596,8 +597,8 @@ template <int TYPE, int GRAD_TYPE, int RT, int COLS>
 __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
 {
     typedef typename ActOf<TYPE>::type Act;
-    typedef GradShape<TYPE, GRAD_TYPE, RT, COLS> Sh;
-    constexpr int kWaves = 4, J = COLS / 64, kRp = 16 * RT, kTerms = Sh::kTerms, kDepth = Sh::kDepth, kParts = TYPE == kTypeF16 ? 2 : 1;
+    typedef GradShape<RT, COLS> Sh;
+    constexpr int kWaves = 4, J = COLS / 64, kRp = 16 * RT, kTerms = kGradTerms, kDepth = Sh::kDepth, kParts = TYPE == kTypeF16 ? 2 : 1;
     typedef AcrossTile<COLS, kWaves> PTile;
     typedef AcrossTile<kRp, kWaves> QTile;  // of one term
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -781,7 +782,7 @@ struct Space {
     size_t offsets, order, sort, h[2], terms[2], operand, up, bytes;
     int slices[2];
 };
-Space space_of(int M, int L, int R, int K, int N, bool grad, int grad_type)
+Space space_of(int M, int L, int R, int K, int N, bool grad)
 {
     Space s = {};
     const size_t row = (size_t)M * (size_t)padded(R);
@@ -790,7 +791,7 @@ Space space_of(int M, int L, int R, int K, int N, bool grad, int grad_type)
         s.bytes = whole(row * 4 * (size_t)s.slices[0]);
         return s;
     }
-    const int sides = grad ? 2 : 1, n_terms = grad ? (grad_type == kTypeF32 ? 3 : 2) : 0;
+    const int sides = grad ? 2 : 1, n_terms = grad ? kGradTerms : 0;
     const size_t tiles = (size_t)many_tiles(M, L);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -849,12 +850,12 @@ hipError_t expand(const LoraArgs &a, const Lists &l, const ExpandArgs &x, bool a
 
 size_t lora_workspace(int M, int L, int R, int K, int N, bool grad)
 {
-    return space_of(M, L, R, K, N, grad, kTypeF32).bytes;
+    return space_of(M, L, R, K, N, grad).bytes;
 }
 
 hipError_t launch_lora_add(const LoraArgs &a, hipStream_t stream)
 {
-    const Space s = space_of(a.M, a.L, a.R, a.K, a.N, false, 0);
+    const Space s = space_of(a.M, a.L, a.R, a.K, a.N, false);
     uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
     Lists l = {a.ids, nullptr, nullptr, a.M, a.L, key_bits(a.L)};
     ExpandArgs x = {static_cast<const uint16_t *>(a.B), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), nullptr, nullptr, nullptr, a.ldbase, a.ldo, a.N, a.R, 1};
@@ -885,7 +886,7 @@ hipError_t launch_lora_add(const LoraArgs &a, hipStream_t stream)
         return with_rank(a.R, [&](auto rt) {
             constexpr int RT = decltype(rt)::value;
             const hipError_t err = enqueue(&lora_shrink_kernel<decltype(type)::value, RT, false>, grid, 256, shrink_lds<RT>(), stream, l, m);
-            return err != hipSuccess ? err : enqueue(&lora_sum_kernel<decltype(type)::value, RT, 0>, dim3(sum_blocks(a.M, a.R)), 256, 0, stream, l, m, 0);
+            return err != hipSuccess ? err : enqueue(&lora_sum_kernel<decltype(type)::value, RT, false>, dim3(sum_blocks(a.M, a.R)), 256, 0, stream, l, m, 0);
         });
     });
     return e != hipSuccess ? e : expand(a, l, x, false, kTileRows, stream);
@@ -893,7 +894,7 @@ hipError_t launch_lora_add(const LoraArgs &a, hipStream_t stream)
 
 hipError_t launch_lora_grad(const LoraArgs &a, hipStream_t stream)
 {
-    const Space s = space_of(a.M, a.L, a.R, a.K, a.N, true, a.grad_type);
+    const Space s = space_of(a.M, a.L, a.R, a.K, a.N, true);
     uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
     const size_t tiles = (size_t)many_tiles(a.M, a.L);
     int32_t *const offsets = reinterpret_cast<int32_t *>(ws + s.offsets), *const order = reinterpret_cast<int32_t *>(ws + s.order);
@@ -915,7 +916,7 @@ hipError_t launch_lora_grad(const LoraArgs &a, hipStream_t stream)
                 const dim3 grid((unsigned)most, (unsigned)tiles, 2);
                 err = enqueue(&lora_shrink_kernel<T, RT, true>, grid, 256, shrink_lds<RT>(), stream, l, m);
                 const dim3 sums(sum_blocks(a.M, a.R), 1, 2);
-                if (err == hipSuccess) err = wide ? enqueue(&lora_sum_kernel<T, RT, 3>, sums, 256, 0, stream, l, m, 1) : enqueue(&lora_sum_kernel<T, RT, 2>, sums, 256, 0, stream, l, m, 1);
+                if (err == hipSuccess) err = enqueue(&lora_sum_kernel<T, RT, true>, sums, 256, 0, stream, l, m, 1);
                 const ExpandArgs x = {static_cast<const uint16_t *>(a.A), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), nullptr, m.operand, m.up, a.ldbase, a.ldo, a.K, a.R, 1};
                 if (err == hipSuccess) err = expand(a, l, x, true, kTileRows, stream);  // (dX may be written over: the last launch reads X and dY only)
                 if (err != hipSuccess) return err;
@@ -928,7 +929,7 @@ hipError_t launch_lora_grad(const LoraArgs &a, hipStream_t stream)
                 constexpr int kGrad = decltype(grad_type)::value, kCols = decltype(columns)::value;
                 for (GradSide &side : g.side) side.blocks = (side.width + kCols - 1) / kCols;
                 return enqueue(&lora_grads_kernel<T, kGrad, RT, kCols>, dim3((unsigned)(g.side[0].blocks + g.side[1].blocks), (unsigned)a.L), 256,
-                               GradShape<T, kGrad, RT, kCols>::kLds, stream, g);
+                               GradShape<RT, kCols>::kLds, stream, g);
             };
             constexpr std::integral_constant<int, 128> k128{};
             constexpr std::integral_constant<int, 64> k64{};

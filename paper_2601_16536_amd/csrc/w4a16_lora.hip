@@ -1,7 +1,8 @@
 // Low-rank adapters of many requests beside a shared projection, and their gradients:
 //     H = s X A^T  [rows, R] (shrink),   out = Y + H B^T (expand);   backward G = s dY B (shrink), dX += G A (expand), dA = G^T X, dB = dY^T H (grads)
 // for the rows of every adapter.  R is at most 128, so all of it is moving X, Y and the adapters; the multiplications are few.  H and G are sums in FP32; into the second
-// products, which are 16-bit MFMAs, they go as sums of two or three 16-bit numbers: to 22 bits in out and dX, to all 24 in dA and dB, whose sums over many rows may cancel.
+// products, which are 16-bit MFMAs, they go as sums of three bfloat16 numbers: all of FP32's 24 bits in all of its range (two FP16 numbers of values scaled by rows lost what is 2^-38 of a row's largest).
+// FP16 operands beside them go as two, whose sum they are exactly: eight and three bits.
 //
 // Rows of an adapter come in tiles of 16 (few rows) or 64.  Up to kFewRows rows a wave finds the tiles from the ids alone; beyond, the ids are sorted first.
 #include "w4a16_group_device.h"
@@ -182,20 +183,18 @@ __global__ __launch_bounds__(256) void lora_few_shrink_kernel(Lists l, ShrinkArg
 // ---- shrink of many rows ----
 //
 // A workgroup has 64 rows, a slice of k and all of R, in stages of 64 k through LDS (w4a16_group_device.h); a wave 16 rows.  A launch of its own adds the slices' sums up, in their
-// order, scales them and writes them as the 16-bit numbers whose sums they are, one behind the other.  (The last slice's workgroup as the one that adds: 16 us more, M = 2048,
+// order, scales them and writes them as the three bfloat16 numbers whose sums they are, one behind the other.  (The last slice's workgroup as the one that adds: 16 us more, M = 2048,
 // K = 8192, rank 64: it waits for memory three times one after the other.)
 struct ShrinkSide {
     const uint16_t *X, *W;
     float *partial;    // [slices][M][Rp]
-    uint16_t *terms;   // of the gradients: [M][terms][Rp]
+    uint16_t *terms;   // [M][kTerms][Rp]
     long long ldx;
     int K, slices;
 };
 struct ShrinkArgsMany {
     ShrinkSide side[2];  // X and A; dY and B, across
     const float *scaling;
-    uint16_t *operand;   // of the expanding product: [M][terms][Rp]
-    int *up;             // FP16: the power of two that a row of it has been scaled by, [M]
     int R;
 };
 
@@ -208,16 +207,42 @@ __device__ __forceinline__ uint16_t bf16_near(float v)
     const uint16_t n = to_16bit(v, 1);
     return (n & 0x7FFFu) == 0x7F80u && finite(v) ? (uint16_t)(n - 1) : n;
 }
-// v as a sum of TERMS bfloat16 numbers, each the nearest to what the ones before leave: off by 2^(-8 TERMS) |v| at most.  What is not finite is itself and zeros.
-template <int TERMS>
-__device__ __forceinline__ void bf16_terms(float v, uint16_t (&terms)[TERMS])
+constexpr int kTerms = 3;
+// v as a sum of kTerms bfloat16 numbers, each the nearest to what the ones before leave.  What is not finite is itself and zeros.
+__device__ __forceinline__ void bf16_terms(float v, uint16_t (&terms)[kTerms])
 {
     float rest = v;
 #pragma unroll
-    for (int n = 0; n < TERMS; ++n) {
+    for (int n = 0; n < kTerms; ++n) {
         terms[n] = bf16_near(rest);
         rest = finite(v) ? rest - bf16_value(terms[n]) : 0.f;
     }
+}
+// Eight 16-bit values as one bfloat16 number each, or FP16 ones as two: v = the sum of parts.  What is not finite is itself and zero.
+template <int TYPE>
+constexpr int kParts = TYPE == kTypeF16 ? 2 : 1;
+template <int TYPE>
+__device__ __forceinline__ void bf16_parts(uint4_t v, uint4_t (&parts)[kParts<TYPE>])
+{
+    parts[0] = v;
+    if constexpr (TYPE == kTypeF16) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float f0 = from_16bit<TYPE>((uint16_t)v[e]), f1 = from_16bit<TYPE>((uint16_t)(v[e] >> 16));
+            const float r0 = finite(f0) ? f0 - bf16_value(bf16_down(f0)) : 0.f, r1 = finite(f1) ? f1 - bf16_value(bf16_down(f1)) : 0.f;
+            parts[0][e] = (uint32_t)bf16_down(f0) | (uint32_t)bf16_down(f1) << 16;
+            parts[1][e] = (uint32_t)bf16_down(r0) | (uint32_t)bf16_down(r1) << 16;
+        }
+    }
+}
+// The sign bits of those of eight bfloat16 numbers that are not finite; the numbers with zeros in their places.
+__device__ __forceinline__ uint4_t not_finite(uint4_t v) { return ((v & 0x7F807F80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint4_t finite_only(uint4_t v) { return v & ~((not_finite(v) >> 15) * 0xFFFFu); }
+// The same, and not ahead of the loop that it is in, where many of them would take as many registers again.
+__device__ __forceinline__ uint4_t finite_only_here(uint4_t v)
+{
+    asm volatile("" : "+v"(v));
+    return finite_only(v);
 }
 
 template <int TYPE, int RT, bool ACROSS, bool UNSEEN>
@@ -278,26 +303,6 @@ __device__ __forceinline__ void shrink_side(const Lists &l, const ShrinkSide &a,
     for (int t = 0; t < RT; ++t) *reinterpret_cast<float4_t *>(to + 16 * t) = acc[t][0];
 }
 
-// What the expanding product takes of a value of H: three bfloat16 numbers, or two FP16 numbers of a value already scaled (below).
-template <int TYPE>
-struct ExpandTerms;
-template <>
-struct ExpandTerms<kTypeBF16> {
-    static constexpr int kTerms = 3;
-    static __device__ __forceinline__ void split(float h, uint16_t (&to)[3]) { bf16_terms<3>(h, to); }
-};
-template <>
-struct ExpandTerms<kTypeF16> {
-    static constexpr int kTerms = 2;
-    static __device__ __forceinline__ void split(float h, uint16_t (&to)[2])
-    {
-        to[0] = to_16bit(h, 0);
-        to[1] = to_16bit(finite(h) ? h - from_16bit<kTypeF16>(to[0]) : 0.f, 0);
-    }
-};
-// A row's power of two for FP16, from its largest value: that one to 2^13 .. 2^14.
-__device__ __forceinline__ int row_scale(float most) { return most > 0.f && finite(most) ? 14 - __builtin_amdgcn_frexp_expf(most) : 0; }
-
 // BOTH: side 1 too, by the grid's third dimension.
 template <int TYPE, int RT, bool BOTH>
 __global__ __launch_bounds__(256, 2) void lora_shrink_kernel(Lists l, ShrinkArgsMany a)
@@ -311,20 +316,16 @@ __global__ __launch_bounds__(256, 2) void lora_shrink_kernel(Lists l, ShrinkArgs
     shrink_side<TYPE, RT, false, BOTH>(l, a.side[0], a, lds, rows, adapter, count);
 }
 
-// A thread four values of one row; rows without an adapter: nothing.  GRAD: the terms for the gradients, of both sides by the grid's third dimension (0: of H), and
-// what `expanded`, the side that goes through the expanding product next, needs for that.
-constexpr int kGradTerms = 3;  // FP32's 24 bits, for gradients of either type (two, 16 bits, for those in 16 bits lost what differs little between rows whose products cancel)
-template <int TYPE, int RT, bool GRAD>
-__global__ __launch_bounds__(256) void lora_sum_kernel(Lists l, ShrinkArgsMany a, int expanded)
+// A thread four values of one row, of either side by the grid's third dimension; rows without an adapter: nothing.
+template <int RT>
+__global__ __launch_bounds__(256) void lora_sum_kernel(Lists l, ShrinkArgsMany a)
 {
-    typedef ExpandTerms<TYPE> Terms;
     constexpr int kRp = 16 * RT, kPer = kRp / 4;
-    const int which = GRAD ? (int)blockIdx.z : 0;
-    const ShrinkSide s = a.side[which];
+    const ShrinkSide s = a.side[blockIdx.z];
     const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i / kPer;
     const int r = (int)(i % kPer) * 4;
     const int adapter = row < l.M ? l.ids[row] : -1;
-    if (adapter < 0 || adapter >= l.L) return;  // (a row's threads are in one wave: all of them go)
+    if (adapter < 0 || adapter >= l.L) return;
     const size_t next = (size_t)l.M * kRp;
     const float *const h = s.partial + (size_t)row * kRp + r;
     float4_t v = *reinterpret_cast<const float4_t *>(h);
@@ -339,51 +340,32 @@ __global__ __launch_bounds__(256) void lora_sum_kernel(Lists l, ShrinkArgsMany a
     for (; k < s.slices; ++k) v += *reinterpret_cast<const float4_t *>(h + (size_t)k * next);
     v = v * (a.scaling ? a.scaling[adapter] : 1.0f);
     if (r >= a.R) v = (float4_t){0.f, 0.f, 0.f, 0.f};
-    auto put = [&](uint16_t *to, const auto &t, int n) {
-        *reinterpret_cast<uint2_t *>(to + n * kRp + r) = (uint2_t){(uint32_t)t[0][n] | (uint32_t)t[1][n] << 16, (uint32_t)t[2][n] | (uint32_t)t[3][n] << 16};
-    };
-    if constexpr (GRAD) {
-        uint16_t t[4][kGradTerms];
+    uint16_t t[4][kTerms];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bf16_terms<kGradTerms>(v[e], t[e]);
+    for (int e = 0; e < 4; ++e) bf16_terms(v[e], t[e]);
 #pragma unroll
-        for (int n = 0; n < kGradTerms; ++n) put(s.terms + (size_t)row * (kGradTerms * kRp), t, n);
-    }
-    if (which != expanded) return;
-    if constexpr (TYPE == kTypeF16) {
-        float most = __builtin_fmaxf(__builtin_fmaxf(__builtin_fabsf(v[0]), __builtin_fabsf(v[1])), __builtin_fmaxf(__builtin_fabsf(v[2]), __builtin_fabsf(v[3])));  // (a NaN is passed over: its row is NaN at any scale)
-#pragma unroll
-        for (int d = 1; d < kPer; d <<= 1) most = __builtin_fmaxf(most, __shfl_xor(most, d, 64));
-        const int up = row_scale(most);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = ldexpf(v[e], up);
-        if (r == 0) a.up[row] = up;
-    }
-    uint16_t t[4][Terms::kTerms];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) Terms::split(v[e], t[e]);
-#pragma unroll
-    for (int n = 0; n < Terms::kTerms; ++n) put(a.operand + (size_t)row * (Terms::kTerms * kRp), t, n);
+    for (int n = 0; n < kTerms; ++n)
+        *reinterpret_cast<uint2_t *>(s.terms + ((size_t)row * kTerms + (size_t)n) * kRp + r) = (uint2_t){(uint32_t)t[0][n] | (uint32_t)t[1][n] << 16, (uint32_t)t[2][n] | (uint32_t)t[3][n] << 16};
 }
 
 // ---- expand: out[i, n] = base[i, n] + sum over r of H[i][r] W[n, r] ----
 //
 // A wave has 128 columns (64 from rank 72 on, for the registers) and the tile's rows by sixteens.  Eight (four) MFMA tiles t: their column c is column 8 c + t, so that a lane ends with eight
 // neighbouring columns of four rows, and sixteen lanes with 256 bytes of a row.  (With the columns as the MFMA's rows it is 64 bytes of sixteen rows: to read and write 2048 x 8192 so alone took 20 us.)  ACROSS: W is A [R, N] (N the columns here): a lane loads eight rows of eight columns and
-// turns them by itself.  H goes in as the sum of three bfloat16 numbers (FP32's 24 bits) or of two FP16 numbers (22): a row of H is first scaled by a power of two, its largest
-// value to 2^13 .. 2^14, so that its smaller ones keep 2^-38 of that; the sums are scaled back.
+// turns them by itself.  H goes in as three bfloat16 numbers, W as one or two: three or six products for each value.  Where W, or H beside W's second numbers, is not finite, what it would be
+// multiplied by is zero but in the first numbers of both: those alone say what the sum is then, and zeros would make a NaN of an infinity.  FP16's second numbers cost registers
+// (one wave fewer on a SIMD up to rank 64) and three products: 2048 rows of five adapters, 8192 x 8192, rank 64 47 -> 55 us a call, rank 128 64 -> 83, against two FP16 numbers of a scaled row.
 struct ExpandArgs {
     const uint16_t *W, *base;
     uint16_t *out;
-    const float *H;           // few rows: [slices][M][Rp], else null
-    const uint16_t *operand;  // else: [M][terms][Rp]
-    const int *up;
+    const float *H;         // few rows: [slices][M][Rp], else null
+    const uint16_t *terms;  // else: [M][kTerms][Rp]
     long long ldbase, ldo;
     int N, R, slices;
 };
 
 template <int TYPE, int G, int RP, bool ACROSS, int TR>
-__global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_kernel(Lists l, ExpandArgs a)
+__global__ __launch_bounds__(256, G == 4 ? 2 : (TYPE == kTypeF16 ? 4 : 5) - G) void lora_expand_kernel(Lists l, ExpandArgs a)
 {
     typedef typename ActOf<TYPE>::type Act;
     constexpr int kTiles = G <= 2 ? 8 : 4;  // MFMA tiles of sixteen columns; a lane's neighbouring columns
@@ -395,10 +377,9 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, p = lane >> 4;
     const int n0 = ((int)blockIdx.x * ((int)blockDim.x >> 6) + wave) * 16 * kTiles;
     const bool product = adapter < l.L;
-    typedef ExpandTerms<TYPE> Terms;
 
     // Of many rows, the operands that H gives come to LDS, for all of the workgroup's waves: read by each of them from memory they are three times base's bytes.
-    constexpr int kPieces = Terms::kTerms * RP / 8, kRow = Terms::kTerms * RP * 2 + 16;  // of a row; its bytes in LDS, so that sixteen rows lie on all banks
+    constexpr int kPieces = kTerms * RP / 8, kRow = kTerms * RP * 2 + 16;  // of a row; its bytes in LDS, so that sixteen rows lie on all banks
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     const int m_each = TR / 16 / (int)gridDim.z, m_begin = (int)blockIdx.z * m_each, m_end = min(m_begin + m_each, (count + 15) / 16);  // the workgroup's part of the tile, by sixteen rows
     if (m_begin >= m_end) return;
@@ -410,7 +391,7 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {  // (past the last: the last again)
                 const int i = min(i0 + j * (int)blockDim.x, to - 1);
-                v[j] = *reinterpret_cast<const uint4_t *>(a.operand + (size_t)rows[i / kPieces] * (kPieces * 8) + i % kPieces * 8);
+                v[j] = *reinterpret_cast<const uint4_t *>(a.terms + (size_t)rows[i / kPieces] * (kPieces * 8) + i % kPieces * 8);
             }
 #pragma unroll
             for (int j = 0; j < kAtOnce; ++j) {
@@ -422,7 +403,8 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
     }
     if (n0 >= a.N) return;
 
-    uint4_t w[G][kTiles];
+    uint4_t w[G][kTiles][kParts<TYPE>];
+    bool odd_w = false;  // something in W is not finite
     if (product) {
         const uint16_t *const from = a.W + (size_t)adapter * (size_t)a.R * (size_t)a.N;
         const int n = min(n0 + kTiles * c, a.N - kTiles);
@@ -438,33 +420,39 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
                     if (!have) v[e] = (Piece)0u;
                 }
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t)
+                for (int t = 0; t < kTiles; ++t) {
+                    uint4_t u;
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) w[g][t][e] = __builtin_amdgcn_perm(v[2 * e + 1][t >> 1], v[2 * e][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
+                    for (int e = 0; e < 4; ++e) u[e] = __builtin_amdgcn_perm(v[2 * e + 1][t >> 1], v[2 * e][t >> 1], t & 1 ? 0x07060302u : 0x05040100u);
+                    bf16_parts<TYPE>(u, w[g][t]);
+                }
             } else {
 #pragma unroll
-                for (int t = 0; t < kTiles; ++t) w[g][t] = load16(from + (size_t)(n + t) * (size_t)a.R + (size_t)(have ? r : 0), have);
+                for (int t = 0; t < kTiles; ++t) bf16_parts<TYPE>(load16(from + (size_t)(n + t) * (size_t)a.R + (size_t)(have ? r : 0), have), w[g][t]);
             }
         }
+        uint4_t odd = {0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) odd |= not_finite(w[g][t][0]);
+        odd_w = __any((odd[0] | odd[1] | odd[2] | odd[3]) != 0);
     }
     // The rows' values of base come sixteen rows ahead.
     const int n = n0 + kTiles * c;
     struct Rows {
         Piece y[4];
-        int up;
     };
-    uint4_t x[G][Terms::kTerms];
+    uint4_t x[G][kTerms];
     auto load = [&](Rows &to, int m) {
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int row = rows[min(16 * m + 4 * p + v, count - 1)];
             to.y[v] = *reinterpret_cast<const Piece *>(a.base ? a.base + (size_t)row * (size_t)a.ldbase + (size_t)min(n, a.N - kTiles) : reinterpret_cast<const uint16_t *>(kGroupZeros));
         }
-        if (!product) return;
-        const int row = rows[min(16 * m + c, count - 1)];
-        if constexpr (TR != 16) {
-            if constexpr (TYPE == kTypeF16) to.up = a.up[row];
-        } else {  // few rows: the slices' sums meet here
+        if constexpr (TR == 16) {  // few rows: the slices' sums meet here
+            if (!product) return;
+            const int row = rows[min(16 * m + c, count - 1)];
             float h[G][8];
             const size_t next = (size_t)l.M * RP;
 #pragma unroll
@@ -490,30 +478,15 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
 #pragma unroll
                 for (int e = 0; e < 8; ++e) h[g][e] = r < a.R ? (e < 4 ? h0[e & 3] : h1[e & 3]) : 0.f;
             }
-            to.up = 0;
-            if constexpr (TYPE == kTypeF16) {
-                float most = 0.f;
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) most = __builtin_fmaxf(most, __builtin_fabsf(h[g][e]));
-                most = __builtin_fmaxf(most, __shfl_xor(most, 16, 64));
-                most = __builtin_fmaxf(most, __shfl_xor(most, 32, 64));
-                to.up = row_scale(most);
-#pragma unroll
-                for (int g = 0; g < G; ++g)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) h[g][e] = ldexpf(h[g][e], to.up);
-            }
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
                 for (int e = 0; e < 8; e += 2) {
-                    uint16_t t0[Terms::kTerms], t1[Terms::kTerms];
-                    Terms::split(h[g][e], t0);
-                    Terms::split(h[g][e + 1], t1);
+                    uint16_t t0[kTerms], t1[kTerms];
+                    bf16_terms(h[g][e], t0);
+                    bf16_terms(h[g][e + 1], t1);
 #pragma unroll
-                    for (int i = 0; i < Terms::kTerms; ++i) x[g][i][e / 2] = (uint32_t)t0[i] | (uint32_t)t1[i] << 16;
+                    for (int i = 0; i < kTerms; ++i) x[g][i][e / 2] = (uint32_t)t0[i] | (uint32_t)t1[i] << 16;
                 }
         }
     };
@@ -528,37 +501,51 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
 #pragma unroll
             for (int g = 0; g < G; ++g)
 #pragma unroll
-                for (int i = 0; i < Terms::kTerms; ++i) {
+                for (int i = 0; i < kTerms; ++i) {
                     const bool have = 32 * g + 8 * p < RP;
                     const uint4_t v = *reinterpret_cast<const uint4_t *>(from + i * RP * 2 + (have ? 64 * g + 16 * p : 0));
                     x[g][i] = have ? v : (uint4_t){0u, 0u, 0u, 0u};
                 }
         }
         if (product) {
+            auto products = [&](auto odd) {
+                constexpr bool kOdd = decltype(odd)::value;
 #pragma unroll
-            for (int half = 0; half < kTiles; half += 4) {  // (four tiles' sums at a time, for the registers)
-                float4_t acc[4];
+                for (int half = 0; half < kTiles; half += 4) {  // (four tiles' sums at a time, for the registers)
+                    float4_t acc[4];
 #pragma unroll
-                for (int t = 0; t < 4; ++t) acc[t] = (float4_t){0.f, 0.f, 0.f, 0.f};
+                    for (int t = 0; t < 4; ++t) acc[t] = (float4_t){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int g = 0; g < G; ++g)
+                    for (int g = 0; g < G; ++g)
 #pragma unroll
-                    for (int i = 0; i < Terms::kTerms; ++i)
+                        for (int i = 0; i < kTerms; ++i)
 #pragma unroll
-                        for (int t = 0; t < 4; ++t) acc[t] = Act::mfma(Act::x_operand(x[g][i]), Act::x_operand(w[g][half + t]), acc[t]);
+                            for (int part = 0; part < kParts<TYPE>; ++part)
 #pragma unroll
-                for (int v = 0; v < 4; ++v) {
-                    [[maybe_unused]] int down = 0;
-                    if constexpr (TYPE == kTypeF16) down = -__shfl(now.up, 4 * p + v, 64);  // of the row that the lane has here
+                                for (int t = 0; t < 4; ++t) {
+                                    uint4_t u = x[g][i], v = w[g][half + t][part];
+                                    if (kOdd && part > 0) u = finite_only_here(u);
+                                    if (kOdd && i > 0) v = finite_only_here(v);
+                                    acc[t] = ActBF16::mfma(ActBF16::x_operand(u), ActBF16::x_operand(v), acc[t]);
+                                }
 #pragma unroll
-                    for (int t = 0; t < 4; t += 2) {
-                        float y0 = acc[t][v], y1 = acc[t + 1][v];
-                        if constexpr (TYPE == kTypeF16) y0 = ldexpf(y0, down), y1 = ldexpf(y1, down);
-                        const uint32_t old = y[v][(half + t) >> 1];
-                        y[v][(half + t) >> 1] = Act::pack2(y0 + from_16bit<TYPE>((uint16_t)old), y1 + from_16bit<TYPE>((uint16_t)(old >> 16)));
-                    }
+                    for (int v = 0; v < 4; ++v)
+#pragma unroll
+                        for (int t = 0; t < 4; t += 2) {
+                            const uint32_t old = y[v][(half + t) >> 1];
+                            y[v][(half + t) >> 1] = Act::pack2(acc[t][v] + from_16bit<TYPE>((uint16_t)old), acc[t + 1][v] + from_16bit<TYPE>((uint16_t)(old >> 16)));
+                        }
                 }
+            };
+            bool odd = odd_w;
+            if constexpr (kParts<TYPE> > 1) {
+                uint4_t of_x = {0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int g = 0; g < G; ++g) of_x |= not_finite(x[g][0]);
+                odd |= __any((of_x[0] | of_x[1] | of_x[2] | of_x[3]) != 0);
             }
+            if (__builtin_expect(odd, 0)) products(std::true_type{});
+            else products(std::false_type{});
         }
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
@@ -572,7 +559,7 @@ __global__ __launch_bounds__(256, G == 1 ? 4 : G == 2 ? 3 : 2) void lora_expand_
 //
 // A workgroup has 128 columns of X or dY and all of R, a wave 32 columns; half of them up to rank 32 where there are few workgroups, as adapters' rows differ (4096 rows of four adapters,
 // K = N = 8192, rank 32: 51 -> 40 us; 250 rows of three, 4096 and 11008, rank 8, FP32 6.5 -> 5.3).  Bound by how X and dY come from memory, 134 MB in the first of these.  Stages of 64 rows through LDS, both operands read across: 128 columns, and the terms of G or H one behind
-// the other, each multiplied into the same sums.  FP16 X enters as two bfloat16 numbers, whose sum it is exactly (eight and three bits), because G may be beyond FP16's range.
+// the other, each multiplied into the same sums.
 // The rows' numbers come to LDS two stages ahead, as in w4a16_group_grad.hip.
 struct GradSide {
     const uint16_t *X, *terms;
@@ -588,7 +575,7 @@ struct GradArgs {
 
 template <int RT, int COLS>
 struct GradShape {
-    static constexpr int kSpan = 16 * RT * kGradTerms, kBuffer = (COLS + kSpan) * 128;
+    static constexpr int kSpan = 16 * RT * kTerms, kBuffer = (COLS + kSpan) * 128;
     static constexpr int kDepth = kBuffer * 3 <= 80 * 1024 - 2048 ? 3 : 2, kLds = kDepth * kBuffer + 4 * 256;
     static_assert(kLds <= 163840 - 1024, "LDS of a compute unit");
 };
@@ -598,7 +585,7 @@ __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
 {
     typedef typename ActOf<TYPE>::type Act;
     typedef GradShape<RT, COLS> Sh;
-    constexpr int kWaves = 4, J = COLS / 64, kRp = 16 * RT, kTerms = kGradTerms, kDepth = Sh::kDepth, kParts = TYPE == kTypeF16 ? 2 : 1;
+    constexpr int kWaves = 4, J = COLS / 64, kRp = 16 * RT, kDepth = Sh::kDepth;
     typedef AcrossTile<COLS, kWaves> PTile;
     typedef AcrossTile<kRp, kWaves> QTile;  // of one term
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -665,33 +652,20 @@ __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
         const uint8_t *const tile = lds + i % kDepth * Sh::kBuffer;
 #pragma unroll
         for (int step = 0; step < 2; ++step) {
-            uint4_t xv[kParts][J];
+            uint4_t xv[J][kParts<TYPE>];
 #pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const uint4_t v = PTile::read(tile, lane, wave * 16 * J + 16 * j, step);
-                if constexpr (TYPE == kTypeBF16) {
-                    xv[0][j] = v;
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float f0 = from_16bit<TYPE>((uint16_t)v[e]), f1 = from_16bit<TYPE>((uint16_t)(v[e] >> 16));
-                        const float r0 = finite(f0) ? f0 - bf16_value(bf16_down(f0)) : 0.f, r1 = finite(f1) ? f1 - bf16_value(bf16_down(f1)) : 0.f;
-                        xv[0][j][e] = (uint32_t)bf16_down(f0) | (uint32_t)bf16_down(f1) << 16;
-                        xv[1][j][e] = (uint32_t)bf16_down(r0) | (uint32_t)bf16_down(r1) << 16;
-                    }
-                }
-            }
+            for (int j = 0; j < J; ++j) bf16_parts<TYPE>(PTile::read(tile, lane, wave * 16 * J + 16 * j, step), xv[j]);
 #pragma unroll
             for (int t = 0; t < kTerms; ++t)
 #pragma unroll
                 for (int u = 0; u < RT; ++u) {
                     const uint4_t g = QTile::read(tile + PTile::kBytes + t * QTile::kBytes, lane, 16 * u, step);
 #pragma unroll
-                    for (int part = 0; part < kParts; ++part)
+                    for (int part = 0; part < kParts<TYPE>; ++part)
 #pragma unroll
                         for (int j = 0; j < J; ++j)
-                            acc[j][u] = decltype(for_a)::value ? ActBF16::mfma(ActBF16::x_operand(xv[part][j]), ActBF16::x_operand(g), acc[j][u])
-                                             : ActBF16::mfma(ActBF16::x_operand(g), ActBF16::x_operand(xv[part][j]), acc[j][u]);
+                            acc[j][u] = decltype(for_a)::value ? ActBF16::mfma(ActBF16::x_operand(xv[j][part]), ActBF16::x_operand(g), acc[j][u])
+                                             : ActBF16::mfma(ActBF16::x_operand(g), ActBF16::x_operand(xv[j][part]), acc[j][u]);
                 }
         }
     }
@@ -779,7 +753,7 @@ long long many_tiles(int M, int L) { return most_row_tiles(L + 1, M, kTileRows);
 size_t whole(size_t bytes) { return (bytes + 255) & ~(size_t)255; }
 // What a call has in its workspace, in bytes from its beginning.
 struct Space {
-    size_t offsets, order, sort, h[2], terms[2], operand, up, bytes;
+    size_t offsets, order, sort, h[2], terms[2], bytes;
     int slices[2];
 };
 Space space_of(int M, int L, int R, int K, int N, bool grad)
@@ -791,7 +765,7 @@ Space space_of(int M, int L, int R, int K, int N, bool grad)
         s.bytes = whole(row * 4 * (size_t)s.slices[0]);
         return s;
     }
-    const int sides = grad ? 2 : 1, n_terms = grad ? kGradTerms : 0;
+    const int sides = grad ? 2 : 1;
     const size_t tiles = (size_t)many_tiles(M, L);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -805,10 +779,8 @@ Space space_of(int M, int L, int R, int K, int N, bool grad)
     for (int i = 0; i < sides; ++i) {
         s.slices[i] = many_slices((long long)tiles * sides, i ? N : K);
         s.h[i] = take(row * 4 * (size_t)s.slices[i]);
-        s.terms[i] = take(row * 2 * (size_t)n_terms);
+        s.terms[i] = take(row * 2 * kTerms);
     }
-    s.operand = take(row * 2 * 3);
-    s.up = take((size_t)M * 4);
     s.bytes = at;
     return s;
 }
@@ -838,7 +810,7 @@ hipError_t expand(const LoraArgs &a, const Lists &l, const ExpandArgs &x, bool a
     return with_type(a.type, [&](auto type) {
         return with_rank(a.R, [&](auto rt) {
             constexpr int T = decltype(type)::value, RT = decltype(rt)::value, G = RT < 2 ? 1 : RT / 2, RP = 16 * RT;
-            constexpr int kLds = kTileRows * (ExpandTerms<T>::kTerms * RP * 2 + 16);
+            constexpr int kLds = kTileRows * (kTerms * RP * 2 + 16);
             if (tr == 16) return enqueue(&lora_expand_kernel<T, G, RP, false, 16>, grid, 64 * waves, 0, stream, l, x);
             return across ? enqueue(&lora_expand_kernel<T, G, RP, true, kTileRows>, grid, 64 * waves, kLds, stream, l, x)
                           : enqueue(&lora_expand_kernel<T, G, RP, false, kTileRows>, grid, 64 * waves, kLds, stream, l, x);
@@ -858,7 +830,7 @@ hipError_t launch_lora_add(const LoraArgs &a, hipStream_t stream)
     const Space s = space_of(a.M, a.L, a.R, a.K, a.N, false);
     uint8_t *const ws = static_cast<uint8_t *>(a.workspace);
     Lists l = {a.ids, nullptr, nullptr, a.M, a.L, key_bits(a.L)};
-    ExpandArgs x = {static_cast<const uint16_t *>(a.B), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), nullptr, nullptr, nullptr, a.ldbase, a.ldo, a.N, a.R, 1};
+    ExpandArgs x = {static_cast<const uint16_t *>(a.B), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), nullptr, nullptr, a.ldbase, a.ldo, a.N, a.R, 1};
     if (a.M <= kFewRows) {
         const int length = slice_length(a.K, s.slices[0]);
         x.slices = (a.K + length - 1) / length;
@@ -879,14 +851,13 @@ hipError_t launch_lora_add(const LoraArgs &a, hipStream_t stream)
     ShrinkArgsMany m = {};
     m.side[0] = side_of(s, ws, 0, a.X, a.ldx, a.A, a.K);
     m.scaling = a.scaling, m.R = a.R;
-    x.operand = m.operand = reinterpret_cast<uint16_t *>(ws + s.operand);
-    x.up = m.up = reinterpret_cast<int *>(ws + s.up);
+    x.terms = m.side[0].terms;
     const dim3 grid((unsigned)m.side[0].slices, (unsigned)tiles);
     e = with_type(a.type, [&](auto type) {
         return with_rank(a.R, [&](auto rt) {
             constexpr int RT = decltype(rt)::value;
             const hipError_t err = enqueue(&lora_shrink_kernel<decltype(type)::value, RT, false>, grid, 256, shrink_lds<RT>(), stream, l, m);
-            return err != hipSuccess ? err : enqueue(&lora_sum_kernel<decltype(type)::value, RT, false>, dim3(sum_blocks(a.M, a.R)), 256, 0, stream, l, m, 0);
+            return err != hipSuccess ? err : enqueue(&lora_sum_kernel<RT>, dim3(sum_blocks(a.M, a.R)), 256, 0, stream, l, m);
         });
     });
     return e != hipSuccess ? e : expand(a, l, x, false, kTileRows, stream);
@@ -905,7 +876,6 @@ hipError_t launch_lora_grad(const LoraArgs &a, hipStream_t stream)
     m.side[0] = side_of(s, ws, 0, a.X, a.ldx, a.A, a.K);
     m.side[1] = side_of(s, ws, 1, a.Y, a.ldy, a.B, a.N);
     m.scaling = a.scaling, m.R = a.R;
-    m.operand = reinterpret_cast<uint16_t *>(ws + s.operand), m.up = reinterpret_cast<int *>(ws + s.up);
     const int most = m.side[0].slices > m.side[1].slices ? m.side[0].slices : m.side[1].slices;
     return with_type(a.type, [&](auto type) {
         return with_rank(a.R, [&](auto rt) {
@@ -916,8 +886,8 @@ hipError_t launch_lora_grad(const LoraArgs &a, hipStream_t stream)
                 const dim3 grid((unsigned)most, (unsigned)tiles, 2);
                 err = enqueue(&lora_shrink_kernel<T, RT, true>, grid, 256, shrink_lds<RT>(), stream, l, m);
                 const dim3 sums(sum_blocks(a.M, a.R), 1, 2);
-                if (err == hipSuccess) err = enqueue(&lora_sum_kernel<T, RT, true>, sums, 256, 0, stream, l, m, 1);
-                const ExpandArgs x = {static_cast<const uint16_t *>(a.A), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), nullptr, m.operand, m.up, a.ldbase, a.ldo, a.K, a.R, 1};
+                if (err == hipSuccess) err = enqueue(&lora_sum_kernel<RT>, sums, 256, 0, stream, l, m);
+                const ExpandArgs x = {static_cast<const uint16_t *>(a.A), static_cast<const uint16_t *>(a.base), static_cast<uint16_t *>(a.out), nullptr, m.side[1].terms, a.ldbase, a.ldo, a.K, a.R, 1};
                 if (err == hipSuccess) err = expand(a, l, x, true, kTileRows, stream);  // (dX may be written over: the last launch reads X and dY only)
                 if (err != hipSuccess) return err;
             }

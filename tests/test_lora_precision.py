@@ -1,10 +1,14 @@
-"""Adapters and their gradients: sums that keep FP32's bits until the one rounding, at values where fewer would show.  Every input, product and sum here is exact in FP32 and every
-result exact in its type, so results are compared as they are: a value of H or G that loses a bit on its way into the second product changes them.
+"""Adapters and their gradients: sums that keep FP32's bits until the one rounding, at values where fewer would show.  Where a test names no bound,
+every input, product and sum is exact in FP32 and every result exact in its type, so results are compared as they are: a value of H or G that loses a bit on its way into the second product
+changes them.
 """
+import math
+
 import numpy as np
 import pytest
 
-from test_lora import KINDS, exact, lora  # noqa: F401
+from oracle import grouped_oracle as go
+from test_lora import KINDS, compare, exact, expected_add, expected_grad, lora, make  # noqa: F401
 
 gpu = pytest.mark.gpu
 
@@ -12,7 +16,7 @@ gpu = pytest.mark.gpu
 def tensor(a, kind):
     import torch
     t = torch.tensor(a, dtype=torch.float64).to(getattr(torch, kind))
-    assert torch.equal(t.double(), torch.tensor(a, dtype=torch.float64))
+    assert np.array_equal(t.double().numpy(), np.asarray(a, dtype=np.float64), equal_nan=True)
     return t.cuda()
 
 
@@ -48,3 +52,69 @@ def test_gradients_of_rows_that_nearly_cancel(lora, M, L, R, K, N, kind, grads):
     A[L - 1] = tensor(a, kind)
     _, _, dB = lora.grad(tensor(dy, kind), tensor(x, kind), A, B, ids, dtype=dtype)
     assert np.array_equal(exact(dB[L - 1]), want.T) and not exact(dB[:L - 1]).any()
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("R", [8, 16, 32, 64, 72, 128])
+@pytest.mark.parametrize("M", [3, 20, 90, 300])
+def test_a_row_of_h_far_from_its_largest_value(lora, M, R, kind):
+    """H is 2^20 in the first rank and 2^-20 in the last; half of the columns of B have the first alone, the others the last alone.  dX the same with G."""
+    import torch
+    K, N = 72, 136
+    x, a, b, y = np.zeros((M, K)), np.zeros((R, K)), np.zeros((N, R)), np.zeros((M, N))
+    x[:, 0], a[0, 0], b[0::2, 0] = 1024.0, 1024.0, 2.0 ** -10
+    x[:, 1], a[R - 1, 1], b[1::2, R - 1] = 2.0 ** -10, 2.0 ** -10, 1024.0
+    y[:, 1::2] = 2.0 ** -9
+    want = np.where(np.arange(N) % 2, 2.0 ** -9 + 2.0 ** -10, 2.0 ** 10)
+    ids = torch.zeros(M, dtype=torch.int32, device="cuda")
+    out = lora.add(tensor(y, kind), tensor(x, kind), tensor(a[None], kind), tensor(b[None], kind), ids)
+    assert np.array_equal(exact(out), np.broadcast_to(want, (M, N)))
+    # G = dY B with dY in X's place and B in A's; dX = G A with A in B's
+    dX, _, _ = lora.grad(tensor(x, kind), tensor(y, kind), tensor(b.T[None].copy(), kind), tensor(a.T[None].copy(), kind), ids, dX=tensor(y, kind), dtype=torch.float32)
+    assert np.array_equal(exact(dX), np.broadcast_to(want, (M, N)))
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("R", [8, 40, 128])
+@pytest.mark.parametrize("M", [7, 75])
+@pytest.mark.parametrize("first,second", [(2.0 ** 12, 2.0 ** -12), (2.0 ** -10, 2.0 ** 6), (1.0, 1.0)])
+def test_h_beyond_fp16_on_either_side(lora, M, R, kind, first, second):
+    """H and G of about 2^24 (beyond 65504), of 2^-20 (among FP16's numbers of fewer bits) and of ordinary size, random, within the bounds of the other tests."""
+    import torch
+    L, K, N = 3, 264, 328
+    Y, X, A, B, ids, scaling = make(M, L, R, K, N, kind, 11, "mixed")
+    X, A, B, Y = X * first, A * first, B * second, Y * second
+    assert all(bool(t.isfinite().all()) for t in (X, A, B, Y))
+    ref, bound = expected_add(exact(Y), exact(X), exact(A), exact(B), ids, exact(scaling))
+    compare(lora.add(Y, X, A, B, ids, scaling), ref, bound, "out")
+    # G of the size of H: dY like X, B like A
+    B, Y = (B / second * first), (Y / second * first)
+    A = A / first * second
+    got = lora.grad(Y, X, A, B, ids, scaling, dtype=torch.float32)
+    want = expected_grad(exact(Y), exact(X), exact(A), exact(B), ids, exact(scaling), np.zeros((M, K)))
+    for g, (r, bnd), name in zip(got, want, ("dX", "dA", "dB")):
+        compare(g, r, bnd, name)
+
+
+@gpu
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("R", [8, 24, 64, 128])
+@pytest.mark.parametrize("M", [5, 90])
+def test_infinities_of_rows_and_weights_stay_infinities(lora, M, R, kind):
+    """Every finite H is 1 and every finite weight of B 1, numbers that are one 16-bit number and zeros."""
+    K, N = 64, 136
+    x, a, b, y = np.ones((M, K)), np.full((2, R, K), 1 / K), np.ones((2, N, R)), np.ones((M, N))
+    x[1, 7], x[4, 0], b[0, 3, 0], b[0, 5, R - 1], b[1, 130, 2] = math.inf, -math.inf, math.inf, -math.inf, math.nan
+    ids = np.arange(M) % 2
+    ids[2] = -1
+    with np.errstate(invalid="ignore"):
+        want = go.lora_add(y, x, a, b, ids, [1.0, 1.0])
+    assert np.isinf(want).sum() >= 2 * N and np.isfinite(want[2]).all()
+    import torch
+    who = torch.tensor(ids, dtype=torch.int32, device="cuda")
+    args = [tensor(v, kind) for v in (y, x, a, b)]
+    np.testing.assert_array_equal(exact(lora.add(*args, who)), want)
+    dX, _, _ = lora.grad(args[1], args[0], args[3].transpose(1, 2).contiguous(), args[2].transpose(1, 2).contiguous(), who, dX=args[0])
+    np.testing.assert_array_equal(exact(dX), want)

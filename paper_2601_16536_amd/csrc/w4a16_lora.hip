@@ -601,10 +601,6 @@ __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
     int *const list = reinterpret_cast<int *>(lds + kDepth * Sh::kBuffer);
 
     float4_t acc[J][RT];  // [16 columns][16 of R]
-#pragma unroll
-    for (int i = 0; i < J; ++i)
-#pragma unroll
-        for (int u = 0; u < RT; ++u) acc[i][u] = (float4_t){0.f, 0.f, 0.f, 0.f};
     auto ask_rows = [&](int stage) __attribute__((always_inline)) {
         if (stage < stages)
             numbers_to_lds_unseen(a.order + begin + stage * kGroupStage, (uint32_t)(count - stage * kGroupStage) * 4u, (uint32_t)lane * 4u, reinterpret_cast<uint8_t *>(list + (stage & 3) * 64));
@@ -635,43 +631,60 @@ __global__ __launch_bounds__(256) void lora_grads_kernel(GradArgs a)
         asm volatile("" ::: "memory");
     };
     constexpr std::integral_constant<int, 0> kNone{};
-    if (stages > 0) {
-        ask_rows(0);
-        ask_rows(1);
-        arrive(kNone);
-        for (int d = 0; d < kDepth - 1 && d < stages; ++d) {
-            fetch(d);
-            if (d + 2 < kDepth - 1) arrive(kNone);  // (its numbers)
+    auto run = [&](auto for_a, auto odd) {
+        constexpr bool kA = decltype(for_a)::value, kOdd = decltype(odd)::value;
+#pragma unroll
+        for (int j = 0; j < J; ++j)
+#pragma unroll
+            for (int u = 0; u < RT; ++u) acc[j][u] = (float4_t){0.f, 0.f, 0.f, 0.f};
+        if (stages > 0) {
+            ask_rows(0);
+            ask_rows(1);
+            arrive(kNone);
+            for (int d = 0; d < kDepth - 1 && d < stages; ++d) fetch(d);
         }
-    }
-    auto run = [&](auto for_a) {
-    for (int i = 0; i < stages; ++i) {
-        if (kDepth == 3 && i + 1 < stages) arrive(std::integral_constant<int, kLoads>{});
-        else arrive(kNone);
-        if (i + kDepth - 1 < stages) fetch(i + kDepth - 1);
-        const uint8_t *const tile = lds + i % kDepth * Sh::kBuffer;
+        for (int i = 0; i < stages; ++i) {
+            if (kDepth == 3 && i + 1 < stages) arrive(std::integral_constant<int, kLoads>{});
+            else arrive(kNone);
+            if (i + kDepth - 1 < stages) fetch(i + kDepth - 1);
+            const uint8_t *const tile = lds + i % kDepth * Sh::kBuffer;
 #pragma unroll
-        for (int step = 0; step < 2; ++step) {
-            uint4_t xv[J][kParts<TYPE>];
+            for (int step = 0; step < 2; ++step) {
+                uint4_t xv[J][kParts<TYPE>];
 #pragma unroll
-            for (int j = 0; j < J; ++j) bf16_parts<TYPE>(PTile::read(tile, lane, wave * 16 * J + 16 * j, step), xv[j]);
+                for (int j = 0; j < J; ++j) bf16_parts<TYPE>(PTile::read(tile, lane, wave * 16 * J + 16 * j, step), xv[j]);
 #pragma unroll
-            for (int t = 0; t < kTerms; ++t)
+                for (int t = 0; t < kTerms; ++t)
 #pragma unroll
-                for (int u = 0; u < RT; ++u) {
-                    const uint4_t g = QTile::read(tile + PTile::kBytes + t * QTile::kBytes, lane, 16 * u, step);
+                    for (int u = 0; u < RT; ++u) {
+                        const uint4_t g = QTile::read(tile + PTile::kBytes + t * QTile::kBytes, lane, 16 * u, step);
 #pragma unroll
-                    for (int part = 0; part < kParts<TYPE>; ++part)
+                        for (int part = 0; part < kParts<TYPE>; ++part)
 #pragma unroll
-                        for (int j = 0; j < J; ++j)
-                            acc[j][u] = decltype(for_a)::value ? ActBF16::mfma(ActBF16::x_operand(xv[j][part]), ActBF16::x_operand(g), acc[j][u])
-                                             : ActBF16::mfma(ActBF16::x_operand(g), ActBF16::x_operand(xv[j][part]), acc[j][u]);
-                }
+                            for (int j = 0; j < J; ++j) {
+                                const auto gx = ActBF16::x_operand(kOdd && part > 0 ? finite_only(g) : g), x = ActBF16::x_operand(kOdd && t > 0 ? finite_only(xv[j][part]) : xv[j][part]);
+                                acc[j][u] = kA ? ActBF16::mfma(x, gx, acc[j][u]) : ActBF16::mfma(gx, x, acc[j][u]);
+                            }
+                    }
+            }
         }
-    }
     };
-    if (of_a) run(std::true_type{});
-    else run(std::false_type{});
+    constexpr std::false_type kPlain{};
+    constexpr std::true_type kOdd{};
+    if (of_a) run(std::true_type{}, kPlain);
+    else run(std::false_type{}, kPlain);
+    // A NaN: perhaps of an infinity and a zero behind the first of the numbers that a value has become.  Once more, such zeros meeting finite numbers only.
+    bool nan = false;
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+        for (int u = 0; u < RT; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) nan |= acc[j][u][e] != acc[j][u][e];
+    if (__syncthreads_or(nan)) {
+        if (of_a) run(std::true_type{}, kOdd);
+        else run(std::false_type{}, kOdd);
+    }
     auto put = [&](size_t at, float4_t v) {
         if constexpr (GRAD_TYPE == kTypeF32) *reinterpret_cast<float4_t *>(static_cast<float *>(s.grad) + at) = v;
         else *reinterpret_cast<uint2_t *>(static_cast<uint16_t *>(s.grad) + at) = to_16bit4<Act>(v);

@@ -118,3 +118,24 @@ def test_infinities_of_rows_and_weights_stay_infinities(lora, M, R, kind):
     np.testing.assert_array_equal(exact(lora.add(*args, who)), want)
     dX, _, _ = lora.grad(args[1], args[0], args[3].transpose(1, 2).contiguous(), args[2].transpose(1, 2).contiguous(), who, dX=args[0])
     np.testing.assert_array_equal(exact(dX), want)
+
+
+@gpu
+@pytest.mark.parametrize("grads", ["same", "float32"])
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("R", [8, 24, 64, 128])
+@pytest.mark.parametrize("M", [9, 90])
+def test_infinities_of_rows_and_gradients_stay_infinities(lora, M, R, kind, grads):
+    """Every finite value of G, H, X and dY is 1."""
+    import torch
+    K, N = 64, 128
+    x, dy, a, b = np.ones((M, K)), np.ones((M, N)), np.full((2, R, K), 1 / K), np.full((2, N, R), 1 / N)
+    x[1, 7], x[6, 9], dy[4, 0], dy[5, 3] = math.inf, -math.inf, math.inf, math.inf
+    ids = np.arange(M) % 2
+    ids[5] = -1
+    with np.errstate(invalid="ignore"):
+        want = go.lora_grad(dy, x, a, b, ids, [1.0, 1.0], np.zeros((M, K)))
+    assert all(np.isinf(w).any() for w in want) and np.isfinite(want[1][1][:, :7]).all() and np.isnan(want[1][0][:, 9]).all()
+    got = lora.grad(*[tensor(v, kind) for v in (dy, x, a, b)], torch.tensor(ids, dtype=torch.int32, device="cuda"), dtype=torch.float32 if grads == "float32" else getattr(torch, kind))
+    for g, w in zip(got, want):
+        np.testing.assert_array_equal(exact(g), w)

@@ -9,6 +9,7 @@
 #pragma once
 #include "w4a16_mx_device.h"
 #include "w4a16_group.h"
+#include "w4a16_group_place.h"
 #include <type_traits>
 
 namespace w4a16 {
@@ -39,90 +40,39 @@ __device__ __forceinline__ float from_16bit(uint16_t v)
     else return (float)__builtin_bit_cast(_Float16, v);
 }
 
-__device__ __forceinline__ int clamp_to(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
-
-// The rows of group g; E: those behind the last group, E + 1: those ahead of the first.
-__device__ __forceinline__ void group_range(const int32_t *offsets, int E, int count, int g, int *begin, int *end)
-{
-    const int b = g <= E ? clamp_to(offsets[g], 0, count) : 0;
-    *begin = b;
-    *end = g == E ? count : clamp_to(offsets[g < E ? g + 1 : 0], b, count);
-}
-
-// Which row tile of which group this workgroup has.  Row tiles are numbered group by group; how many there are only the device knows, so the launch has as many
-// workgroups as there could be, and those past the last tile have none.  XCD x (workgroup mod 8) takes the x-th eighth of the (row tile, column tile)
-// pairs that there are, in order: neighbours read the same rows and weights through one L2.
-struct RowTile {
-    int group, row0, end;  // rows row0 .. min(end, row0 + tile) - 1
-    int col;               // column tile
-};
-constexpr int kBlockRows = 4;
+// The workgroup's tile (w4a16_group_place.h): a sum over the groups' tiles by all threads, some 2 us.
 template <int THREADS>
 __device__ __forceinline__ bool find_row_tile(const int32_t *offsets, int E, int groups, int count, int tile_rows, int cols, RowTile *found)
 {
     constexpr int kWaves = THREADS / 64;
-    __shared__ int s[kWaves + 4];
-    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6, per = (groups + THREADS - 1) / THREADS;
-    int tiles = 0;
-    for (int i = 0; i < per; ++i) {
-        const int g = tid * per + i;
-        if (g < groups) {
-            int b, e;
-            group_range(offsets, E, count, g, &b, &e);
-            tiles += (e - b + tile_rows - 1) / tile_rows;
-        }
-    }
-    int upto = tiles;
+    __shared__ TileCount sums[kWaves];
+    __shared__ RowTile mine;
+    const GroupTiling g = {offsets, E, groups, count, tile_rows, cols};
+    const int tid = (int)threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const TileCount tiles = tiles_of_thread(g, tid, THREADS);
+    TileCount upto = tiles;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
-        const int v = __shfl_up(upto, d, 64);
+        const TileCount v = __shfl_up(upto, d, 64);
         if (lane >= d) upto += v;
     }
-    if (lane == 63) s[wave] = upto;
+    if (lane == 63) sums[wave] = upto;
     __syncthreads();
-    int before = 0, total = 0;
+    TileCount before = 0, total = 0, pair;
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) before += s[w];
-        total += s[w];
+        if (w < wave) before += sums[w];
+        total += sums[w];
     }
-    const long long pairs = (long long)total * cols, eighth = (pairs + kPlaceXcds - 1) / kPlaceXcds;
-    const long long in = blockIdx.x / kPlaceXcds, id = (long long)(blockIdx.x % kPlaceXcds) * eighth + in;
-    if (in >= eighth || id >= pairs) return false;
-    const int tile = (int)(id / cols);
-    int at = before + upto - tiles;
-    if (tile >= at && tile < at + tiles)
-        for (int i = 0; i < per; ++i) {
-            const int g = tid * per + i;
-            if (g >= groups) break;
-            int b, e;
-            group_range(offsets, E, count, g, &b, &e);
-            const int n = (e - b + tile_rows - 1) / tile_rows;
-            if (tile < at + n) {
-                // In a group, kBlockRows row tiles at a time, column by column.
-                const long long in_group = id - (long long)at * cols;
-                const int block = (int)(in_group / ((long long)kBlockRows * cols)), high = min(kBlockRows, n - block * kBlockRows);
-                const int rest = (int)(in_group - (long long)block * kBlockRows * cols);
-                s[kWaves] = g;
-                s[kWaves + 1] = b + (block * kBlockRows + rest % high) * tile_rows;
-                s[kWaves + 2] = e;
-                s[kWaves + 3] = rest / high;
-                break;
-            }
-            at += n;
-        }
+    if (!pair_of_block(total, cols, blockIdx.x, &pair)) return false;
+    RowTile t;
+    if (tile_of_thread(g, tid, THREADS, before + upto - tiles, tiles, pair, &t)) mine = t;
     __syncthreads();
-    found->group = __builtin_amdgcn_readfirstlane(s[kWaves]);
-    found->row0 = __builtin_amdgcn_readfirstlane(s[kWaves + 1]);
-    found->end = __builtin_amdgcn_readfirstlane(s[kWaves + 2]);
-    found->col = __builtin_amdgcn_readfirstlane(s[kWaves + 3]);
+    found->group = __builtin_amdgcn_readfirstlane(mine.group);
+    found->row0 = __builtin_amdgcn_readfirstlane(mine.row0);
+    found->end = __builtin_amdgcn_readfirstlane(mine.end);
+    found->col = __builtin_amdgcn_readfirstlane(mine.col);
     return true;
-}
-// At most so many row tiles.
-inline long long most_row_tiles(long long groups, long long count, int tile_rows)
-{
-    if (groups > count) groups = count;
-    return (count + groups * (tile_rows - 1)) / tile_rows;
 }
 
 __device__ __forceinline__ void load_to_lds(const uint8_t *from, uint8_t *to)

@@ -87,8 +87,8 @@ __device__ __forceinline__ uint4_t load16(const uint16_t *p, bool have)
 
 // ---- shrink of few rows: H[s][i][r] = scaling * sum over slice s of k of X[i, k] W[r, k] ----
 //
-// A workgroup has 16 rows, a slice of k and all of R; its four waves take steps of 32 k in turn and their sums meet in LDS, in their order.  ACROSS: W is B [K, R] (K the
-// sum's length here), brought to LDS by a wave for itself and read across.  The MFMA's row operand is W, so that a lane has four neighbouring r.
+// A workgroup has 16 rows, a slice of k and all of R; its four waves take steps of 32 k in turn and their sums meet in LDS, in their order.  The MFMA's row operand is W, so that a lane has
+// four neighbouring r.
 constexpr int kShrinkUnroll = 4;
 
 struct ShrinkArgs {
@@ -99,83 +99,50 @@ struct ShrinkArgs {
     int K, R, slice;  // slice: a multiple of 128
 };
 
-template <int TYPE, int RT, bool ACROSS>
+template <int TYPE, int RT>
 __global__ __launch_bounds__(256) void lora_few_shrink_kernel(Lists l, ShrinkArgs a)
 {
     typedef typename ActOf<TYPE>::type Act;
-    constexpr int kRp = 16 * RT, kWaves = 4, TR = 16;
+    constexpr int kRp = 16 * RT, kWaves = 4, TR = 16, kStep = 32 * kWaves;
     __shared__ int rows[TR];
     __shared__ __attribute__((aligned(16))) float4_t sums[(kWaves - 1) * RT * 64];
-    __shared__ __attribute__((aligned(16))) uint16_t across[ACROSS ? kWaves * 32 * kRp : 8];
     int adapter, count;
     if (!adapter_tile<TR>(l, (int)blockIdx.x, rows, &adapter, &count) || adapter == l.L) return;
     const int lane = (int)threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), c = lane & 15, p = lane >> 4;
-    const int row = c;
-    const uint16_t *const x = a.X + (size_t)rows[min(row, count - 1)] * (size_t)a.ldx;
+    const uint16_t *const x = a.X + (size_t)rows[min(c, count - 1)] * (size_t)a.ldx;
     const uint16_t *const w = a.W + (size_t)adapter * (size_t)a.R * (size_t)a.K;
     const int k0 = (int)blockIdx.y * a.slice, k1 = min(a.K, k0 + a.slice);
-    constexpr int kStep = 32 * kWaves;
-    uint16_t *const mine = across + (ACROSS ? wave * 32 * kRp : 0);
 
     float4_t acc[RT];
 #pragma unroll
     for (int t = 0; t < RT; ++t) acc[t] = (float4_t){0.f, 0.f, 0.f, 0.f};
-        for (int k = k0 + wave * 32; k < k1; k += kStep * kShrinkUnroll) {
-            uint4_t xv[kShrinkUnroll], wv[kShrinkUnroll][RT];
+    for (int k = k0 + wave * 32; k < k1; k += kStep * kShrinkUnroll) {
+        uint4_t xv[kShrinkUnroll], wv[kShrinkUnroll][RT];
 #pragma unroll
-            for (int u = 0; u < kShrinkUnroll; ++u) {
-                const int kk = k + u * kStep;
-                const bool have = kk + 8 * p < k1;
-                xv[u] = load16(x + (have ? kk + 8 * p : 0), have);
+        for (int u = 0; u < kShrinkUnroll; ++u) {
+            const int kk = k + u * kStep;
+            const bool have = kk + 8 * p < k1;
+            xv[u] = load16(x + (have ? kk + 8 * p : 0), have);
 #pragma unroll
-                for (int t = 0; t < RT; ++t) {
-                    if constexpr (ACROSS) {  // pieces of the 32 rows of B
-                        const int q = t * 64 + lane, n = kk + q / (2 * RT), r = q % (2 * RT) * 8;
-                        const bool in = n < k1 && r < a.R;
-                        wv[u][t] = load16(w + (in ? (size_t)n * (size_t)a.R + (size_t)r : 0), in);
-                    } else {
-                        wv[u][t] = load16(w + (size_t)min(16 * t + c, a.R - 1) * (size_t)a.K + (size_t)(have ? kk + 8 * p : 0), have);
-                    }
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < kShrinkUnroll; ++u) {
-                if constexpr (ACROSS) {
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        const int q = t * 64 + lane;
-                        *reinterpret_cast<uint4_t *>(mine + q / (2 * RT) * kRp + q % (2 * RT) * 8) = wv[u][t];
-                    }
-                    const uint16_t *const at = mine + (8 * p + (c >> 2)) * kRp + 4 * (c & 3);
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) {
-                        union {
-                            short4_t s[2];
-                            uint4_t u;
-                        } v;
-                        v.s[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(at + 16 * t));
-                        v.s[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4_t)(at + 4 * kRp + 16 * t));
-                        wv[u][t] = v.u;
-                    }
-                }
-#pragma unroll
-                for (int t = 0; t < RT; ++t) acc[t] = Act::mfma(Act::x_operand(wv[u][t]), Act::x_operand(xv[u]), acc[t]);
-            }
+            for (int t = 0; t < RT; ++t) wv[u][t] = load16(w + (size_t)min(16 * t + c, a.R - 1) * (size_t)a.K + (size_t)(have ? kk + 8 * p : 0), have);
         }
-    {  // the waves' sums, in their order
-        if (wave > 0)
 #pragma unroll
-            for (int t = 0; t < RT; ++t) sums[((wave - 1) * RT + t) * 64 + lane] = acc[t];
-        __syncthreads();
-        if (wave > 0) return;
+        for (int u = 0; u < kShrinkUnroll; ++u)
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int v = 0; v < kWaves - 1; ++v) acc[t] += sums[(v * RT + t) * 64 + lane];
+            for (int t = 0; t < RT; ++t) acc[t] = Act::mfma(Act::x_operand(wv[u][t]), Act::x_operand(xv[u]), acc[t]);
     }
-    if (row >= count) return;
+    if (wave > 0)
+#pragma unroll
+        for (int t = 0; t < RT; ++t) sums[((wave - 1) * RT + t) * 64 + lane] = acc[t];
+    __syncthreads();
+    if (wave > 0) return;
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int v = 0; v < kWaves - 1; ++v) acc[t] += sums[(v * RT + t) * 64 + lane];
+    if (c >= count) return;
     const float s = a.scaling ? a.scaling[adapter] : 1.0f;
-    float *const h = a.H + ((size_t)blockIdx.y * (size_t)l.M + (size_t)rows[row]) * kRp + 4 * p;
+    float *const h = a.H + ((size_t)blockIdx.y * (size_t)l.M + (size_t)rows[c]) * kRp + 4 * p;
 #pragma unroll
     for (int t = 0; t < RT; ++t) *reinterpret_cast<float4_t *>(h + 16 * t) = acc[t] * s;
 }
@@ -851,7 +818,7 @@ hipError_t launch_lora_add(const LoraArgs &a, hipStream_t stream)
         const ShrinkArgs f = {static_cast<const uint16_t *>(a.X), static_cast<const uint16_t *>(a.A), reinterpret_cast<float *>(ws), a.scaling, a.ldx, a.K, a.R, length};
         const dim3 grid((unsigned)few_tiles(a.M, a.L), (unsigned)x.slices);
         const hipError_t e = with_type(a.type, [&](auto type) {
-            return with_rank(a.R, [&](auto rt) { return enqueue(&lora_few_shrink_kernel<decltype(type)::value, decltype(rt)::value, false>, grid, 256, 0, stream, l, f); });
+            return with_rank(a.R, [&](auto rt) { return enqueue(&lora_few_shrink_kernel<decltype(type)::value, decltype(rt)::value>, grid, 256, 0, stream, l, f); });
         });
         return e != hipSuccess ? e : expand(a, l, x, false, 16, stream);
     }

@@ -60,12 +60,19 @@ def check_ints(t, name: str) -> None:
         raise TypeError("%s must be a contiguous CUDA tensor of dtype torch.int32" % name)
 
 
+def check_sizes(shape, name: str) -> None:
+    """Sizes that the library's 32-bit arguments hold; it refuses by itself what is smaller and still too large."""
+    if any(n >= 1 << 31 for n in shape):
+        raise ValueError("%s %r has a size past 32 bits" % (name, tuple(shape)))
+
+
 def matrix(X, name: str, like=None):
     """(rows, width, leading dimension) of a matrix whose rows are contiguous and 16-byte aligned; `like`: of the same type."""
     if not X.is_cuda or (like is not None and X.dtype is not like.dtype):
         raise TypeError("%s must be a CUDA tensor%s" % (name, "" if like is None else " of dtype %s" % like.dtype))
     if X.dim() != 2:
         raise ValueError("%s must be a matrix, not %r" % (name, tuple(X.shape)))
+    check_sizes(X.shape, name)
     return mx.rows_of(X, name)
 
 
@@ -126,6 +133,7 @@ def _rows(rows, top_k: int, count):
             raise ValueError("top_k goes with rows")
         return
     check_ints(rows, "rows")
+    check_sizes((top_k,), "top_k")
     if top_k < 1 or (count is not None and rows.numel() != count):
         raise ValueError("rows must have %s values, top_k be at least 1" % count)
 
@@ -145,6 +153,7 @@ def gemm(X, W, offsets, rows=None, top_k: int = 1, transposed: bool = False, out
     x_rows, K, ldx = matrix(X, "X")
     if W.dim() != 3 or not W.is_cuda or W.dtype is not X.dtype:
         raise TypeError("W must be a CUDA tensor [E, %s] of dtype %s" % ("K, N" if transposed else "N, K", X.dtype))
+    check_sizes(W.shape, "W")
     E, w_rows, w_width = W.shape
     N = w_width if transposed else w_rows
     if (w_rows if transposed else w_width) != K:

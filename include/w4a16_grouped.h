@@ -5,14 +5,14 @@
  *
  * All data pointers are DEVICE pointers owned by the caller.  Matrices are FP16 or BF16 (`dtype`), their values contiguous along a
  * row; a leading dimension (ld) is the values from a row to the next.  Rows are 16-byte aligned, so dimensions along rows and ld are multiples
- * of 8 (ld at most 2^21).  ids, offsets, rows and FP32 arrays need no more than their type's alignment, workspaces 256 bytes.  Calls only enqueue
+ * of 8 (ld at most 2^21).  ids, offsets, rows and scaling need no more than their type's alignment, gradients of either type 16 bytes, workspaces 256.  Calls only enqueue
  * work on `stream` (a hipStream_t, NULL = the default stream); none allocates, waits or keeps anything, so all may be captured into a HIP graph,
  * and calls on different streams may overlap, each with its own workspace and outputs.  Outputs may not overlap inputs or each other, but where
  * it is said.  No rows: W4A16_OK; nothing is launched but what w4a16_grouped_gemm_grad and w4a16_lora_grad need to write their zeros, and
  * w4a16_grouped_sort its offsets.
  *
  * Errors: a w4a16_status; on any error nothing is launched.  Sums are FP32, with one rounding to the output's type; results are
- * bitwise reproducible for fixed arguments.
+ * bitwise reproducible for fixed arguments.  Infinities and NaN are what the formulas make of them, in the rows and groups that have them.
  */
 #ifndef W4A16_GROUPED_H
 #define W4A16_GROUPED_H
@@ -40,7 +40,7 @@ int w4a16_grouped_sort(const int32_t *ids, long long count, int E, int32_t *offs
  *   X [x_rows, K], ldx;  Y [count, N], ldy;  offsets int32 [E + 1], ascending, within 0 .. count
  *   W: group e begins e * stride_w values on; [N, K] with leading dimension ldw or, `transposed` nonzero, [K, N]: Y[i] = X[r(i)] W_e, which is
  *   also the gradient of the first form's rows, with the gradients of its outputs as X.
- * Rows of Y that no group has are left as they are, or set to 0 with `fill` nonzero.  A row number outside of X stands for a row of zeros; offsets that
+ * Rows of Y that no group has are left as they are, or set to 0 with `fill` nonzero.  A row number outside of X stands for a row of zeros and makes one; offsets that
  * descend or leave the range make some rows' values undefined and touch no memory outside of the arguments.
  * E <= 1024, K <= 131072, N <= 2^20, count and x_rows < 2^30; without `rows` x_rows >= count.
  */
@@ -56,7 +56,10 @@ int w4a16_grouped_gemm(const void *X, int dtype, long long x_rows, long long ldx
 int w4a16_grouped_gemm_grad(const void *dY, int dtype, long long ldy, const void *X, long long x_rows, long long ldx, const int32_t *rows, int top_k,
                             const int32_t *offsets, int E, long long count, int N, int K, void *dW, int grad_dtype, int accumulate, void *stream);
 
-/* The tile that the products above take for these sizes: rows of a group and columns (of Y; of dW: its rows and columns). */
+/*
+ * The tile that the products above take for these sizes: rows of a group and columns (of Y; of dW: its rows and columns).  Where it is 256 x 256, rows gathered
+ * from an X of x_rows * ldx values of 2 GiB or more go in tiles of 128 x 128.
+ */
 int w4a16_grouped_query_tile(int E, long long count, int N, int K, int transposed, int grad, int *tile_rows, int *tile_cols);
 
 /*
@@ -72,7 +75,7 @@ int w4a16_lora_add(const void *Y, long long ldy, const void *X, int dtype, long 
                    const float *scaling, int M, int L, int R, int K, int N, void *out, long long ldo, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
- * Its gradients, with H = s_a X A_a^T and G = s_a dY B_a in FP32:
+ * Its gradients, with H = s_a X A_a^T and G = s_a dY B_a in FP32 (all of its 24 bits go into the products below, for gradients of either type):
  *   dX_out[i] = dX[i] + G[i] A_a   (dX: what the shared projection passed back, or NULL: 0; dX_out may be dX, with the same ld)
  *   dA_a = sum over the adapter's rows of G[i]^T X[i],  dB_a = sum of dY[i]^T H[i]   (zeros for an adapter without rows)
  * dA [L, R, K] and dB [L, N, R], contiguous, of type `grad_dtype`: `dtype`'s or W4A16_F32.  Workspace with `grad` nonzero.

@@ -8,6 +8,8 @@ include/w4a16_grouped.h; argument marshalling only, as in `binding`.
 
     dY -> dX = grouped.gemm(dY, W, offsets, transposed=True)         # [T top_k, K], by expert; a token's gradient is the sum of its rows
     dW = grouped.gemm_grad(dY, X, offsets, rows=order, top_k=top_k)  # [E, N, K]
+
+A call goes to the current stream, or to `stream`; new results come from torch's allocator on the current one.  With another `stream` bring `out` too, or keep the results until it is done.
 """
 from __future__ import annotations
 
@@ -77,7 +79,8 @@ def matrix(X, name: str, like=None):
 
 
 def query_tile(E: int, count: int, N: int, K: int, transposed: bool = False, grad: bool = False) -> tuple:
-    """(rows of a group, columns) of the tiles that gemm, or with `grad` gemm_grad (rows and columns of dW), takes for these sizes."""
+    """(rows of a group, columns) of the tiles that gemm, or with `grad` gemm_grad (rows and columns of dW), takes for these sizes; where it is (256, 256), (128, 128) for rows
+    gathered from an X of 2 GiB or more."""
     rows, cols = ctypes.c_int(), ctypes.c_int()
     _check(lib().w4a16_grouped_query_tile(E, count, N, K, int(transposed), int(grad), ctypes.byref(rows), ctypes.byref(cols)), "w4a16_grouped_query_tile")
     return rows.value, cols.value

@@ -7,7 +7,10 @@ include/w4a16_grouped.h; argument marshalling only, as in `binding`.
     dX, dA, dB = lora.grad(dY, X, A, B, ids, scaling, dX=dX)   # dX: what the shared projection passed back
 
 A [L, R, K] and B [L, N, R] hold L adapters of rank R (a multiple of 8, at most 128; shorter ones end in rows of A and columns of B of zeros), ids int32 [M]
-names each row's; a row whose id is outside of 0 .. L - 1 has none.
+names each row's; a row whose id is outside of 0 .. L - 1 has none.  Streams: as in `grouped`.
+
+The gradient of a shared projection's rows is not this library's: its projections on 4-bit weights have no transposed form, so `dX` comes from the caller (grouped.gemm with `transposed` gives it
+for 16-bit weights).
 """
 from __future__ import annotations
 

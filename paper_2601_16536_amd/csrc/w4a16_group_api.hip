@@ -65,7 +65,7 @@ int w4a16_grouped_gemm(const void *X, int dtype, long long x_rows, long long ldx
                        void *stream)
 {
     clear_hip_error();
-    int rc = check_groups(dtype, E, count, N, K, rows, top_k, x_rows);
+    int rc = check_groups(dtype, E, count, N, K, count > 0 ? rows : nullptr, top_k, x_rows);
     if (rc == W4A16_ERR_SHAPE) return rc;
     if (count == 0) return W4A16_OK;
     if (!X || !W || !offsets || !Y) return W4A16_ERR_NULL;

@@ -38,3 +38,16 @@ def test_sizes_past_32_bits_are_refused():
                 lambda: lora.grad(Tensor((4, 8), half), Tensor((4, 8), half), Tensor((1, big, 8), half), Tensor((1, 8, big), half), rows)):
         with pytest.raises(ValueError, match="past 32 bits"):
             bad()
+
+
+def test_no_rows_of_an_x_without_rows_is_no_error():
+    """A batch of no tokens, its (empty) list of rows in a buffer that has an address."""
+    import os
+    from paper_2601_16536_amd import binding as b, build, grouped
+    if not os.path.exists(b.LIB_PATH):
+        build.build(verbose=False)
+    L = grouped.lib()
+    # X, type, x_rows, ldx, rows, top_k, W, stride_w, ldw, transposed, offsets, E, count, N, K, Y, ldy, fill, stream
+    for rows, top_k in ((0, 1), (64, 2), (64, 1)):
+        assert L.w4a16_grouped_gemm(0, 0, 0, 64, rows, top_k, 16, 2048, 64, 0, 16, 2, 0, 32, 64, 0, 32, 1, 0) == b.OK
+    assert L.w4a16_grouped_gemm(16, 0, 0, 64, 64, 2, 16, 2048, 64, 0, 16, 2, 4, 32, 64, 16, 32, 1, 0) == b.ERR_SHAPE

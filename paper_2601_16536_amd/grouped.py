@@ -62,10 +62,9 @@ def check_ints(t, name: str) -> None:
         raise TypeError("%s must be a contiguous CUDA tensor of dtype torch.int32" % name)
 
 
-def check_sizes(shape, name: str) -> None:
-    """Sizes that the library's 32-bit arguments hold; it refuses by itself what is smaller and still too large."""
-    if any(n >= 1 << 31 for n in shape):
-        raise ValueError("%s %r has a size past 32 bits" % (name, tuple(shape)))
+def too_large(name: str, shape) -> ValueError:
+    """For sizes that the library's 32-bit arguments do not hold; it refuses by itself what is smaller and still too large."""
+    return ValueError("%s %r has a size past 32 bits" % (name, tuple(shape)))
 
 
 def matrix(X, name: str, like=None):
@@ -74,8 +73,10 @@ def matrix(X, name: str, like=None):
         raise TypeError("%s must be a CUDA tensor%s" % (name, "" if like is None else " of dtype %s" % like.dtype))
     if X.dim() != 2:
         raise ValueError("%s must be a matrix, not %r" % (name, tuple(X.shape)))
-    check_sizes(X.shape, name)
-    return mx.rows_of(X, name)
+    found = rows, width, _ = mx.rows_of(X, name)
+    if (rows | width) >> 31:
+        raise too_large(name, X.shape)
+    return found
 
 
 def query_tile(E: int, count: int, N: int, K: int, transposed: bool = False, grad: bool = False) -> tuple:
@@ -136,7 +137,8 @@ def _rows(rows, top_k: int, count):
             raise ValueError("top_k goes with rows")
         return
     check_ints(rows, "rows")
-    check_sizes((top_k,), "top_k")
+    if top_k >> 31 > 0:
+        raise too_large("top_k", (top_k,))
     if top_k < 1 or (count is not None and rows.numel() != count):
         raise ValueError("rows must have %s values, top_k be at least 1" % count)
 
@@ -156,8 +158,9 @@ def gemm(X, W, offsets, rows=None, top_k: int = 1, transposed: bool = False, out
     x_rows, K, ldx = matrix(X, "X")
     if W.dim() != 3 or not W.is_cuda or W.dtype is not X.dtype:
         raise TypeError("W must be a CUDA tensor [E, %s] of dtype %s" % ("K, N" if transposed else "N, K", X.dtype))
-    check_sizes(W.shape, "W")
     E, w_rows, w_width = W.shape
+    if (E | w_rows | w_width) >> 31:
+        raise too_large("W", W.shape)
     N = w_width if transposed else w_rows
     if (w_rows if transposed else w_width) != K:
         raise ValueError("X %r does not fit W %r%s" % (tuple(X.shape), tuple(W.shape), ", transposed" if transposed else ""))

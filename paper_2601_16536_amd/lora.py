@@ -52,10 +52,11 @@ def _check(X, A, B, ids, scaling, other, name: str):
     for t, n in ((A, "A"), (B, "B")):
         if not (t.is_cuda and t.dtype is X.dtype and t.is_contiguous() and t.dim() == 3):
             raise TypeError("%s must be a contiguous CUDA tensor of three dimensions and dtype %s" % (n, X.dtype))
-        grouped.check_sizes(t.shape, n)
     L, R, _ = A.shape
     if M2 != M or A.shape[2] != K or tuple(B.shape) != (L, N, R):
         raise ValueError("X %r, %s %r, A %r and B %r do not fit each other" % (tuple(X.shape), name, tuple(other.shape), tuple(A.shape), tuple(B.shape)))
+    if (L | R) >> 31:
+        raise grouped.too_large("A", A.shape)
     grouped.check_ints(ids, "ids")
     if ids.numel() != M:
         raise ValueError("ids must have %d values, not %d" % (M, ids.numel()))

@@ -40,7 +40,7 @@ int w4a16_grouped_sort(const int32_t *ids, long long count, int E, int32_t *offs
  *   X [x_rows, K], ldx;  Y [count, N], ldy;  offsets int32 [E + 1], ascending, within 0 .. count
  *   W: group e begins e * stride_w values on; [N, K] with leading dimension ldw or, `transposed` nonzero, [K, N]: Y[i] = X[r(i)] W_e, which is
  *   also the gradient of the first form's rows, with the gradients of its outputs as X.
- * Rows of Y that no group has are left as they are, or set to 0 with `fill` nonzero.  A row number outside of X stands for a row of zeros and makes one; offsets that
+ * Rows of Y that no group has are left as they are, or set to 0 with `fill` nonzero.  A row number outside of X stands for a row of zeros (Y's is 0 then); offsets that
  * descend or leave the range make some rows' values undefined and touch no memory outside of the arguments.
  * E <= 1024, K <= 131072, N <= 2^20, count and x_rows < 2^30; without `rows` x_rows >= count.
  */

@@ -525,7 +525,7 @@ __global__ __launch_bounds__(256, G == 4 ? 2 : (TYPE == kTypeF16 ? 4 : 5) - G) v
 // ---- grads: dA[r, k] = sum over the adapter's rows of G[i][r] X[i, k];  dB[n, r] = sum of dY[i, n] H[i][r] ----
 //
 // A workgroup has 128 columns of X or dY and all of R, a wave 32 columns; half of them up to rank 32 where there are few workgroups, as adapters' rows differ (250 rows of three adapters,
-// K = 4096, N = 11008, rank 8, FP32 7.6 -> 6.1 us; 4096 rows of four, K = N = 8192, rank 32, four times as many workgroups: 55 either way).  Bound by how X and dY come from memory, 134 MB in the
+// K = 4096, N = 11008, rank 8, FP32, 708 of them, 7.6 -> 6.1 us; 4096 rows of four, K = N = 8192, rank 32, 1024 workgroups of 64 columns: 55 either way).  Bound by how X and dY come from memory, 134 MB in the
 // second of these, and by the three numbers of G and H beside them (of two, that lost bits, 40 us).  Stages of 64 rows through LDS, both operands read across: 128 columns, and the terms of G or H
 // one behind the other, each multiplied into the same sums.
 // The rows' numbers come to LDS two stages ahead, as in w4a16_group_grad.hip.
